@@ -289,6 +289,90 @@ etr_status etr_moe_forward_profiled(const etr_config* cfg, const void* x, const 
                                     int32_t* slot_token, int32_t* counts,
                                     void* ws, size_t ws_bytes, void* stream, void* const* events);
 
+/* ---- the block around the layer, rows sorted by expert --------------- */
+
+/* The join of a block's output with the residual stream and the norm in front of the next block, in one pass:
+ *   x_out[t] = residual_scale x[t] + block_scale gate[t] P(y[t]),   P(y) = N(y) .* w_post  (y itself without w_post)
+ *   h[t]     = N(x_out[t]) .* w_pre,                                N(v) = v / sqrt(mean(v^2) + eps)
+ * h is computed from x_out as it is stored, so the pass gives what its two halves give one after the other.
+ *   y = NULL:     no block joins (the first norm of a stack): h comes from x; x_out, gate and w_post must be NULL
+ *   w_pre = NULL: no norm follows (the last join); h must be NULL too.  One of y and w_pre is required.
+ * Limits: d % 8 == 0 and rows of at most 64 KiB (ETR_ERR_UNSUPPORTED); eps > 0 and finite scales (ETR_ERR_SHAPE). */
+typedef struct {
+    int32_t T, d;
+    int32_t dtype;          /* etr_dtype of x, y, x_out, h and their gradients */
+    float eps, residual_scale, block_scale;
+} etr_norm_config;
+
+/*   x [T][d], y [T][d] dtype in; gate [T] fp32 in, optional (1 everywhere); w_post, w_pre [d] fp32 in, optional
+ *   x_out [T][d], h [T][d] dtype out; x_out may be x */
+etr_status etr_block_norm(const etr_norm_config* cfg, const void* x, const void* y, const float* gate,
+                          const float* w_post, const float* w_pre, void* x_out, void* h, void* stream);
+
+/* Scratch of etr_block_norm_backward (partial sums of the weights' gradients). 0 for an invalid config. */
+size_t etr_norm_workspace_bytes(const etr_norm_config* cfg);
+
+/* Gradient of etr_block_norm for the upstream gradients dx_out (along the stream) and dh, with r = dx_out + dN(x_out)^T (dh .* w_pre):
+ *   dx = residual_scale r;  dy = dP(y)^T (block_scale gate r);  dgate[t] = block_scale <r[t], P(y[t])>
+ *   dw_post = sum_t block_scale gate r .* N(y);  dw_pre = sum_t dh .* N(x_out)      (overwritten, fixed summation order)
+ *   x_out, y, gate, w_post, w_pre: as in the forward call (x_out: what it wrote; without y: its x; may be NULL without w_pre)
+ *   dx_out [T][d] dtype in, optional (zero); dh [T][d] dtype in, with w_pre only (required then)
+ *   dx [T][d], dy [T][d] dtype out; dx may be dx_out; without y dx = r and dy must be NULL
+ *   dgate [T], dw_post [d], dw_pre [d] fp32 out, each optional; with gate, w_post, w_pre only */
+etr_status etr_block_norm_backward(const etr_norm_config* cfg, const void* x_out, const void* y, const float* gate,
+                                   const float* w_post, const float* w_pre, const void* dx_out, const void* dh, void* dx,
+                                   void* dy, float* dgate, float* dw_post, float* dw_pre, void* ws, size_t ws_bytes,
+                                   void* stream);
+
+/* Rows sorted by expert, without padding: the pairs (token, place in its list) of a routing in the order (expert, token,
+ * place) are rows 0 ... offsets[E] of a matrix; what etr_dispatch and etr_combine do in buffers of fixed capacity, for layers
+ * that drop nothing and for exchanges that send each expert's rows as one piece. */
+typedef struct {
+    int32_t T, k, E, d;     /* k <= E <= 64, d % 8 == 0, rows of at most 128 KiB, T * k <= 2^30 */
+    int32_t dtype;          /* etr_dtype of the rows */
+    int32_t gate_norm;      /* 0: weight of a pair = gate[t][e]; 1: divided by their sum over the token's pairs in use */
+} etr_sort_config;
+
+/* Scratch of etr_sort_tokens. 0 for an invalid config. */
+size_t etr_sort_workspace_bytes(const etr_sort_config* cfg);
+
+/* The tables.  A pair is in use if its expert is in [0, E) and, with slot_of, if slot_of[t][e] >= 0 (a selection under a
+ * capacity has kept it).
+ *   topk_expert [T][k] int32 in;  slot_of [T][E] int32 in, optional
+ *   offsets [E+1] int32 out: expert e has rows offsets[e] ... offsets[e+1] - 1
+ *   row_of [T][k] int32 out: row of the pair, -1 if not in use
+ *   pair_of [T*k] int32 out: t * k + place of a row's pair; -1 from row offsets[E] on */
+etr_status etr_sort_tokens(const etr_sort_config* cfg, const int32_t* topk_expert, const int32_t* slot_of, int32_t* offsets,
+                           int32_t* row_of, int32_t* pair_of, void* ws, size_t ws_bytes, void* stream);
+
+/* xs[row_of[t][j]] = x[t] for the pairs in use; rows from offsets[E] on are left untouched.  x [T][d], xs [T*k][d]. */
+etr_status etr_sort_rows(const etr_sort_config* cfg, const void* x, const int32_t* row_of, void* xs, void* stream);
+
+/* Its gradient: dx[t] = sum_j dxs[row_of[t][j]], ascending j, fp32, rounded once; zero for a token without a pair. */
+etr_status etr_sort_rows_backward(const etr_sort_config* cfg, const void* dxs, const int32_t* row_of, void* dx,
+                                  void* stream);
+
+/* out[t] = sum_j weight[t][j] ys[row_of[t][j]], ascending j, fp32, rounded once; zero for a token without a pair.
+ *   ys [T*k][d]; gate [T][E] fp32; topk_expert, row_of as above; out [T][d] */
+etr_status etr_unsort_rows(const etr_sort_config* cfg, const void* ys, const float* gate, const int32_t* topk_expert,
+                           const int32_t* row_of, void* out, void* stream);
+
+/* Its gradients: dys[row_of[t][j]] = weight[t][j] dout[t] (rows from offsets[E] on untouched) and dgate [T][E] fp32, the
+ * gradient with respect to gate (through the division with gate_norm), 0 where the token has no pair in use; an expert that a token
+ * lists twice gets both parts. */
+etr_status etr_unsort_rows_backward(const etr_sort_config* cfg, const void* dout, const void* ys, const float* gate,
+                                    const int32_t* topk_expert, const int32_t* row_of, void* dys, float* dgate,
+                                    void* stream);
+
+/* Gradient of etr_route with respect to the tokens, for the gradient dgate [T][E] of its gates (etr_moe_backward has it
+ * inside; layers put together from the calls above need it by itself):
+ *   dscore = gate .* (dgate - <dgate, gate>);   dx[t] = dx_add[t] + sum_e dscore[t][e] d score[t][e] / d x[t]
+ *   x [T][d], w_emb [E][d/D], score, gate [T][E]: of the forward call; dx_add [T][d] dtype in, optional (zero): the gradient
+ *   that reaches x by the other ways; dx [T][d] dtype out; may be dx_add.  A zero-norm token gets dx_add.
+ * E * (d/D) * 4 bytes must fit in 120 KiB (ETR_ERR_UNSUPPORTED). */
+etr_status etr_route_backward(const etr_config* cfg, const void* x, const float* w_emb, const float* score,
+                              const float* gate, const float* dgate, const void* dx_add, void* dx, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -22,7 +22,10 @@ EXPORTS = ("etr_workspace_bytes", "etr_select_workspace_bytes", "etr_ffn_workspa
            "etr_route", "etr_select", "etr_dispatch", "etr_expert_ffn", "etr_combine", "etr_moe_forward",
            "etr_moe_forward_profiled", "etr_select_adaptive", "etr_stats_workspace_bytes", "etr_route_stats",
            "etr_capacity_lower_bound", "etr_backward_workspace_bytes", "etr_moe_backward",
-           "etr_moe_forward_train", "etr_select_noalloc", "etr_select_noalloc_max_bytes")
+           "etr_moe_forward_train", "etr_select_noalloc", "etr_select_noalloc_max_bytes",
+           "etr_block_norm", "etr_norm_workspace_bytes", "etr_block_norm_backward", "etr_sort_workspace_bytes",
+           "etr_sort_tokens", "etr_sort_rows", "etr_sort_rows_backward", "etr_unsort_rows", "etr_unsort_rows_backward",
+           "etr_route_backward")
 N_STAGE_EVENTS = 7
 STAGE_NAMES = ("route", "select", "dispatch", "ffn_gate_up", "ffn_down", "combine")
 
@@ -30,6 +33,15 @@ STAGE_NAMES = ("route", "select", "dispatch", "ffn_gate_up", "ffn_down", "combin
 class EtrConfig(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("T", "d", "E", "D", "k", "capacity", "H", "dtype", "mode", "cos",
                                              "gate_norm")]
+
+
+class EtrNormConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "d", "dtype")] + [(n, ctypes.c_float) for n in
+                                                                    ("eps", "residual_scale", "block_scale")]
+
+
+class EtrSortConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "k", "E", "d", "dtype", "gate_norm")]
 
 
 class EtrError(RuntimeError):
@@ -55,6 +67,10 @@ def load_library():
                  "etr_stats_workspace_bytes", "etr_backward_workspace_bytes"):
         getattr(lib, name).restype = sz
         getattr(lib, name).argtypes = [cp]
+    np_, sp = (ctypes.POINTER(c) for c in (EtrNormConfig, EtrSortConfig))
+    for name, arg in (("etr_norm_workspace_bytes", np_), ("etr_sort_workspace_bytes", sp)):
+        getattr(lib, name).restype = sz
+        getattr(lib, name).argtypes = [arg]
     lib.etr_select_noalloc_max_bytes.restype = sz
     lib.etr_select_noalloc_max_bytes.argtypes = []
     lib.etr_status_string.restype = ctypes.c_char_p
@@ -74,6 +90,14 @@ def load_library():
         "etr_moe_forward_train": [cp] + [vp] * 15 + [sz, vp],
         "etr_moe_forward_profiled": [cp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp,
                                      ctypes.POINTER(ctypes.c_void_p)],
+        "etr_block_norm": [np_] + [vp] * 8,
+        "etr_block_norm_backward": [np_] + [vp] * 13 + [sz, vp],
+        "etr_sort_tokens": [sp] + [vp] * 6 + [sz, vp],
+        "etr_sort_rows": [sp] + [vp] * 4,
+        "etr_sort_rows_backward": [sp] + [vp] * 4,
+        "etr_unsort_rows": [sp] + [vp] * 6,
+        "etr_unsort_rows_backward": [sp] + [vp] * 8,
+        "etr_route_backward": [cp] + [vp] * 8,
     }
     for name, args in sigs.items():
         getattr(lib, name).restype = ctypes.c_int
@@ -87,6 +111,26 @@ def make_config(shape: EtrShape, mode: Optional[int] = None, capacity: Optional[
     return EtrConfig(shape.T, shape.d, shape.E, shape.D, shape.k,
                      shape.capacity if capacity is None else capacity, shape.H, shape.dtype,
                      shape.mode if mode is None else mode, shape.cos if cos is None else cos, gate_norm)
+
+
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _dtype(dtype) -> int:
+    """etr_dtype of a torch type (or the number itself)."""
+    if isinstance(dtype, int):
+        return dtype
+    if dtype not in _DTYPES:
+        raise ValueError(f"rows are float32 or bfloat16, not {dtype}")
+    return _DTYPES[dtype]
+
+
+def make_norm_config(T, d, dtype, eps: float = 1e-5, residual_scale: float = 1.0, block_scale: float = 1.0) -> EtrNormConfig:
+    return EtrNormConfig(T, d, _dtype(dtype), eps, residual_scale, block_scale)
+
+
+def make_sort_config(T, k, E, d, dtype, gate_norm: int = 0) -> EtrSortConfig:
+    return EtrSortConfig(T, k, E, d, _dtype(dtype), gate_norm)
 
 
 # Small calls are bound by the host: addresses go to ctypes as plain integers (None = NULL; the declared argument types
@@ -210,6 +254,57 @@ def etr_moe_forward(cfg, x, w_emb, w_gate, w_up, w_down, out, ws, score=None, ga
     _check("etr_moe_forward", load_library().etr_moe_forward(
         ctypes.byref(cfg), _ptr(x), _ptr(w_emb), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(out), _ptr(score),
         _ptr(gate), _ptr(topk_expert), _ptr(slot_of), _ptr(slot_token), _ptr(counts), _ptr(ws), _nbytes(ws), _stream()))
+
+
+def etr_norm_workspace_bytes(cfg: EtrNormConfig) -> int:
+    return int(load_library().etr_norm_workspace_bytes(ctypes.byref(cfg)))
+
+
+def etr_block_norm(cfg, x, y=None, gate=None, w_post=None, w_pre=None, x_out=None, h=None):
+    _check("etr_block_norm", load_library().etr_block_norm(
+        ctypes.byref(cfg), _ptr(x), _ptr(y), _ptr(gate), _ptr(w_post), _ptr(w_pre), _ptr(x_out), _ptr(h), _stream()))
+
+
+def etr_block_norm_backward(cfg, x_out, y, gate, w_post, w_pre, dx_out, dh, dx, dy=None, dgate=None, dw_post=None,
+                            dw_pre=None, ws=None):
+    _check("etr_block_norm_backward", load_library().etr_block_norm_backward(
+        ctypes.byref(cfg), _ptr(x_out), _ptr(y), _ptr(gate), _ptr(w_post), _ptr(w_pre), _ptr(dx_out), _ptr(dh), _ptr(dx),
+        _ptr(dy), _ptr(dgate), _ptr(dw_post), _ptr(dw_pre), _ptr(ws), _nbytes(ws), _stream()))
+
+
+def etr_sort_workspace_bytes(cfg: EtrSortConfig) -> int:
+    return int(load_library().etr_sort_workspace_bytes(ctypes.byref(cfg)))
+
+
+def etr_sort_tokens(cfg, topk_expert, slot_of, offsets, row_of, pair_of, ws):
+    _check("etr_sort_tokens", load_library().etr_sort_tokens(
+        ctypes.byref(cfg), _ptr(topk_expert), _ptr(slot_of), _ptr(offsets), _ptr(row_of), _ptr(pair_of), _ptr(ws), _nbytes(ws),
+        _stream()))
+
+
+def etr_sort_rows(cfg, x, row_of, xs):
+    _check("etr_sort_rows", load_library().etr_sort_rows(ctypes.byref(cfg), _ptr(x), _ptr(row_of), _ptr(xs), _stream()))
+
+
+def etr_sort_rows_backward(cfg, dxs, row_of, dx):
+    _check("etr_sort_rows_backward", load_library().etr_sort_rows_backward(ctypes.byref(cfg), _ptr(dxs), _ptr(row_of),
+                                                                           _ptr(dx), _stream()))
+
+
+def etr_unsort_rows(cfg, ys, gate, topk_expert, row_of, out):
+    _check("etr_unsort_rows", load_library().etr_unsort_rows(ctypes.byref(cfg), _ptr(ys), _ptr(gate), _ptr(topk_expert),
+                                                             _ptr(row_of), _ptr(out), _stream()))
+
+
+def etr_unsort_rows_backward(cfg, dout, ys, gate, topk_expert, row_of, dys, dgate):
+    _check("etr_unsort_rows_backward", load_library().etr_unsort_rows_backward(
+        ctypes.byref(cfg), _ptr(dout), _ptr(ys), _ptr(gate), _ptr(topk_expert), _ptr(row_of), _ptr(dys), _ptr(dgate),
+        _stream()))
+
+
+def etr_route_backward(cfg, x, w_emb, score, gate, dgate, dx_add, dx):
+    _check("etr_route_backward", load_library().etr_route_backward(
+        ctypes.byref(cfg), _ptr(x), _ptr(w_emb), _ptr(score), _ptr(gate), _ptr(dgate), _ptr(dx_add), _ptr(dx), _stream()))
 
 
 class StageEvents:

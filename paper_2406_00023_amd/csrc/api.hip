@@ -77,6 +77,27 @@ etr_status check_config(const etr_config* c) {
     return ETR_OK;
 }
 
+bool known_dtype(int dtype) { return dtype == ETR_F32 || dtype == ETR_BF16; }
+
+etr_status check_norm(const etr_norm_config* c) {
+    if (!c) return ETR_ERR_NULL;
+    if (c->T <= 0 || c->d <= 0 || !(c->eps > 0.f) || !std::isfinite(c->eps)) return ETR_ERR_SHAPE;
+    if (!std::isfinite(c->residual_scale) || !std::isfinite(c->block_scale)) return ETR_ERR_SHAPE;
+    if (!known_dtype(c->dtype) || c->d % 8 != 0) return ETR_ERR_UNSUPPORTED;
+    if (static_cast<size_t>(c->d) * elt_bytes(c->dtype) > 64 * 1024) return ETR_ERR_UNSUPPORTED;     // a row in the registers of 1024 threads
+    return ETR_OK;
+}
+
+etr_status check_sort(const etr_sort_config* c) {
+    if (!c) return ETR_ERR_NULL;
+    if (c->T <= 0 || c->d <= 0 || c->E <= 0 || c->k < 1 || c->k > c->E) return ETR_ERR_SHAPE;
+    if (!known_dtype(c->dtype) || (c->gate_norm != 0 && c->gate_norm != 1)) return ETR_ERR_UNSUPPORTED;
+    if (c->E > 64 || c->d % 8 != 0) return ETR_ERR_UNSUPPORTED;
+    if (static_cast<size_t>(c->d) * elt_bytes(c->dtype) > 128 * 1024) return ETR_ERR_UNSUPPORTED;
+    if (static_cast<long long>(c->T) * c->k > (1ll << 30)) return ETR_ERR_UNSUPPORTED;               // 32-bit pair numbers, with headroom
+    return ETR_OK;
+}
+
 // Workspace of etr_moe_forward: optional outputs that the caller did not ask for, the
 // select scratch, the permuted buffers and the hidden activation.
 struct ForwardWs {
@@ -369,6 +390,111 @@ etr_status etr_moe_forward_profiled(const etr_config* cfg, const void* x, const 
     if (!events) return ETR_ERR_NULL;
     return forward_impl(cfg, x, w_emb, w_gate, w_up, w_down, out, score, gate_out, topk_expert, slot_of, slot_token,
                         counts, ws, ws_bytes, stream, events);
+}
+
+size_t etr_norm_workspace_bytes(const etr_norm_config* cfg) {
+    if (check_norm(cfg) != ETR_OK) return 0;
+    return norm_ws_bytes(*cfg);
+}
+
+etr_status etr_block_norm(const etr_norm_config* cfg, const void* x, const void* y, const float* gate, const float* w_post,
+                          const float* w_pre, void* x_out, void* h, void* stream) {
+    etr_status s = check_norm(cfg);
+    if (s != ETR_OK) return s;
+    ETR_REQUIRE_PTR(x);
+    ETR_OPTIONAL_PTR(y); ETR_OPTIONAL_PTR(gate); ETR_OPTIONAL_PTR(w_post); ETR_OPTIONAL_PTR(w_pre); ETR_OPTIONAL_PTR(x_out);
+    ETR_OPTIONAL_PTR(h);
+    if (!y && !w_pre) return ETR_ERR_NULL;
+    if ((w_pre == nullptr) != (h == nullptr) || (y == nullptr) != (x_out == nullptr)) return ETR_ERR_NULL;
+    if (!y && (gate || w_post)) return ETR_ERR_NULL;                 // nothing for them to weigh
+    ETR_HIP(launch_block_norm(*cfg, x, y, gate, w_post, w_pre, x_out, h, static_cast<hipStream_t>(stream)));
+    return ETR_OK;
+}
+
+etr_status etr_block_norm_backward(const etr_norm_config* cfg, const void* x_out, const void* y, const float* gate,
+                                   const float* w_post, const float* w_pre, const void* dx_out, const void* dh, void* dx,
+                                   void* dy, float* dgate, float* dw_post, float* dw_pre, void* ws, size_t ws_bytes,
+                                   void* stream) {
+    etr_status s = check_norm(cfg);
+    if (s != ETR_OK) return s;
+    ETR_REQUIRE_PTR(dx);
+    ETR_OPTIONAL_PTR(x_out); ETR_OPTIONAL_PTR(y); ETR_OPTIONAL_PTR(gate); ETR_OPTIONAL_PTR(w_post); ETR_OPTIONAL_PTR(w_pre);
+    ETR_OPTIONAL_PTR(dx_out); ETR_OPTIONAL_PTR(dh); ETR_OPTIONAL_PTR(dy); ETR_OPTIONAL_PTR(dgate); ETR_OPTIONAL_PTR(dw_post);
+    ETR_OPTIONAL_PTR(dw_pre);
+    if (!y && !w_pre) return ETR_ERR_NULL;
+    if ((w_pre == nullptr) != (dh == nullptr) || (y == nullptr) != (dy == nullptr)) return ETR_ERR_NULL;
+    if (w_pre && !x_out) return ETR_ERR_NULL;
+    if (!y && (gate || w_post)) return ETR_ERR_NULL;
+    if ((dgate && !gate) || (dw_post && !w_post) || (dw_pre && !w_pre)) return ETR_ERR_NULL;
+    if (dw_post || dw_pre) {
+        ETR_REQUIRE_PTR(ws);
+        if (ws_bytes < norm_ws_bytes(*cfg)) return ETR_ERR_WORKSPACE;
+    }
+    ETR_HIP(launch_block_norm_backward(*cfg, x_out, y, gate, w_post, w_pre, dx_out, dh, dx, dy, dgate, dw_post, dw_pre, ws,
+                                       static_cast<hipStream_t>(stream)));
+    return ETR_OK;
+}
+
+size_t etr_sort_workspace_bytes(const etr_sort_config* cfg) {
+    if (check_sort(cfg) != ETR_OK) return 0;
+    return sort_ws_bytes(*cfg);
+}
+
+etr_status etr_sort_tokens(const etr_sort_config* cfg, const int32_t* topk_expert, const int32_t* slot_of, int32_t* offsets,
+                           int32_t* row_of, int32_t* pair_of, void* ws, size_t ws_bytes, void* stream) {
+    etr_status s = check_sort(cfg);
+    if (s != ETR_OK) return s;
+    ETR_REQUIRE_PTR(topk_expert); ETR_REQUIRE_PTR(offsets); ETR_REQUIRE_PTR(row_of); ETR_REQUIRE_PTR(pair_of); ETR_REQUIRE_PTR(ws);
+    ETR_OPTIONAL_PTR(slot_of);
+    if (ws_bytes < sort_ws_bytes(*cfg)) return ETR_ERR_WORKSPACE;
+    ETR_HIP(launch_sort_tokens(*cfg, topk_expert, slot_of, offsets, row_of, pair_of, ws, static_cast<hipStream_t>(stream)));
+    return ETR_OK;
+}
+
+etr_status etr_sort_rows(const etr_sort_config* cfg, const void* x, const int32_t* row_of, void* xs, void* stream) {
+    etr_status s = check_sort(cfg);
+    if (s != ETR_OK) return s;
+    ETR_REQUIRE_PTR(x); ETR_REQUIRE_PTR(row_of); ETR_REQUIRE_PTR(xs);
+    ETR_HIP(launch_sort_rows(*cfg, x, row_of, xs, static_cast<hipStream_t>(stream)));
+    return ETR_OK;
+}
+
+etr_status etr_sort_rows_backward(const etr_sort_config* cfg, const void* dxs, const int32_t* row_of, void* dx, void* stream) {
+    etr_status s = check_sort(cfg);
+    if (s != ETR_OK) return s;
+    ETR_REQUIRE_PTR(dxs); ETR_REQUIRE_PTR(row_of); ETR_REQUIRE_PTR(dx);
+    ETR_HIP(launch_sort_rows_backward(*cfg, dxs, row_of, dx, static_cast<hipStream_t>(stream)));
+    return ETR_OK;
+}
+
+etr_status etr_unsort_rows(const etr_sort_config* cfg, const void* ys, const float* gate, const int32_t* topk_expert,
+                           const int32_t* row_of, void* out, void* stream) {
+    etr_status s = check_sort(cfg);
+    if (s != ETR_OK) return s;
+    ETR_REQUIRE_PTR(ys); ETR_REQUIRE_PTR(gate); ETR_REQUIRE_PTR(topk_expert); ETR_REQUIRE_PTR(row_of); ETR_REQUIRE_PTR(out);
+    ETR_HIP(launch_unsort_rows(*cfg, ys, gate, topk_expert, row_of, out, static_cast<hipStream_t>(stream)));
+    return ETR_OK;
+}
+
+etr_status etr_unsort_rows_backward(const etr_sort_config* cfg, const void* dout, const void* ys, const float* gate,
+                                    const int32_t* topk_expert, const int32_t* row_of, void* dys, float* dgate, void* stream) {
+    etr_status s = check_sort(cfg);
+    if (s != ETR_OK) return s;
+    ETR_REQUIRE_PTR(dout); ETR_REQUIRE_PTR(ys); ETR_REQUIRE_PTR(gate); ETR_REQUIRE_PTR(topk_expert); ETR_REQUIRE_PTR(row_of);
+    ETR_REQUIRE_PTR(dys); ETR_REQUIRE_PTR(dgate);
+    ETR_HIP(launch_unsort_rows_backward(*cfg, dout, ys, gate, topk_expert, row_of, dys, dgate, static_cast<hipStream_t>(stream)));
+    return ETR_OK;
+}
+
+etr_status etr_route_backward(const etr_config* cfg, const void* x, const float* w_emb, const float* score, const float* gate,
+                              const float* dgate, const void* dx_add, void* dx, void* stream) {
+    etr_status s = check_config(cfg);
+    if (s != ETR_OK) return s;
+    ETR_REQUIRE_PTR(x); ETR_REQUIRE_PTR(w_emb); ETR_REQUIRE_PTR(score); ETR_REQUIRE_PTR(gate); ETR_REQUIRE_PTR(dgate);
+    ETR_REQUIRE_PTR(dx); ETR_OPTIONAL_PTR(dx_add);
+    if (static_cast<size_t>(cfg->E) * (cfg->d / cfg->D) * 4 > 120 * 1024) return ETR_ERR_UNSUPPORTED;
+    ETR_HIP(launch_route_backward(*cfg, x, w_emb, score, gate, dgate, dx_add, dx, static_cast<hipStream_t>(stream)));
+    return ETR_OK;
 }
 
 }  // extern "C"

@@ -130,6 +130,29 @@ hipError_t launch_route_stats(const etr_config& c, const float* gate, const int3
 hipError_t launch_capacity_lower_bound(const etr_config& c, const float* score, float* dmax, int32_t* capacity,
                                        void* ws, hipStream_t st);
 
+// norm.hip
+size_t norm_ws_bytes(const etr_norm_config& c);
+hipError_t launch_block_norm(const etr_norm_config& c, const void* x, const void* y, const float* gate, const float* w_post,
+                             const float* w_pre, void* x_out, void* h, hipStream_t st);
+hipError_t launch_block_norm_backward(const etr_norm_config& c, const void* x_out, const void* y, const float* gate,
+                                      const float* w_post, const float* w_pre, const void* dx_out, const void* dh, void* dx,
+                                      void* dy, float* dgate, float* dw_post, float* dw_pre, void* ws, hipStream_t st);
+
+// sort.hip
+size_t sort_ws_bytes(const etr_sort_config& c);
+hipError_t launch_sort_tokens(const etr_sort_config& c, const int32_t* topk, const int32_t* slot_of, int32_t* offsets,
+                              int32_t* row_of, int32_t* pair_of, void* ws, hipStream_t st);
+hipError_t launch_sort_rows(const etr_sort_config& c, const void* x, const int32_t* row_of, void* xs, hipStream_t st);
+hipError_t launch_sort_rows_backward(const etr_sort_config& c, const void* dxs, const int32_t* row_of, void* dx, hipStream_t st);
+hipError_t launch_unsort_rows(const etr_sort_config& c, const void* ys, const float* gate, const int32_t* topk,
+                              const int32_t* row_of, void* out, hipStream_t st);
+hipError_t launch_unsort_rows_backward(const etr_sort_config& c, const void* dout, const void* ys, const float* gate,
+                                       const int32_t* topk, const int32_t* row_of, void* dys, float* dgate, hipStream_t st);
+
+// route_backward.hip
+hipError_t launch_route_backward(const etr_config& c, const void* x, const float* w_emb, const float* score, const float* gate,
+                                 const float* dgate, const void* dx_add, void* dx, hipStream_t st);
+
 // Host-side launch helpers (api.hip).  Both remember their answer per device, so a steady-state call issues no
 // runtime call besides its launches.
 //   cu_count            compute units of the current device (256 if the query fails)
