@@ -289,7 +289,7 @@ etr_status etr_moe_forward_profiled(const etr_config* cfg, const void* x, const 
                                     int32_t* slot_token, int32_t* counts,
                                     void* ws, size_t ws_bytes, void* stream, void* const* events);
 
-/* ---- the block around the layer, rows sorted by expert --------------- */
+/* ---- the block around the layer, rows sorted by expert, the experts' products on them ---------------- */
 
 /* The join of a block's output with the residual stream and the norm in front of the next block, in one pass:
  *   x_out[t] = residual_scale x[t] + block_scale gate[t] P(y[t]),   P(y) = N(y) .* w_post  (y itself without w_post)
@@ -363,6 +363,42 @@ etr_status etr_unsort_rows(const etr_sort_config* cfg, const void* ys, const flo
 etr_status etr_unsort_rows_backward(const etr_sort_config* cfg, const void* dout, const void* ys, const float* gate,
                                     const int32_t* topk_expert, const int32_t* row_of, void* dys, float* dgate,
                                     void* stream);
+
+typedef enum { ETR_ACT_NONE = 0, ETR_ACT_SILU = 1, ETR_ACT_GELU = 2, ETR_ACT_SWIGLU = 3 } etr_act;
+
+/* The experts' products on sorted rows, with the epilogue fused: for the rows r of expert e
+ *   a = x[r] W[e]^T + bias[e];   y[r] = act(a) + residual[r]
+ *   act: a itself | SiLU(a) = a / (1 + exp(-a)) | GELU(a) = a Phi(a) | SwiGLU: SiLU(a) .* (x[r] W_up[e]^T + bias_up[e])
+ * fp32 accumulation, one rounding to dtype.  E = 1 with offsets = NULL is a dense product of all rows. */
+typedef struct {
+    int32_t rows;           /* rows of x and y (T * k of the sort); offsets[E] <= rows of them belong to an expert */
+    int32_t K, N, E;        /* K % 8 == 0, N % 8 == 0, E <= 64 */
+    int32_t dtype;          /* etr_dtype of x, w, residual, y, pre and their gradients */
+    int32_t act;            /* etr_act */
+} etr_linear_config;
+
+/*   x [rows][K], w [E][N][K] (SwiGLU: w_up too, else NULL) dtype in; offsets [E+1] int32 in (ascending from 0, clamped to rows)
+ *   bias, bias_up [E][N] fp32 in, optional (SwiGLU: both or neither; else bias_up NULL); residual [rows][N] dtype in, optional
+ *   y [rows][N] dtype out; may be residual; rows that belong to no expert are left untouched
+ *   pre, pre_up [rows][N] dtype out, optional (SwiGLU: both or neither; else pre_up NULL): a, and the up product, for the
+ *   backward */
+etr_status etr_expert_linear(const etr_linear_config* cfg, const void* x, const int32_t* offsets, const void* w,
+                             const void* w_up, const float* bias, const float* bias_up, const void* residual, void* y,
+                             void* pre, void* pre_up, void* stream);
+
+/* Scratch of etr_expert_linear_backward. 0 for an invalid config. */
+size_t etr_linear_workspace_bytes(const etr_linear_config* cfg);
+
+/* Gradient of etr_expert_linear for the upstream gradient dy [rows][N] (the residual's gradient is dy itself):
+ *   da = dy act'(a), at the pre-activations that the forward kept (not needed with ETR_ACT_NONE);  SwiGLU: db = dy SiLU(a) too
+ *   dx = da W (+ db W_up);  dw[e] = da^T x;  dbias[e] = sum da over the expert's rows (likewise dw_up, dbias_up)
+ *   dx [rows][K], dw, dw_up [E][N][K] dtype out, dbias, dbias_up [E][N] fp32 out, each optional, overwritten; an expert
+ *   without rows gets zeros; rows of dx that belong to no expert are left untouched
+ * bf16: da and db are rounded to bf16 once, as operands of the products (the biases' gradients are summed before that). */
+etr_status etr_expert_linear_backward(const etr_linear_config* cfg, const void* x, const int32_t* offsets, const void* w,
+                                      const void* w_up, const void* pre, const void* pre_up, const void* dy, void* dx,
+                                      void* dw, void* dw_up, float* dbias, float* dbias_up, void* ws, size_t ws_bytes,
+                                      void* stream);
 
 /* Gradient of etr_route with respect to the tokens, for the gradient dgate [T][E] of its gates (etr_moe_backward has it
  * inside; layers put together from the calls above need it by itself):

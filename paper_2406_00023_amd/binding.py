@@ -25,7 +25,7 @@ EXPORTS = ("etr_workspace_bytes", "etr_select_workspace_bytes", "etr_ffn_workspa
            "etr_moe_forward_train", "etr_select_noalloc", "etr_select_noalloc_max_bytes",
            "etr_block_norm", "etr_norm_workspace_bytes", "etr_block_norm_backward", "etr_sort_workspace_bytes",
            "etr_sort_tokens", "etr_sort_rows", "etr_sort_rows_backward", "etr_unsort_rows", "etr_unsort_rows_backward",
-           "etr_route_backward")
+           "etr_expert_linear", "etr_linear_workspace_bytes", "etr_expert_linear_backward", "etr_route_backward")
 N_STAGE_EVENTS = 7
 STAGE_NAMES = ("route", "select", "dispatch", "ffn_gate_up", "ffn_down", "combine")
 
@@ -42,6 +42,13 @@ class EtrNormConfig(ctypes.Structure):
 
 class EtrSortConfig(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("T", "k", "E", "d", "dtype", "gate_norm")]
+
+
+class EtrLinearConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "K", "N", "E", "dtype", "act")]
+
+
+ACT_NONE, ACT_SILU, ACT_GELU, ACT_SWIGLU = 0, 1, 2, 3
 
 
 class EtrError(RuntimeError):
@@ -67,8 +74,9 @@ def load_library():
                  "etr_stats_workspace_bytes", "etr_backward_workspace_bytes"):
         getattr(lib, name).restype = sz
         getattr(lib, name).argtypes = [cp]
-    np_, sp = (ctypes.POINTER(c) for c in (EtrNormConfig, EtrSortConfig))
-    for name, arg in (("etr_norm_workspace_bytes", np_), ("etr_sort_workspace_bytes", sp)):
+    np_, sp, lp = (ctypes.POINTER(c) for c in (EtrNormConfig, EtrSortConfig, EtrLinearConfig))
+    for name, arg in (("etr_norm_workspace_bytes", np_), ("etr_sort_workspace_bytes", sp),
+                      ("etr_linear_workspace_bytes", lp)):
         getattr(lib, name).restype = sz
         getattr(lib, name).argtypes = [arg]
     lib.etr_select_noalloc_max_bytes.restype = sz
@@ -97,6 +105,8 @@ def load_library():
         "etr_sort_rows_backward": [sp] + [vp] * 4,
         "etr_unsort_rows": [sp] + [vp] * 6,
         "etr_unsort_rows_backward": [sp] + [vp] * 8,
+        "etr_expert_linear": [lp] + [vp] * 11,
+        "etr_expert_linear_backward": [lp] + [vp] * 13 + [sz, vp],
         "etr_route_backward": [cp] + [vp] * 8,
     }
     for name, args in sigs.items():
@@ -131,6 +141,10 @@ def make_norm_config(T, d, dtype, eps: float = 1e-5, residual_scale: float = 1.0
 
 def make_sort_config(T, k, E, d, dtype, gate_norm: int = 0) -> EtrSortConfig:
     return EtrSortConfig(T, k, E, d, _dtype(dtype), gate_norm)
+
+
+def make_linear_config(rows, K, N, E, dtype, act: int = ACT_NONE) -> EtrLinearConfig:
+    return EtrLinearConfig(rows, K, N, E, _dtype(dtype), act)
 
 
 # Small calls are bound by the host: addresses go to ctypes as plain integers (None = NULL; the declared argument types
@@ -300,6 +314,23 @@ def etr_unsort_rows_backward(cfg, dout, ys, gate, topk_expert, row_of, dys, dgat
     _check("etr_unsort_rows_backward", load_library().etr_unsort_rows_backward(
         ctypes.byref(cfg), _ptr(dout), _ptr(ys), _ptr(gate), _ptr(topk_expert), _ptr(row_of), _ptr(dys), _ptr(dgate),
         _stream()))
+
+
+def etr_linear_workspace_bytes(cfg: EtrLinearConfig) -> int:
+    return int(load_library().etr_linear_workspace_bytes(ctypes.byref(cfg)))
+
+
+def etr_expert_linear(cfg, x, offsets, w, y, w_up=None, bias=None, bias_up=None, residual=None, pre=None, pre_up=None):
+    _check("etr_expert_linear", load_library().etr_expert_linear(
+        ctypes.byref(cfg), _ptr(x), _ptr(offsets), _ptr(w), _ptr(w_up), _ptr(bias), _ptr(bias_up), _ptr(residual), _ptr(y),
+        _ptr(pre), _ptr(pre_up), _stream()))
+
+
+def etr_expert_linear_backward(cfg, x, offsets, w, dy, ws, w_up=None, pre=None, pre_up=None, dx=None, dw=None, dw_up=None,
+                               dbias=None, dbias_up=None):
+    _check("etr_expert_linear_backward", load_library().etr_expert_linear_backward(
+        ctypes.byref(cfg), _ptr(x), _ptr(offsets), _ptr(w), _ptr(w_up), _ptr(pre), _ptr(pre_up), _ptr(dy), _ptr(dx), _ptr(dw),
+        _ptr(dw_up), _ptr(dbias), _ptr(dbias_up), _ptr(ws), _nbytes(ws), _stream()))
 
 
 def etr_route_backward(cfg, x, w_emb, score, gate, dgate, dx_add, dx):

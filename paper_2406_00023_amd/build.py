@@ -13,7 +13,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libetr_hip.so")
 SOURCES = ["api.hip", "route.hip", "select.hip", "permute.hip", "ffn.hip", "stats.hip", "backward.hip", "norm.hip",
-           "sort.hip", "route_backward.hip"]
+           "sort.hip", "route_backward.hip", "linear.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

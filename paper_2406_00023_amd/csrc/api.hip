@@ -1,5 +1,6 @@
 // C-ABI layer: host-side argument validation, workspace carving and the stage chain
 // of the whole layer (Sec. Model Architecture, Eqs. 1-6).  Nothing here computes.
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <mutex>
@@ -95,6 +96,18 @@ etr_status check_sort(const etr_sort_config* c) {
     if (c->E > 64 || c->d % 8 != 0) return ETR_ERR_UNSUPPORTED;
     if (static_cast<size_t>(c->d) * elt_bytes(c->dtype) > 128 * 1024) return ETR_ERR_UNSUPPORTED;
     if (static_cast<long long>(c->T) * c->k > (1ll << 30)) return ETR_ERR_UNSUPPORTED;               // 32-bit pair numbers, with headroom
+    return ETR_OK;
+}
+
+etr_status check_linear(const etr_linear_config* c) {
+    if (!c) return ETR_ERR_NULL;
+    if (c->rows <= 0 || c->K <= 0 || c->N <= 0 || c->E <= 0) return ETR_ERR_SHAPE;
+    if (!known_dtype(c->dtype) || c->act < ETR_ACT_NONE || c->act > ETR_ACT_SWIGLU) return ETR_ERR_UNSUPPORTED;
+    if (c->E > 64 || c->K % 8 != 0 || c->N % 8 != 0) return ETR_ERR_UNSUPPORTED;
+    // 32-bit byte offsets inside a tile's rows and 32-bit numbers of tiles
+    if (c->K > (1 << 20) || c->N > (1 << 20) || c->rows > (1 << 28)) return ETR_ERR_UNSUPPORTED;
+    const long long columns = (std::max(c->K, c->N) + 31) / 32;
+    if (columns * (c->rows / 32 + c->E) > (1ll << 30) || columns * columns * c->E > (1ll << 30)) return ETR_ERR_UNSUPPORTED;
     return ETR_OK;
 }
 
@@ -483,6 +496,48 @@ etr_status etr_unsort_rows_backward(const etr_sort_config* cfg, const void* dout
     ETR_REQUIRE_PTR(dout); ETR_REQUIRE_PTR(ys); ETR_REQUIRE_PTR(gate); ETR_REQUIRE_PTR(topk_expert); ETR_REQUIRE_PTR(row_of);
     ETR_REQUIRE_PTR(dys); ETR_REQUIRE_PTR(dgate);
     ETR_HIP(launch_unsort_rows_backward(*cfg, dout, ys, gate, topk_expert, row_of, dys, dgate, static_cast<hipStream_t>(stream)));
+    return ETR_OK;
+}
+
+size_t etr_linear_workspace_bytes(const etr_linear_config* cfg) {
+    if (check_linear(cfg) != ETR_OK) return 0;
+    return linear_ws_bytes(*cfg);
+}
+
+etr_status etr_expert_linear(const etr_linear_config* cfg, const void* x, const int32_t* offsets, const void* w, const void* w_up,
+                             const float* bias, const float* bias_up, const void* residual, void* y, void* pre, void* pre_up,
+                             void* stream) {
+    etr_status s = check_linear(cfg);
+    if (s != ETR_OK) return s;
+    const bool glu = cfg->act == ETR_ACT_SWIGLU;
+    ETR_REQUIRE_PTR(x); ETR_REQUIRE_PTR(w); ETR_REQUIRE_PTR(y);
+    ETR_OPTIONAL_PTR(offsets); ETR_OPTIONAL_PTR(w_up); ETR_OPTIONAL_PTR(bias); ETR_OPTIONAL_PTR(bias_up); ETR_OPTIONAL_PTR(residual);
+    ETR_OPTIONAL_PTR(pre); ETR_OPTIONAL_PTR(pre_up);
+    if (!offsets && cfg->E != 1) return ETR_ERR_NULL;
+    if (glu != (w_up != nullptr)) return ETR_ERR_NULL;
+    if (glu ? (bias == nullptr) != (bias_up == nullptr) || (pre == nullptr) != (pre_up == nullptr) : bias_up || pre_up) return ETR_ERR_NULL;
+    ETR_HIP(launch_expert_linear(*cfg, x, offsets, w, w_up, bias, bias_up, residual, y, pre, pre_up, static_cast<hipStream_t>(stream)));
+    return ETR_OK;
+}
+
+etr_status etr_expert_linear_backward(const etr_linear_config* cfg, const void* x, const int32_t* offsets, const void* w,
+                                      const void* w_up, const void* pre, const void* pre_up, const void* dy, void* dx, void* dw,
+                                      void* dw_up, float* dbias, float* dbias_up, void* ws, size_t ws_bytes, void* stream) {
+    etr_status s = check_linear(cfg);
+    if (s != ETR_OK) return s;
+    const bool glu = cfg->act == ETR_ACT_SWIGLU, act = cfg->act != ETR_ACT_NONE;
+    ETR_REQUIRE_PTR(dy); ETR_REQUIRE_PTR(ws);
+    ETR_OPTIONAL_PTR(x); ETR_OPTIONAL_PTR(offsets); ETR_OPTIONAL_PTR(w); ETR_OPTIONAL_PTR(w_up); ETR_OPTIONAL_PTR(pre);
+    ETR_OPTIONAL_PTR(pre_up); ETR_OPTIONAL_PTR(dx); ETR_OPTIONAL_PTR(dw); ETR_OPTIONAL_PTR(dw_up); ETR_OPTIONAL_PTR(dbias);
+    ETR_OPTIONAL_PTR(dbias_up);
+    if (!offsets && cfg->E != 1) return ETR_ERR_NULL;
+    if (!dx && !dw && !dbias) return ETR_ERR_NULL;                   // nothing asked for
+    if ((act && !pre) || (glu && !pre_up)) return ETR_ERR_NULL;
+    if ((dx && !w) || (dw && !x) || (dx && glu && !w_up)) return ETR_ERR_NULL;
+    if (glu ? (dw == nullptr) != (dw_up == nullptr) || (dbias == nullptr) != (dbias_up == nullptr) : dw_up || dbias_up) return ETR_ERR_NULL;
+    if (ws_bytes < linear_ws_bytes(*cfg)) return ETR_ERR_WORKSPACE;
+    ETR_HIP(launch_expert_linear_backward(*cfg, x, offsets, w, w_up, pre, pre_up, dy, dx, dw, dw_up, dbias, dbias_up, ws,
+                                          static_cast<hipStream_t>(stream)));
     return ETR_OK;
 }
 

@@ -149,6 +149,15 @@ hipError_t launch_unsort_rows(const etr_sort_config& c, const void* ys, const fl
 hipError_t launch_unsort_rows_backward(const etr_sort_config& c, const void* dout, const void* ys, const float* gate,
                                        const int32_t* topk, const int32_t* row_of, void* dys, float* dgate, hipStream_t st);
 
+// linear.hip
+size_t linear_ws_bytes(const etr_linear_config& c);
+hipError_t launch_expert_linear(const etr_linear_config& c, const void* x, const int32_t* offsets, const void* w, const void* w_up,
+                                const float* bias, const float* bias_up, const void* residual, void* y, void* pre, void* pre_up,
+                                hipStream_t st);
+hipError_t launch_expert_linear_backward(const etr_linear_config& c, const void* x, const int32_t* offsets, const void* w,
+                                         const void* w_up, const void* pre, const void* pre_up, const void* dy, void* dx, void* dw,
+                                         void* dw_up, float* dbias, float* dbias_up, void* ws, hipStream_t st);
+
 // route_backward.hip
 hipError_t launch_route_backward(const etr_config& c, const void* x, const float* w_emb, const float* score, const float* gate,
                                  const float* dgate, const void* dx_add, void* dx, hipStream_t st);

@@ -1,0 +1,605 @@
+// The experts' products on rows sorted by expert, with bias, activation and residual in the epilogue, and their gradients.
+//   forward  y[r][n] = act(sum_k x[r][k] w[e][n][k] + bias[e][n]) + residual[r][n]       rows of expert e: offsets[e] ... offsets[e+1] - 1
+//   dx[r][k] = sum_n da[r][n] w[e][n][k] (+ the same of db, w_up);  dw[e][n][k] = sum_r da[r][n] x[r][k];  dbias[e][n] = sum_r da[r][n]
+//   da = dy act'(a), SwiGLU: da = dy up SiLU'(a), db = dy SiLU(a)                          (an element-wise pass, none for act = none)
+// Every product is C[m][n] = sum_k A(m, k) B(n, k) with operands that are read as they lie: contraction contiguous ("rows") or
+// contraction slow ("columns": w in dx, both in dw).  Both kinds go straight into LDS in 16-byte pieces; rows are read back as
+// MFMA fragments, columns by transposing LDS reads (bf16) or single words (fp32), so nothing is transposed in memory.  What lies
+// past the end of a contraction (a ragged K, the rows of the next expert) is zero-filled by the copy.
+#include <algorithm>
+#include <cmath>
+
+#include "row_ops.h"
+
+namespace etr {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((address_space(3))) void* lds_ptr;
+
+enum Product { FORWARD = 0, INPUT = 1, WEIGHT = 2 };     // y, dx, dw
+
+struct LinearParams {
+    const void* A[2]; const void* B[2];                  // second: SwiGLU (FORWARD: B; INPUT: both; WEIGHT: A)
+    void* C[2];                                          // second: WEIGHT with SwiGLU
+    const int32_t* offsets;
+    const float* bias[2];
+    const void* residual;
+    void* pre[2];
+    int rows, E;
+    int M, N, K;                                         // WEIGHT: output rows; output columns; contraction (of each half)
+    int lda, ldb;
+    int act, glu;
+    int NT;                                              // column tiles
+};
+
+// Buffer descriptors that bound nothing that exists, and an offset past any of them: such a lane copies zeros.
+constexpr uint32_t kRange = 0xFFFFFF00u, kPast = 0xFFFFFF80u;
+
+__device__ __forceinline__ void copy_piece(uint64_t base, uint32_t off, void* dst) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(base));
+    const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(base >> 32));
+    void* at = reinterpret_cast<void*>((static_cast<uint64_t>(hi) << 32) | lo);
+    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(at, 0, static_cast<int>(kRange), 0x00027000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)dst, 16, static_cast<int>(off), 0, 0, 0);
+}
+
+// s_waitcnt: at most n vector memory operations outstanding, the others as they are
+template <int N> __device__ __forceinline__ void wait_copies() { __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0F70); }
+
+// Rows of the groups, one group per lane (E <= 64): first row, number, and the row tiles before it.
+struct Groups {
+    int first, count, tiles_incl, tiles;
+    __device__ __forceinline__ void load(const LinearParams& p, int BM) {
+        const int lane = threadIdx.x & 63;
+        first = 0; count = 0;
+        if (lane < p.E) {
+            first = p.offsets ? min(max(p.offsets[lane], 0), p.rows) : 0;
+            const int end = p.offsets ? min(max(p.offsets[lane + 1], first), p.rows) : p.rows;
+            count = end - first;
+        }
+        tiles = (count + BM - 1) / BM;
+        tiles_incl = wave_scan_incl(tiles);
+    }
+};
+
+struct Tile { int e, first, m0, n0, count, half; };      // half: WEIGHT with SwiGLU, which of the two outputs
+
+// The tile list: groups one after the other; inside a group bands of 8 row tiles, in a band the row tiles of a column tile next to
+// each other.  Each XCD (workgroups go round them) has an equal contiguous part of the list, so its 32 CUs work on some 8 x 4 tiles at
+// once and share 8 + 4 operand slabs in its L2.
+template <int MODE>
+__device__ __forceinline__ bool find_tile(const LinearParams& p, const Groups& g, int BM, int BN, int j, int& share, Tile& t) {
+    int total, MTw = 0;
+    if (MODE == WEIGHT) {
+        MTw = (p.M + BM - 1) / BM;
+        total = p.E * MTw * (p.glu ? 2 : 1) * p.NT;
+    } else {
+        total = __builtin_amdgcn_readlane(g.tiles_incl, 63) * p.NT;
+    }
+    share = (total + 7) >> 3;
+    const int q = (blockIdx.x & 7) * share + j;
+    if (j >= share || q >= total) return false;
+    int in, rows;
+    if (MODE == WEIGHT) {
+        rows = MTw * (p.glu ? 2 : 1);
+        t.e = q / (rows * p.NT);
+        in = q - t.e * (rows * p.NT);
+    } else {
+        t.e = __builtin_ctzll(__ballot(g.tiles_incl * p.NT > q));
+        rows = __builtin_amdgcn_readlane(g.tiles, t.e);
+        in = q - (__builtin_amdgcn_readlane(g.tiles_incl, t.e) - rows) * p.NT;
+    }
+    const int band = in / (8 * p.NT), in_band = in - band * 8 * p.NT, height = min(8, rows - band * 8);
+    const int nt = in_band / height, mt = band * 8 + in_band - nt * height;
+    t.first = __builtin_amdgcn_readlane(g.first, t.e);
+    t.count = __builtin_amdgcn_readlane(g.count, t.e);
+    t.half = MODE == WEIGHT && mt >= MTw ? 1 : 0;
+    t.m0 = (mt - t.half * MTw) * BM;
+    t.n0 = nt * BN;
+    return true;
+}
+
+// ---- epilogue --------------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ float sigmoid(float a) { return 1.0f / (1.0f + __expf(-a)); }
+// The normal distribution function by the Chebyshev fit of erfc in Press et al., Numerical Recipes, 6.2 (fractional error below
+// 1.2e-7): no branch, where erff has two and keeps every value of a tile alive across them (789 spilled registers).
+__device__ __forceinline__ float normal_cdf(float a) {
+    const float x = fabsf(a) * 0.70710678118654752f, u = 1.0f / fmaf(0.5f, x, 1.0f);
+    float s = 0.17087277f;
+    s = fmaf(s, u, -0.82215223f); s = fmaf(s, u, 1.48851587f); s = fmaf(s, u, -1.13520398f); s = fmaf(s, u, 0.27886807f);
+    s = fmaf(s, u, -0.18628806f); s = fmaf(s, u, 0.09678418f); s = fmaf(s, u, 0.37409196f); s = fmaf(s, u, 1.00002368f);
+    s = fmaf(s, u, -1.26551223f);
+    const float half = 0.5f * u * __expf(fmaf(-x, x, s));
+    return a < 0.f ? half : 1.0f - half;
+}
+template <bool BF16>
+__device__ __forceinline__ void load4(const void* p, uint32_t at, float (&f)[4]) {
+    if constexpr (BF16) {
+        const uint2 v = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + at);
+        f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xFFFF0000u);
+        f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xFFFF0000u);
+    } else {
+        const float4 v = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
+        f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
+    }
+}
+template <bool BF16>
+__device__ __forceinline__ void store4(void* p, uint32_t at, const float (&f)[4]) {
+    if constexpr (BF16) {
+        typedef __attribute__((ext_vector_type(2))) float f32x2;
+        typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+        const uint2 v = make_uint2(__builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{f[0], f[1]}, bf16x2)),
+                                   __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{f[2], f[3]}, bf16x2)));
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + at) = v;
+    } else {
+        *reinterpret_cast<float4*>(static_cast<float*>(p) + at) = make_float4(f[0], f[1], f[2], f[3]);
+    }
+}
+
+// acc[i][j]: 16 x 16 block i of the wave's rows, j of its columns; a lane has row l16 of a block and four columns from 4 kq on.
+// GLU: blocks j < NB / 2 are gate columns, the others the up columns of the same outputs.  What is optional goes over the
+// accumulators in a pass of its own, so that a call pays for what it asks for and the code stays small.
+template <bool BF16, int MODE, bool GLU, int MB, int NB>
+__device__ __forceinline__ void store_tile(const LinearParams& p, const Tile& t, f32x4 (&acc)[MB][NB], int m_wave, int n_wave) {
+    constexpr int NO = GLU ? NB / 2 : NB;
+    const int lane = threadIdx.x & 63, l16 = lane & 15, kq = lane >> 4;
+    const int limit = (MODE == WEIGHT ? p.M : t.count) - t.m0, n_first = t.n0 + n_wave + 4 * kq;
+    // uniform start of the tile, 32-bit offsets in it (one register, made anew in each pass: the passes' common addresses kept across them
+    // would not fit)
+    const size_t tile = ((MODE == WEIGHT ? static_cast<size_t>(t.e) * p.M : static_cast<size_t>(t.first)) + t.m0) * p.N;
+    auto each = [&](auto&& f) {
+        int m = m_wave + l16;
+        asm volatile("" : "+v"(m));
+#pragma unroll
+        for (int i = 0; i < MB; ++i, m += 16) {
+            const uint32_t row = static_cast<uint32_t>(m) * p.N + n_first;
+#pragma unroll
+            for (int j = 0; j < NO; ++j)
+                if (m < limit && n_first + j * 16 < p.N) f(i, j, row + j * 16);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto put = [&](void* to, auto&& of) {
+        char* base = static_cast<char*>(to) + tile * (BF16 ? 2 : 4);
+        each([&](int i, int j, uint32_t at) {
+            const f32x4& v = of(i, j);
+            const float f[4] = {v[0], v[1], v[2], v[3]};
+            store4<BF16>(base, at, f);
+        });
+    };
+    if constexpr (MODE == FORWARD) {
+#pragma unroll
+        for (int h = 0; h < (GLU ? 2 : 1); ++h) {
+            if (p.bias[h]) {
+#pragma unroll
+                for (int j = 0; j < NO; ++j) {
+                    float b[4] = {0.f, 0.f, 0.f, 0.f};
+                    if (n_first + j * 16 < p.N) load4<false>(p.bias[h] + static_cast<size_t>(t.e) * p.N, n_first + j * 16, b);
+#pragma unroll
+                    for (int i = 0; i < MB; ++i)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) acc[i][h * NO + j][v] += b[v];
+                }
+            }
+            if (p.pre[h]) put(p.pre[h], [&](int i, int j) -> const f32x4& { return acc[i][h * NO + j]; });
+        }
+        auto map = [&](auto&& f) {
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j = 0; j < NO; ++j) {
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) acc[i][j][v] = f(acc[i][j][v], GLU ? acc[i][(GLU ? NO : 0) + j][v] : 1.0f);
+                    __builtin_amdgcn_sched_barrier(0);   // one block at a time: keeps the live set small
+                }
+        };
+        if constexpr (GLU) {
+            map([](float a, float u) { return a * sigmoid(a) * u; });
+        } else {
+            if (p.act == ETR_ACT_SILU) map([](float a, float) { return a * sigmoid(a); });
+            // (the empty statements keep the compiler from making one pass of the two, with both results of every value alive)
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j = 0; j < NO; ++j) asm volatile("" : "+v"(acc[i][j]));
+            if (p.act == ETR_ACT_GELU) map([](float a, float) { return a * normal_cdf(a); });
+        }
+        if (p.residual) {
+            const char* base = static_cast<const char*>(p.residual) + tile * (BF16 ? 2 : 4);
+            each([&](int i, int j, uint32_t at) {
+                float r[4];
+                load4<BF16>(base, at, r);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[i][j][v] += r[v];
+            });
+        }
+    }
+    put(p.C[MODE == WEIGHT ? t.half : 0], [&](int i, int j) -> const f32x4& { return acc[i][j]; });
+}
+
+// ---- the products ----------------------------------------------------------------------------------------------------
+//
+// A k-tile is 128 bytes of contraction (64 bf16, 32 fp32).  LDS, one operand of one k-tile:
+//   rows kind     [row][8 pieces]; the piece at place s of a row is s ^ (row / 2 % 8), so that the 16 rows of a fragment spread over
+//                 the banks
+//   columns kind  bf16: [group of 64 columns][k][64 columns], the 16-column blocks of a k row in the order o ^ f(k), f(k) = bit 1 of
+//                 k and twice bit 3, for the transposing reads; fp32: [k][columns], the piece at place s of a k row is s ^ 4 (k / 4 % 4)
+// A workgroup of WM x WN waves has a BM x BN tile at a time; NBUF buffers, of which all but one are on their way.
+// The MFMAs take the columns' fragment first, so that a lane ends up with four neighbouring columns of one row.
+template <bool BF16, int BM, int BN, int WM, int WN, int NBUF, int MODE, bool GLU>
+__global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) {
+    constexpr bool AT = MODE == WEIGHT, BT = MODE != FORWARD;
+    static_assert(!GLU || MODE == FORWARD, "two weights side by side: the forward product only");
+    constexpr int ES = BF16 ? 2 : 4, KE = 128 / ES, PE = 16 / ES;        // bytes of an element; elements of a k-tile, of a piece
+    constexpr int NW = WM * WN, MB = BM / WM / 16, NB = BN / WN / 16;
+    constexpr int CA = BM / 8 / NW, CB = BN / 8 / NW;    // copies of 64 pieces per wave, operand and k-tile
+    static_assert(CA * NW * 8 == BM && CB * NW * 8 == BN, "whole copies for every wave");
+    static_assert((!AT || BM % 64 == 0) && (!BT || BN % 64 == 0), "columns come in groups of 64");
+    constexpr int A_BYTES = BM * 128, STAGE = (BM + BN) * 128, OUT_N = GLU ? BN / 2 : BN;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    const int lane = threadIdx.x & 63, l16 = lane & 15, kq = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
+
+    Groups groups;
+    groups.load(p, BM);
+    int share;
+    Tile t;
+    int j = blockIdx.x >> 3;
+    if (!find_tile<MODE>(p, groups, BM, OUT_N, j, share, t)) return;
+
+    // k-tiles of a tile, of each half of a contraction in two halves (INPUT of SwiGLU)
+    const int two = MODE == INPUT && p.glu ? 2 : 1;
+    auto half_tiles = [&](const Tile& x) { return MODE == WEIGHT ? max((x.count + KE - 1) / KE, 1) : (p.K + KE - 1) / KE; };
+
+    // ---- the copy side: a tile and a k-tile of its own, ahead of the products
+    // copy c of an operand: 64 pieces, lane after lane; the k (columns kind) or first k (rows kind) of a lane's piece in its k-tile, and
+    // its first column
+    auto columns_k = [&](int c, int width) { return BF16 ? 8 * (c & 7) + (lane >> 3) : (c * 64 + lane) / (width / 4); };
+    auto columns_at = [&](int c, int width) {
+        const int k = columns_k(c, width);
+        if constexpr (BF16) return 64 * (c >> 3) + 16 * (((lane & 7) >> 1) ^ (((k >> 1) & 1) | ((k >> 2) & 2))) + 8 * (lane & 1);
+        else return 4 * ((lane % (width / 4)) ^ (4 * ((k >> 2) & 3)));
+    };
+    auto rows_piece = [&](int c) { return (lane & 7) ^ (((8 * c + (lane >> 3)) >> 1) & 7); };
+    struct Source { uint64_t A, B[2]; uint32_t a[CA], b[CB]; int KTh, length, kt; };
+    Source s;
+    bool more = true;                                    // s is a tile that is still to be copied
+    auto aim = [&](const Tile& x) {
+        s.KTh = half_tiles(x);
+        s.length = MODE == WEIGHT ? x.count : p.K;
+        s.kt = 0;
+        if constexpr (AT) s.A = reinterpret_cast<uint64_t>(p.A[x.half]) + static_cast<uint64_t>(x.first) * p.lda * ES;
+        else s.A = static_cast<uint64_t>(x.first + x.m0) * p.lda * ES;                                   // + the half's array
+        const uint64_t group = MODE == WEIGHT ? static_cast<uint64_t>(x.first) * p.ldb * ES
+                                              : static_cast<uint64_t>(x.e) * (MODE == FORWARD ? p.N : p.K) * p.ldb * ES;
+        s.B[0] = reinterpret_cast<uint64_t>(p.B[0]) + group;
+        s.B[1] = GLU || two == 2 ? reinterpret_cast<uint64_t>(p.B[1]) + group : 0;
+#pragma unroll
+        for (int i = 0; i < CA; ++i) {
+            const int c = wave * CA + i;
+            if constexpr (AT) s.a[i] = (static_cast<uint32_t>(columns_k(c, BM)) * p.lda + min(x.m0 + columns_at(c, BM), p.M - PE)) * ES;
+            else s.a[i] = static_cast<uint32_t>(min(8 * c + (lane >> 3), x.count - 1 - x.m0)) * p.lda * ES + rows_piece(c) * 16u;
+        }
+#pragma unroll
+        for (int i = 0; i < CB; ++i) {
+            const int c = wave * CB + i;
+            if constexpr (BT) {
+                s.b[i] = (static_cast<uint32_t>(columns_k(c, BN)) * p.ldb + min(x.n0 + columns_at(c, BN), p.N - PE)) * ES;
+            } else {
+                const int r = 8 * c + (lane >> 3), n = x.n0 + (GLU && r >= BN / 2 ? r - BN / 2 : r);
+                s.b[i] = static_cast<uint32_t>(min(n, p.N - 1)) * p.ldb * ES + rows_piece(c) * 16u;
+            }
+        }
+    };
+    auto issue = [&](int buf) {
+        const int h = s.kt >= s.KTh ? 1 : 0, kt = s.kt - h * s.KTh;
+        const int left = s.length - kt * KE;             // of the contraction, from this k-tile on
+        const uint64_t a = AT ? s.A + static_cast<uint64_t>(kt) * KE * ES * p.lda
+                              : s.A + reinterpret_cast<uint64_t>(p.A[h]) + static_cast<uint64_t>(kt) * 128;
+        unsigned char* dst = lds + buf * STAGE;
+#pragma unroll
+        for (int i = 0; i < CA; ++i) {
+            const int c = wave * CA + i, k = AT ? columns_k(c, BM) : PE * rows_piece(c);
+            copy_piece(a, k < left ? s.a[i] : kPast, dst + c * 1024);
+        }
+#pragma unroll
+        for (int i = 0; i < CB; ++i) {
+            const int c = wave * CB + i, k = BT ? columns_k(c, BN) : PE * rows_piece(c);
+            const uint64_t b = s.B[GLU ? (c >= BN / 16 ? 1 : 0) : h] + static_cast<uint64_t>(kt) * (BT ? static_cast<uint64_t>(KE) * ES * p.ldb : 128);
+            copy_piece(b, k < left ? s.b[i] : kPast, dst + A_BYTES + c * 1024);
+        }
+    };
+    int jn = j;
+    auto advance = [&]() {                               // (a source past the last tile goes on copying its last k-tile)
+        if (!more) return;
+        if (s.kt + 1 < s.KTh * two) { ++s.kt; return; }
+        jn += gridDim.x >> 3;
+        Tile n;
+        int unused;
+        if (find_tile<MODE>(p, groups, BM, OUT_N, jn, unused, n)) aim(n);
+        else more = false;
+    };
+
+    // ---- the product side
+    struct Fragment { float f[4]; };                     // bf16: 8 values of k; fp32: 4
+    auto fragment = [&](const unsigned char* op, bool columns, int width, int block, int ks) -> Fragment {
+        Fragment r;
+        if (!columns) {
+            const int row = block * 16 + l16;
+            const float4 v = *reinterpret_cast<const float4*>(op + row * 128 + ((4 * ks + kq) ^ ((row >> 1) & 7)) * 16);
+            r.f[0] = v.x; r.f[1] = v.y; r.f[2] = v.z; r.f[3] = v.w;
+        } else if constexpr (BF16) {
+            const int q = l16 & 3, jj = l16 >> 2, f = ((jj >> 1) & 1) | ((kq & 1) << 1);
+            const unsigned char* at = op + (block >> 2) * 8192 + (32 * ks + 8 * kq + jj) * 128 + (((block & 3) ^ f) * 32) + q * 8;
+            typedef __attribute__((address_space(3))) s16x4* tr_ptr;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)at);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(at + 512));
+            typedef __attribute__((ext_vector_type(2))) float f32x2;
+            const f32x2 l = __builtin_bit_cast(f32x2, lo), h = __builtin_bit_cast(f32x2, hi);
+            r.f[0] = l[0]; r.f[1] = l[1]; r.f[2] = h[0]; r.f[3] = h[1];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int k = 16 * ks + 4 * kq + i, col = block * 16 + l16;
+                r.f[i] = *reinterpret_cast<const float*>(op + k * width * 4 + (((col >> 2) ^ (4 * kq)) * 16) + (col & 3) * 4);
+            }
+        }
+        return r;
+    };
+    auto multiply = [&](const Fragment& b, const Fragment& a, f32x4 c) -> f32x4 {
+        if constexpr (BF16) {
+            return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(b.f[i], a.f[i], c, 0, 0, 0);
+            return c;
+        }
+    };
+    // GLU: the first half of the staged weight rows are gate rows, the second the up rows of the same outputs
+    auto b_block = [&](int jb) { return GLU ? (jb >= NB / 2 ? BN / 32 : 0) + wn * (NB / 2) + (jb >= NB / 2 ? jb - NB / 2 : jb) : wn * NB + jb; };
+
+    f32x4 acc[MB][NB];
+    aim(t);
+#pragma unroll
+    for (int b = 0; b < NBUF - 1; ++b) { issue(b); advance(); }
+    int buf = 0;
+    for (;;) {
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+            for (int jb = 0; jb < NB; ++jb) acc[i][jb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const int KT = half_tiles(t) * two;
+        for (int kt = 0; kt < KT; ++kt) {
+            wait_copies<(NBUF - 2) * (CA + CB)>();       // this wave's part of the k-tile has landed
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();                // ... and everybody's; and everybody is done with the buffer before it
+            asm volatile("" ::: "memory");
+            issue(buf == 0 ? NBUF - 1 : buf - 1);
+            advance();
+            const unsigned char* op = lds + buf * STAGE;
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                Fragment fb[NB];
+#pragma unroll
+                for (int jb = 0; jb < NB; ++jb) fb[jb] = fragment(op + A_BYTES, BT, BN, b_block(jb), ks);
+#pragma unroll
+                for (int i = 0; i < MB; ++i) {
+                    const Fragment fa = fragment(op, AT, BM, wm * MB + i, ks);
+#pragma unroll
+                    for (int jb = 0; jb < NB; ++jb) acc[i][jb] = multiply(fb[jb], fa, acc[i][jb]);
+                }
+            }
+            buf = buf + 1 == NBUF ? 0 : buf + 1;
+        }
+        store_tile<BF16, MODE, GLU, MB, NB>(p, t, acc, wm * MB * 16, GLU ? wn * (NB / 2) * 16 : wn * NB * 16);
+        j += gridDim.x >> 3;
+        int unused;
+        if (!find_tile<MODE>(p, groups, BM, OUT_N, j, unused, t)) break;
+        wait_copies<0>();                                // (the stores too: the counted waits are for copies alone)
+    }
+    wait_copies<0>();                                    // the copies that nobody needed
+}
+
+// ---- the element-wise middle of the backward ----------------------------------------------------------------------------
+//
+// da = dy act'(a) (db = dy SiLU(a)) and the column sums of both over 128 rows of an expert, before they are rounded.  A workgroup has such
+// a chunk of rows and 64 pieces of columns; a wave every fourth row of it.  Bound by memory: one or two rows of pre-activations and
+// one of dy in, one or two out.
+constexpr int kChunk = 128;
+struct MiddleParams {
+    const piece_t* pre; const piece_t* pre_up; const piece_t* dy; piece_t* da; piece_t* db;
+    float* part;            // [2 with SwiGLU][chunks][N], optional
+    const int32_t* offsets;
+    int rows, E, N, pieces, act, chunks;
+};
+template <bool BF16>
+__global__ __launch_bounds__(256) void linear_middle_kernel(MiddleParams p) {
+    using R = Piece<BF16>;
+    constexpr int V = R::kN;
+    __shared__ float sums[3][64][2 * V];
+    LinearParams q{};
+    q.offsets = p.offsets; q.rows = p.rows; q.E = p.E;
+    Groups g;
+    g.load(q, kChunk);
+    const int chunk = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (chunk >= __builtin_amdgcn_readlane(g.tiles_incl, 63)) return;
+    const int e = __builtin_ctzll(__ballot(g.tiles_incl > chunk));
+    const int in_group = chunk - (__builtin_amdgcn_readlane(g.tiles_incl, e) - __builtin_amdgcn_readlane(g.tiles, e));
+    const int first = __builtin_amdgcn_readlane(g.first, e) + in_group * kChunk;
+    const int n_rows = min(kChunk, __builtin_amdgcn_readlane(g.count, e) - in_group * kChunk);
+    const int c = blockIdx.y * 64 + lane;
+    const bool in = c < p.pieces, glu = p.act == ETR_ACT_SWIGLU;
+    float sa[V], sb[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) sa[i] = sb[i] = 0.f;
+    for (int r = wave; in && r < n_rows; r += 4) {
+        const size_t at = static_cast<size_t>(first + r) * p.pieces + c;
+        float d[V], a[V], b[V];
+        R::unpack(p.dy[at], d);
+        if (p.act != ETR_ACT_NONE) R::unpack(p.pre[at], a);
+        if (glu) R::unpack(p.pre_up[at], b);
+        if (p.act == ETR_ACT_GELU) {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                a[i] = d[i] * (normal_cdf(a[i]) + a[i] * 0.39894228040143268f * __expf(-0.5f * a[i] * a[i]));
+        } else if (p.act != ETR_ACT_NONE) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float sg = sigmoid(a[i]), grad = sg * (1.0f + a[i] * (1.0f - sg));
+                const float up = glu ? b[i] : 1.0f;
+                b[i] = d[i] * a[i] * sg;
+                a[i] = d[i] * up * grad;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) a[i] = d[i];
+        }
+        if (p.da) p.da[at] = R::pack(a);
+        if (glu && p.db) p.db[at] = R::pack(b);
+#pragma unroll
+        for (int i = 0; i < V; ++i) { sa[i] += a[i]; sb[i] += glu ? b[i] : 0.f; }
+    }
+    if (!p.part) return;
+    if (wave > 0) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) { sums[wave - 1][lane][i] = sa[i]; sums[wave - 1][lane][V + i] = sb[i]; }
+    }
+    __syncthreads();
+    if (wave > 0 || !in) return;
+    float* out = p.part + static_cast<size_t>(chunk) * p.N + static_cast<size_t>(c) * V;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        out[i] = ((sa[i] + sums[0][lane][i]) + sums[1][lane][i]) + sums[2][lane][i];
+        if (glu) out[static_cast<size_t>(p.chunks) * p.N + i] = ((sb[i] + sums[0][lane][V + i]) + sums[1][lane][V + i]) + sums[2][lane][V + i];
+    }
+}
+
+// dbias[e][n]: the chunks of expert e, four groups of them side by side, in a fixed order
+__global__ __launch_bounds__(256) void linear_bias_kernel(MiddleParams p, float* dbias, float* dbias_up) {
+    __shared__ float sums[4][64];
+    LinearParams q{};
+    q.offsets = p.offsets; q.rows = p.rows; q.E = p.E;
+    Groups g;
+    g.load(q, kChunk);
+    const int e = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.x * 64 + lane;
+    const int tiles = __builtin_amdgcn_readlane(g.tiles, e), begin = __builtin_amdgcn_readlane(g.tiles_incl, e) - tiles;
+    const float* part = p.part + static_cast<size_t>(blockIdx.z) * p.chunks * p.N;
+    float s = 0.f;
+    if (n < p.N) {
+#pragma unroll 4
+        for (int i = wave; i < tiles; i += 4) s += part[static_cast<size_t>(begin + i) * p.N + n];
+    }
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && n < p.N) (blockIdx.z ? dbias_up : dbias)[static_cast<size_t>(e) * p.N + n] = ((sums[0][lane] + sums[1][lane]) + sums[2][lane]) + sums[3][lane];
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+
+long long tiles_at_most(const LinearParams& p, int mode, int BM, int out_n) {
+    const long long columns = (p.N + out_n - 1) / out_n;
+    if (mode == WEIGHT) return columns * ((p.M + BM - 1) / BM) * p.E * (p.glu ? 2 : 1);
+    // full tiles of all rows together, and one more in part for each group
+    return columns * (p.rows / BM + std::min(p.E, p.rows));
+}
+
+template <bool BF16, int BM, int BN, int WM, int WN, int NBUF, int MODE, bool GLU>
+hipError_t launch_tiles(LinearParams p, hipStream_t st) {
+    constexpr size_t lds = static_cast<size_t>(BM + BN) * 128 * NBUF;
+    auto kern = linear_kernel<BF16, BM, BN, WM, WN, NBUF, MODE, GLU>;
+    const hipError_t err = ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds);
+    if (err != hipSuccess) return err;
+    p.NT = (p.N + (GLU ? BN / 2 : BN) - 1) / (GLU ? BN / 2 : BN);
+    const long long tiles = tiles_at_most(p, MODE, BM, GLU ? BN / 2 : BN);
+    if (tiles > (1ll << 30)) return hipErrorInvalidValue;
+    // one workgroup on each CU that walks the tiles, or (small tiles) one for each of them
+    const long long most = BM * BN >= 256 * 256 ? cu_count() / 8 : 1 << 17;
+    const long long blocks = std::min((tiles + 7) / 8, most) * 8;
+    hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(blocks)), dim3(WM * WN * 64), lds, st, p);
+    return hipGetLastError();
+}
+
+template <int MODE, bool GLU>
+hipError_t launch_product(const LinearParams& p, bool bf16, hipStream_t st) {
+    const int out256 = GLU ? 128 : 256;
+    const int rows_each = MODE == WEIGHT ? p.M : (p.rows + p.E - 1) / p.E;           // rows of a group, on average
+    const long long groups = MODE == WEIGHT ? p.E * (p.glu ? 2 : 1) : std::min(p.E, p.rows);
+    auto tiles = [&](int BM, int BN) { return groups * ((rows_each + BM - 1) / BM) * ((p.N + BN - 1) / BN); };
+    if (!bf16) {
+        if (tiles(128, out256 / 2) >= 2ll * cu_count()) return launch_tiles<false, 128, 128, 2, 2, 2, MODE, GLU>(p, st);
+        return launch_tiles<false, 64, 64, 2, 2, 3, MODE, GLU>(p, st);
+    }
+    if constexpr (MODE != WEIGHT) {
+        if (rows_each <= 32) {
+            if constexpr (GLU || MODE == INPUT) return launch_tiles<true, 32, 128, 1, 4, 4, MODE, GLU>(p, st);
+            else return launch_tiles<true, 32, 64, 1, 4, 4, MODE, GLU>(p, st);
+        }
+    }
+    if (tiles(256, out256) >= cu_count() / 2) return launch_tiles<true, 256, 256, 2, 4, 2, MODE, GLU>(p, st);
+    return launch_tiles<true, 128, 128, 2, 2, 2, MODE, GLU>(p, st);
+}
+
+int chunks_at_most(const etr_linear_config& c) { return c.rows / kChunk + std::min(c.E, c.rows); }
+size_t middle_bytes(const etr_linear_config& c) {
+    return c.act == ETR_ACT_NONE ? 0 : align_up(static_cast<size_t>(c.rows) * c.N * elt_bytes(c.dtype));
+}
+
+}  // namespace
+
+size_t linear_ws_bytes(const etr_linear_config& c) {
+    const int n = c.act == ETR_ACT_SWIGLU ? 2 : 1;
+    return n * middle_bytes(c) + align_up(static_cast<size_t>(n) * chunks_at_most(c) * c.N * 4);
+}
+
+hipError_t launch_expert_linear(const etr_linear_config& c, const void* x, const int32_t* offsets, const void* w, const void* w_up, const float* bias,
+                                const float* bias_up, const void* residual, void* y, void* pre, void* pre_up, hipStream_t st) {
+    LinearParams p{};
+    p.A[0] = x; p.B[0] = w; p.B[1] = w_up; p.C[0] = y;
+    p.offsets = offsets; p.bias[0] = bias; p.bias[1] = bias_up; p.residual = residual; p.pre[0] = pre; p.pre[1] = pre_up;
+    p.rows = c.rows; p.E = c.E; p.N = c.N; p.K = c.K; p.lda = p.ldb = c.K; p.act = c.act; p.glu = c.act == ETR_ACT_SWIGLU;
+    return p.glu ? launch_product<FORWARD, true>(p, c.dtype == ETR_BF16, st) : launch_product<FORWARD, false>(p, c.dtype == ETR_BF16, st);
+}
+
+hipError_t launch_expert_linear_backward(const etr_linear_config& c, const void* x, const int32_t* offsets, const void* w, const void* w_up,
+                                         const void* pre, const void* pre_up, const void* dy, void* dx, void* dw, void* dw_up, float* dbias,
+                                         float* dbias_up, void* ws, hipStream_t st) {
+    const bool glu = c.act == ETR_ACT_SWIGLU, bf16 = c.dtype == ETR_BF16;
+    char* at = static_cast<char*>(ws);
+    const size_t middle = middle_bytes(c);
+    void* da = c.act == ETR_ACT_NONE ? nullptr : at;
+    void* db = glu ? at + middle : nullptr;
+    const MiddleParams m{static_cast<const piece_t*>(pre), static_cast<const piece_t*>(pre_up), static_cast<const piece_t*>(dy), static_cast<piece_t*>(da),
+                         static_cast<piece_t*>(db), dbias ? reinterpret_cast<float*>(at + (glu ? 2 : 1) * middle) : nullptr, offsets, c.rows, c.E, c.N,
+                         static_cast<int>(static_cast<size_t>(c.N) * elt_bytes(c.dtype) / 16), c.act, chunks_at_most(c)};
+    hipError_t err;
+    if (da || dbias) {
+        const dim3 grid(m.chunks, (m.pieces + 63) / 64);
+        if (bf16) hipLaunchKernelGGL(linear_middle_kernel<true>, grid, dim3(256), 0, st, m);
+        else hipLaunchKernelGGL(linear_middle_kernel<false>, grid, dim3(256), 0, st, m);
+        if ((err = hipGetLastError()) != hipSuccess) return err;
+    }
+    if (dbias) {
+        hipLaunchKernelGGL(linear_bias_kernel, dim3((c.N + 63) / 64, c.E, glu ? 2 : 1), dim3(256), 0, st, m, dbias, dbias_up);
+        if ((err = hipGetLastError()) != hipSuccess) return err;
+    }
+    LinearParams p{};
+    p.offsets = offsets; p.rows = c.rows; p.E = c.E; p.glu = glu;
+    p.A[0] = da ? da : dy; p.A[1] = db;
+    if (dx) {
+        p.B[0] = w; p.B[1] = w_up; p.C[0] = dx;
+        p.N = c.K; p.K = c.N; p.lda = c.N; p.ldb = c.K;
+        if ((err = launch_product<INPUT, false>(p, bf16, st)) != hipSuccess) return err;
+    }
+    if (dw) {
+        p.B[0] = x; p.B[1] = nullptr; p.C[0] = dw; p.C[1] = dw_up;
+        p.M = c.N; p.N = c.K; p.K = c.rows; p.lda = c.N; p.ldb = c.K;
+        if ((err = launch_product<WEIGHT, false>(p, bf16, st)) != hipSuccess) return err;
+    }
+    return hipSuccess;
+}
+
+}  // namespace etr

@@ -111,3 +111,44 @@ def test_types_and_strides_that_the_binding_refuses():
     cfg = B.make_norm_config(4, 64, F)
     with pytest.raises(ValueError):                            # a strided view
         B.etr_block_norm(cfg, torch.zeros(4, 128)[:, ::2], w_pre=torch.ones(64), h=torch.zeros(4, 64))
+
+
+@pytest.mark.parametrize("cfg,status", [
+    (B.make_linear_config(0, 64, 64, 1, F), SHAPE), (B.make_linear_config(4, 0, 64, 1, F), SHAPE), (B.make_linear_config(4, 64, -8, 1, F), SHAPE),
+    (B.make_linear_config(4, 64, 64, 0, F), SHAPE), (B.make_linear_config(4, 60, 64, 1, F), UNSUPPORTED), (B.make_linear_config(4, 64, 60, 1, F), UNSUPPORTED),
+    (B.make_linear_config(4, 64, 64, 65, F), UNSUPPORTED), (B.make_linear_config(4, 64, 64, 1, 2), UNSUPPORTED),
+    (B.make_linear_config(4, 64, 64, 1, F, act=4), UNSUPPORTED), (B.make_linear_config(4, 64, 64, 1, F, act=-1), UNSUPPORTED),
+    (B.make_linear_config(4, (1 << 20) + 8, 64, 1, F), UNSUPPORTED), (B.make_linear_config((1 << 28) + 1, 64, 64, 1, F), UNSUPPORTED),
+    (B.make_linear_config(4, 1 << 20, 1 << 20, 64, F), UNSUPPORTED)])
+def test_linear_configs(lib, cfg, status):
+    c = ctypes.byref(cfg)
+    assert B.etr_linear_workspace_bytes(cfg) == 0
+    assert lib.etr_expert_linear(c, ok, ok, ok, null, null, null, null, ok, null, null, null) == status
+    assert lib.etr_expert_linear_backward(c, ok, ok, ok, null, ok, null, ok, ok, ok, null, ok, null, ok, 1 << 40, null) == status
+
+
+def test_linear_arguments(lib):
+    plain, glu, one = (ctypes.byref(B.make_linear_config(40, 64, 64, e, F, act=a)) for e, a in ((2, B.ACT_SILU), (2, B.ACT_SWIGLU), (1, B.ACT_NONE)))
+    f = lambda c, *a: lib.etr_expert_linear(c, *a, null)       # x offsets w w_up bias bias_up residual y pre pre_up
+    assert lib.etr_expert_linear(None, ok, ok, ok, null, null, null, null, ok, null, null, null) == NULL
+    for i in (0, 1, 2, 7):
+        assert f(plain, *[null if j == i else (ok if j in (0, 1, 2, 7) else null) for j in range(10)]) == NULL
+    assert f(one, null, null, ok, null, null, null, null, ok, null, null) == NULL
+    assert f(plain, ok, ok, ok, ok, null, null, null, ok, null, null) == NULL           # w_up and nothing to do with it
+    assert f(plain, ok, ok, ok, null, null, ok, null, ok, null, null) == NULL           # bias_up likewise
+    assert f(plain, ok, ok, ok, null, null, null, null, ok, null, ok) == NULL
+    assert f(glu, ok, ok, ok, null, null, null, null, ok, null, null) == NULL           # no w_up
+    assert f(glu, ok, ok, ok, ok, ok, null, null, ok, null, null) == NULL               # one bias of two
+    assert f(glu, ok, ok, ok, ok, null, null, null, ok, ok, null) == NULL               # one pre-activation of two
+    for i in range(10):
+        assert f(glu, *[odd if j == i else ok for j in range(10)]) == ALIGN
+    b = lambda c, *a, ws=ok, n=1 << 30: lib.etr_expert_linear_backward(c, *a, ws, n, null)   # x off w w_up pre pre_up dy dx dw dw_up dbias dbias_up
+    full = [ok] * 12
+    for i in (0, 1, 2, 3, 4, 5, 6, 9, 11):
+        assert b(glu, *[null if j == i else ok for j in range(12)]) == NULL, i
+    for i in range(12):
+        assert b(glu, *[odd if j == i else ok for j in range(12)]) == ALIGN
+    assert b(glu, *full, ws=null) == NULL and b(glu, *full, n=16) == WORKSPACE
+    assert b(glu, ok, ok, ok, ok, ok, ok, ok, null, null, null, null, null) == NULL     # nothing asked for
+    assert b(plain, ok, ok, ok, null, ok, null, ok, ok, ok, ok, null, null) == NULL     # dw_up and no second weight
+    assert b(plain, ok, ok, ok, null, null, null, ok, ok, ok, null, null, null) == NULL # an activation and no pre-activation
