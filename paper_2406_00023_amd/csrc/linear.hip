@@ -330,8 +330,8 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
         Fragment r;
         if (!columns) {
             const int row = block * 16 + l16;
-            const float4 v = *reinterpret_cast<const float4*>(op + row * 128 + ((4 * ks + kq) ^ ((row >> 1) & 7)) * 16);
-            r.f[0] = v.x; r.f[1] = v.y; r.f[2] = v.z; r.f[3] = v.w;
+            const f32x4 v = *reinterpret_cast<const f32x4*>(op + row * 128 + ((4 * ks + kq) ^ ((row >> 1) & 7)) * 16);
+            r.f[0] = v[0]; r.f[1] = v[1]; r.f[2] = v[2]; r.f[3] = v[3];
         } else if constexpr (BF16) {
             const int q = l16 & 3, jj = l16 >> 2, f = ((jj >> 1) & 1) | ((kq & 1) << 1);
             const unsigned char* at = op + (block >> 2) * 8192 + (32 * ks + 8 * kq + jj) * 128 + (((block & 3) ^ f) * 32) + q * 8;
@@ -351,65 +351,234 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
         return r;
     };
     auto multiply = [&](const Fragment& b, const Fragment& a, f32x4 c) -> f32x4 {
-        if constexpr (BF16) {
-            return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(b.f[i], a.f[i], c, 0, 0, 0);
-            return c;
-        }
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
     };
     // GLU: the first half of the staged weight rows are gate rows, the second the up rows of the same outputs
     auto b_block = [&](int jb) { return GLU ? (jb >= NB / 2 ? BN / 32 : 0) + wn * (NB / 2) + (jb >= NB / 2 ? jb - NB / 2 : jb) : wn * NB + jb; };
 
     f32x4 acc[MB][NB];
-    aim(t);
-#pragma unroll
-    for (int b = 0; b < NBUF - 1; ++b) { issue(b); advance(); }
-    int buf = 0;
-    for (;;) {
+    auto clear = [&]() {
 #pragma unroll
         for (int i = 0; i < MB; ++i)
 #pragma unroll
             for (int jb = 0; jb < NB; ++jb) acc[i][jb] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const int KT = half_tiles(t) * two;
-        for (int kt = 0; kt < KT; ++kt) {
-            wait_copies<(NBUF - 2) * (CA + CB)>();       // this wave's part of the k-tile has landed
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_s_barrier();                // ... and everybody's; and everybody is done with the buffer before it
-            asm volatile("" ::: "memory");
-            issue(buf == 0 ? NBUF - 1 : buf - 1);
-            advance();
-            const unsigned char* op = lds + buf * STAGE;
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                Fragment fb[NB];
-#pragma unroll
-                for (int jb = 0; jb < NB; ++jb) fb[jb] = fragment(op + A_BYTES, BT, BN, b_block(jb), ks);
-#pragma unroll
-                for (int i = 0; i < MB; ++i) {
-                    const Fragment fa = fragment(op, AT, BM, wm * MB + i, ks);
-#pragma unroll
-                    for (int jb = 0; jb < NB; ++jb) acc[i][jb] = multiply(fb[jb], fa, acc[i][jb]);
-                }
-            }
-            buf = buf + 1 == NBUF ? 0 : buf + 1;
-        }
-        store_tile<BF16, MODE, GLU, MB, NB>(p, t, acc, wm * MB * 16, GLU ? wn * (NB / 2) * 16 : wn * NB * 16);
+    };
+    auto store = [&]() { store_tile<BF16, MODE, GLU, MB, NB>(p, t, acc, wm * MB * 16, GLU ? wn * (NB / 2) * 16 : wn * NB * 16); };
+    auto next_tile = [&]() {
         j += gridDim.x >> 3;
         int unused;
-        if (!find_tile<MODE>(p, groups, BM, OUT_N, j, unused, t)) break;
-        wait_copies<0>();                                // (the stores too: the counted waits are for copies alone)
+        return find_tile<MODE>(p, groups, BM, OUT_N, j, unused, t);
+    };
+    auto barrier = [&]() {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    aim(t);
+    if constexpr (BF16 && MB == 8 && NB == 4 && NBUF == 2) {
+        // 128 rows x 64 columns to a wave, one workgroup to a CU: nothing else covers a wait, so the loop is written out.  A k-tile is four
+        // substeps of 16 MFMAs: k-step 0 and 1 of row blocks 0 - 3 and 4 - 7.  Fragments are read a substep ahead; the barrier stands
+        // before the last substep, when all reads of the buffer are done: behind it go the next k-tile's first reads (that it has landed is
+        // what was waited for), and the copies of the one after that into the buffer just left.
+        // Transposing reads are assembly: through the builtin each of them waits for all copies on their way, because it is taken to alias
+        // what they write.  A statement holds 8 MFMAs (two row blocks, four column blocks), behind the first of them the reads of up to
+        // four fragments, and its own wait at the end, so that they land under the other MFMAs and its outputs are ordinary registers.  What the
+        // compiler cannot see in it: two wait states between an ordinary write of an operand and the MFMA (the s_nop in front), and
+        // that an accumulator is not to be touched right behind (settle, before the epilogue).
+        Fragment fa[2][4], fb[2][4];
+        const int tr_q = l16 & 3, tr_j = l16 >> 2, tr_f = ((tr_j >> 1) & 1) | ((kq & 1) << 1);
+        uint32_t tr[4];                                  // this lane's place of the four 16-column blocks of a group
+#pragma unroll
+        for (int o = 0; o < 4; ++o)
+            tr[o] = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr)lds)) + (8 * kq + tr_j) * 128 + ((o ^ tr_f) * 32) + tr_q * 8;
+        const uint32_t tr_a = wm * 16384, tr_b = A_BYTES + wn * 8192;
+        auto read_a = [&](int b, int ks, int h, int i) { fa[h][i] = fragment(lds + b * STAGE, false, BM, wm * MB + 4 * h + i, ks); };
+        auto read_b = [&](int b, int ks, int i) { fb[ks][i] = fragment(lds + b * STAGE + A_BYTES, false, BN, b_block(i), ks); };
+#define ETR_MF(C, B, A) "v_mfma_f32_16x16x32_bf16 %[c" #C "], %[b" #B "], %[a" #A "], %[c" #C "]\n\t"
+#define ETR_REST ETR_MF(1, 0, 1) ETR_MF(3, 1, 1) ETR_MF(2, 1, 0) ETR_MF(4, 2, 0) ETR_MF(5, 2, 1) ETR_MF(7, 3, 1) ETR_MF(6, 3, 0)
+#define ETR_TR(N) "ds_read_b64_tr_b16 %[x" #N "], %[p" #N "] offset:%c[o" #N "]\n\tds_read_b64_tr_b16 %[y" #N "], %[p" #N "] offset:%c[q" #N "]\n\t"
+#define ETR_ACC [c0] "+v"(acc[I][0]), [c1] "+v"(acc[I + 1][0]), [c2] "+v"(acc[I][1]), [c3] "+v"(acc[I + 1][1]), [c4] "+v"(acc[I][2]), \
+                [c5] "+v"(acc[I + 1][2]), [c6] "+v"(acc[I][3]), [c7] "+v"(acc[I + 1][3])
+#define ETR_FRAGMENTS [a0] "v"(a[0]), [a1] "v"(a[1]), [b0] "v"(b[0]), [b1] "v"(b[1]), [b2] "v"(b[2]), [b3] "v"(b[3])
+#define ETR_OUT(N) [x##N] "=&v"(x[N]), [y##N] "=&v"(y[N])
+#define ETR_AT(N) [p##N] "v"(at + tr[F + N]), [o##N] "n"(OFF), [q##N] "n"(OFF + 512)
+        // acc[I], acc[I + 1] += a0[0..1] x b0[0..3]; R fragments from block F of the group at `at` + OFF on into `out`
+        auto mfma8 = [&](auto reads, auto block, const Fragment* a0, const Fragment* b0, Fragment* out, uint32_t at, auto from, auto offset) {
+            constexpr int R = decltype(reads)::value, I = decltype(block)::value, F = decltype(from)::value, OFF = decltype(offset)::value;
+            typedef int v2i __attribute__((ext_vector_type(2)));
+            bf16x8 a[2], b[4];
+            v2i x[4], y[4];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) a[i] = __builtin_bit_cast(bf16x8, a0[i]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) b[i] = __builtin_bit_cast(bf16x8, b0[i]);
+            if constexpr (R == 0)
+                asm volatile("s_nop 1\n\t" ETR_MF(0, 0, 0) ETR_REST : ETR_ACC : ETR_FRAGMENTS);
+            else if constexpr (R == 2)
+                asm volatile("s_nop 1\n\t" ETR_MF(0, 0, 0) ETR_TR(0) ETR_TR(1) ETR_REST "s_waitcnt lgkmcnt(0)"
+                             : ETR_ACC, ETR_OUT(0), ETR_OUT(1) : ETR_FRAGMENTS, ETR_AT(0), ETR_AT(1) : "memory");
+            else
+                asm volatile("s_nop 1\n\t" ETR_MF(0, 0, 0) ETR_TR(0) ETR_TR(1) ETR_TR(2) ETR_TR(3) ETR_REST "s_waitcnt lgkmcnt(0)"
+                             : ETR_ACC, ETR_OUT(0), ETR_OUT(1), ETR_OUT(2), ETR_OUT(3)
+                             : ETR_FRAGMENTS, ETR_AT(0), ETR_AT(1), ETR_AT(2), ETR_AT(3) : "memory");
+            typedef float v2f __attribute__((ext_vector_type(2)));
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const v2f l = __builtin_bit_cast(v2f, x[i]), h = __builtin_bit_cast(v2f, y[i]);
+                out[i].f[0] = l[0]; out[i].f[1] = l[1]; out[i].f[2] = h[0]; out[i].f[3] = h[1];
+            }
+        };
+#undef ETR_MF
+#undef ETR_REST
+#undef ETR_TR
+#undef ETR_ACC
+#undef ETR_FRAGMENTS
+#undef ETR_OUT
+#undef ETR_AT
+#define ETR_INT(V) std::integral_constant<int, (V)>{}
+        // Substep (ks, h); then the next fragments: of A (NH, NKS) and, with NB_KS >= 0, of B, from buffer b.
+        auto substep = [&](auto ks_, auto h_, int b, auto nh_, auto nks_, auto nbks_, auto&& behind) {
+            constexpr int ks = decltype(ks_)::value, h = decltype(h_)::value, nh = decltype(nh_)::value, nks = decltype(nks_)::value,
+                          nbks = decltype(nbks_)::value;
+            const uint32_t slot = static_cast<uint32_t>(b) * STAGE;
+            if constexpr (!BT) {
+#pragma unroll
+                for (int m = 0; m < 16; ++m) {           // neighbours share an operand, back and forth over the row blocks
+                    const int jb = m >> 2, i = jb & 1 ? 3 - (m & 3) : m & 3;
+                    acc[4 * h + i][jb] = multiply(fb[ks][jb], fa[h][i], acc[4 * h + i][jb]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (m < 4) read_a(b, nks, nh, m);
+                    else if (m < 8 && nbks >= 0) read_b(b, nbks, m - 4);
+                    else if (m == 8) behind();
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
+                // first statement: the fragments of B (all four), or the first two of A; second: those of A that are left
+                if constexpr (nbks >= 0)
+                    mfma8(ETR_INT(4), ETR_INT(4 * h), fa[h], fb[ks], fb[nbks < 0 ? 0 : nbks], tr_b + slot, ETR_INT(0), ETR_INT(nbks * 4096));
+                else if constexpr (AT)
+                    mfma8(ETR_INT(2), ETR_INT(4 * h), fa[h], fb[ks], fa[nh], tr_a + slot, ETR_INT(0), ETR_INT(nks * 4096 + nh * 8192));
+                else
+                    mfma8(ETR_INT(0), ETR_INT(4 * h), fa[h], fb[ks], fa[nh], 0u, ETR_INT(0), ETR_INT(0));
+                behind();
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (!AT) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) read_a(b, nks, nh, i);
+                    __builtin_amdgcn_sched_barrier(0);
+                    mfma8(ETR_INT(0), ETR_INT(4 * h + 2), fa[h] + 2, fb[ks], fa[nh], 0u, ETR_INT(0), ETR_INT(0));
+                } else if constexpr (nbks >= 0) {
+                    mfma8(ETR_INT(4), ETR_INT(4 * h + 2), fa[h] + 2, fb[ks], fa[nh], tr_a + slot, ETR_INT(0), ETR_INT(nks * 4096 + nh * 8192));
+                } else {
+                    mfma8(ETR_INT(2), ETR_INT(4 * h + 2), fa[h] + 2, fb[ks], fa[nh] + 2, tr_a + slot, ETR_INT(2), ETR_INT(nks * 4096 + nh * 8192));
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        auto settle = [&]() {                            // nothing behind this reads an accumulator sooner than its MFMA has written it
+            if constexpr (BT) {
+                asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+                for (int i = 0; i < MB; ++i)
+#pragma unroll
+                    for (int jb = 0; jb < NB; ++jb) asm volatile("" : "+v"(acc[i][jb]));
+            }
+        };
+        auto read_first = [&]() {
+            typedef int v2i __attribute__((ext_vector_type(2)));
+            typedef float v2f __attribute__((ext_vector_type(2)));
+            auto columns = [&](uint32_t at) -> Fragment {
+                v2i x, y;
+                asm volatile("ds_read_b64_tr_b16 %0, %2\n\tds_read_b64_tr_b16 %1, %2 offset:512\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x), "=&v"(y) : "v"(at) : "memory");
+                const v2f l = __builtin_bit_cast(v2f, x), h = __builtin_bit_cast(v2f, y);
+                return Fragment{{l[0], l[1], h[0], h[1]}};
+            };
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (AT) fa[0][i] = columns(tr_a + tr[i]);
+                else read_a(0, 0, 0, i);
+                if constexpr (BT) fb[0][i] = columns(tr_b + tr[i]);
+                else read_b(0, 0, i);
+            }
+        };
+        issue(0); advance();
+        issue(1); advance();
+        wait_copies<CA + CB>();
+        barrier();
+        read_first();
+        int buf = 0;
+        do {
+            clear();
+            const int KT = half_tiles(t) * two;
+            for (int kt = 0; kt < KT; ++kt) {
+                substep(ETR_INT(0), ETR_INT(0), buf, ETR_INT(1), ETR_INT(0), ETR_INT(1), [&]() {});
+                substep(ETR_INT(0), ETR_INT(1), buf, ETR_INT(0), ETR_INT(1), ETR_INT(-1), [&]() {});
+                substep(ETR_INT(1), ETR_INT(0), buf, ETR_INT(1), ETR_INT(1), ETR_INT(-1), [&]() {});
+                __builtin_amdgcn_s_waitcnt(0x0070);      // vmcnt(0), lgkmcnt(0): the next k-tile is here, this wave's reads are done
+                barrier();
+                __builtin_amdgcn_sched_barrier(0);
+                substep(ETR_INT(1), ETR_INT(1), buf ^ 1, ETR_INT(0), ETR_INT(0), ETR_INT(0), [&]() { issue(buf); });
+                advance();
+                buf ^= 1;
+            }
+            settle();
+            store();
+        } while (next_tile());
+#undef ETR_INT
+    } else {
+#pragma unroll
+        for (int b = 0; b < NBUF - 1; ++b) { issue(b); advance(); }
+        int buf = 0;
+        for (;;) {
+            clear();
+            const int KT = half_tiles(t) * two;
+            for (int kt = 0; kt < KT; ++kt) {
+                wait_copies<(NBUF - 2) * (CA + CB)>();   // this wave's part of the k-tile has landed
+                barrier();                               // ... and everybody's; and everybody is done with the buffer before it
+                issue(buf == 0 ? NBUF - 1 : buf - 1);
+                advance();
+                const unsigned char* op = lds + buf * STAGE;
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) {
+                    Fragment fb[NB];
+#pragma unroll
+                    for (int jb = 0; jb < NB; ++jb) fb[jb] = fragment(op + A_BYTES, BT, BN, b_block(jb), ks);
+                    if constexpr (BF16) {
+#pragma unroll
+                        for (int i = 0; i < MB; ++i) {
+                            const Fragment fa = fragment(op, AT, BM, wm * MB + i, ks);
+#pragma unroll
+                            for (int jb = 0; jb < NB; ++jb) acc[i][jb] = multiply(fb[jb], fa, acc[i][jb]);
+                        }
+                    } else {                             // four MFMAs to a pair of fragments: not one behind the other
+                        Fragment fa[MB];
+#pragma unroll
+                        for (int i = 0; i < MB; ++i) fa[i] = fragment(op, AT, BM, wm * MB + i, ks);
+#pragma unroll
+                        for (int v = 0; v < 4; ++v)
+#pragma unroll
+                            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                                for (int jb = 0; jb < NB; ++jb)
+                                    acc[i][jb] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[jb].f[v], fa[i].f[v], acc[i][jb], 0, 0, 0);
+                    }
+                }
+                buf = buf + 1 == NBUF ? 0 : buf + 1;
+            }
+            store();
+            if (!next_tile()) break;
+            wait_copies<0>();                            // (the stores too: the counted waits are for copies alone)
+        }
     }
     wait_copies<0>();                                    // the copies that nobody needed
 }
 
 // ---- the element-wise middle of the backward ----------------------------------------------------------------------------
 //
-// da = dy act'(a) (db = dy SiLU(a)) and the column sums of both over 128 rows of an expert, before they are rounded.  A workgroup has such
+// da = dy act'(a) (db = dy SiLU(a)) and the column sums of both over 32 rows of an expert, before they are rounded.  A workgroup has such
 // a chunk of rows and 64 pieces of columns; a wave every fourth row of it.  Bound by memory: one or two rows of pre-activations and
 // one of dy in, one or two out.
-constexpr int kChunk = 128;
+constexpr int kChunk = 32;
 struct MiddleParams {
     const piece_t* pre; const piece_t* pre_up; const piece_t* dy; piece_t* da; piece_t* db;
     float* part;            // [2 with SwiGLU][chunks][N], optional
@@ -436,32 +605,46 @@ __global__ __launch_bounds__(256) void linear_middle_kernel(MiddleParams p) {
     float sa[V], sb[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) sa[i] = sb[i] = 0.f;
-    for (int r = wave; in && r < n_rows; r += 4) {
-        const size_t at = static_cast<size_t>(first + r) * p.pieces + c;
-        float d[V], a[V], b[V];
-        R::unpack(p.dy[at], d);
-        if (p.act != ETR_ACT_NONE) R::unpack(p.pre[at], a);
-        if (glu) R::unpack(p.pre_up[at], b);
-        if (p.act == ETR_ACT_GELU) {
+    // four rows of a wave at a time, all of them requested before the first is used
+    for (int r0 = wave; in && r0 < n_rows; r0 += 16) {
+        piece_t dv[4], av[4], bv[4];
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-                a[i] = d[i] * (normal_cdf(a[i]) + a[i] * 0.39894228040143268f * __expf(-0.5f * a[i] * a[i]));
-        } else if (p.act != ETR_ACT_NONE) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float sg = sigmoid(a[i]), grad = sg * (1.0f + a[i] * (1.0f - sg));
-                const float up = glu ? b[i] : 1.0f;
-                b[i] = d[i] * a[i] * sg;
-                a[i] = d[i] * up * grad;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i) a[i] = d[i];
+        for (int u = 0; u < 4; ++u) {
+            if (r0 + 4 * u >= n_rows) continue;
+            const size_t at = static_cast<size_t>(first + r0 + 4 * u) * p.pieces + c;
+            dv[u] = p.dy[at];
+            if (p.act != ETR_ACT_NONE) av[u] = p.pre[at];
+            if (glu) bv[u] = p.pre_up[at];
         }
-        if (p.da) p.da[at] = R::pack(a);
-        if (glu && p.db) p.db[at] = R::pack(b);
 #pragma unroll
-        for (int i = 0; i < V; ++i) { sa[i] += a[i]; sb[i] += glu ? b[i] : 0.f; }
+        for (int u = 0; u < 4; ++u) {
+            if (r0 + 4 * u >= n_rows) continue;
+            const size_t at = static_cast<size_t>(first + r0 + 4 * u) * p.pieces + c;
+            float d[V], a[V], b[V];
+            R::unpack(dv[u], d);
+            if (p.act != ETR_ACT_NONE) R::unpack(av[u], a);
+            if (glu) R::unpack(bv[u], b);
+            if (p.act == ETR_ACT_GELU) {
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    a[i] = d[i] * (normal_cdf(a[i]) + a[i] * 0.39894228040143268f * __expf(-0.5f * a[i] * a[i]));
+            } else if (p.act != ETR_ACT_NONE) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float sg = sigmoid(a[i]), grad = sg * (1.0f + a[i] * (1.0f - sg));
+                    const float up = glu ? b[i] : 1.0f;
+                    b[i] = d[i] * a[i] * sg;
+                    a[i] = d[i] * up * grad;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i) a[i] = d[i];
+            }
+            if (p.da) p.da[at] = R::pack(a);
+            if (glu && p.db) p.db[at] = R::pack(b);
+#pragma unroll
+            for (int i = 0; i < V; ++i) { sa[i] += a[i]; sb[i] += glu ? b[i] : 0.f; }
+        }
     }
     if (!p.part) return;
     if (wave > 0) {
@@ -478,9 +661,9 @@ __global__ __launch_bounds__(256) void linear_middle_kernel(MiddleParams p) {
     }
 }
 
-// dbias[e][n]: the chunks of expert e, four groups of them side by side, in a fixed order
-__global__ __launch_bounds__(256) void linear_bias_kernel(MiddleParams p, float* dbias, float* dbias_up) {
-    __shared__ float sums[4][64];
+// dbias[e][n]: the chunks of expert e, sixteen groups of them side by side, in a fixed order
+__global__ __launch_bounds__(1024) void linear_bias_kernel(MiddleParams p, float* dbias, float* dbias_up) {
+    __shared__ float sums[16][64];
     LinearParams q{};
     q.offsets = p.offsets; q.rows = p.rows; q.E = p.E;
     Groups g;
@@ -491,11 +674,15 @@ __global__ __launch_bounds__(256) void linear_bias_kernel(MiddleParams p, float*
     float s = 0.f;
     if (n < p.N) {
 #pragma unroll 4
-        for (int i = wave; i < tiles; i += 4) s += part[static_cast<size_t>(begin + i) * p.N + n];
+        for (int i = wave; i < tiles; i += 16) s += part[static_cast<size_t>(begin + i) * p.N + n];
     }
     sums[wave][lane] = s;
     __syncthreads();
-    if (wave == 0 && n < p.N) (blockIdx.z ? dbias_up : dbias)[static_cast<size_t>(e) * p.N + n] = ((sums[0][lane] + sums[1][lane]) + sums[2][lane]) + sums[3][lane];
+    if (wave > 0 || n >= p.N) return;
+    s = 0.f;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) s += sums[w][lane];
+    (blockIdx.z ? dbias_up : dbias)[static_cast<size_t>(e) * p.N + n] = s;
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
@@ -583,7 +770,7 @@ hipError_t launch_expert_linear_backward(const etr_linear_config& c, const void*
         if ((err = hipGetLastError()) != hipSuccess) return err;
     }
     if (dbias) {
-        hipLaunchKernelGGL(linear_bias_kernel, dim3((c.N + 63) / 64, c.E, glu ? 2 : 1), dim3(256), 0, st, m, dbias, dbias_up);
+        hipLaunchKernelGGL(linear_bias_kernel, dim3((c.N + 63) / 64, c.E, glu ? 2 : 1), dim3(1024), 0, st, m, dbias, dbias_up);
         if ((err = hipGetLastError()) != hipSuccess) return err;
     }
     LinearParams p{};
