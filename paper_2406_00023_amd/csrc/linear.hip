@@ -46,6 +46,8 @@ __device__ __forceinline__ void copy_piece(uint64_t base, uint32_t off, void* ds
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)dst, 16, static_cast<int>(off), 0, 0, 0);
 }
 
+constexpr int kPatch = 4096;                             // LDS of a wave's epilogue (large tiles)
+
 // s_waitcnt: at most n vector memory operations outstanding, the others as they are
 template <int N> __device__ __forceinline__ void wait_copies() { __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0F70); }
 
@@ -127,14 +129,15 @@ __device__ __forceinline__ void load4(const void* p, uint32_t at, float (&f)[4])
         f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
     }
 }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {           // round to nearest even (v_cvt_pk_bf16_f32)
+    typedef __attribute__((ext_vector_type(2))) float f32x2;
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
+}
 template <bool BF16>
 __device__ __forceinline__ void store4(void* p, uint32_t at, const float (&f)[4]) {
     if constexpr (BF16) {
-        typedef __attribute__((ext_vector_type(2))) float f32x2;
-        typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-        const uint2 v = make_uint2(__builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{f[0], f[1]}, bf16x2)),
-                                   __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{f[2], f[3]}, bf16x2)));
-        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + at) = v;
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + at) = make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]));
     } else {
         *reinterpret_cast<float4*>(static_cast<float*>(p) + at) = make_float4(f[0], f[1], f[2], f[3]);
     }
@@ -143,10 +146,15 @@ __device__ __forceinline__ void store4(void* p, uint32_t at, const float (&f)[4]
 // acc[i][j]: 16 x 16 block i of the wave's rows, j of its columns; a lane has row l16 of a block and four columns from 4 kq on.
 // GLU: blocks j < NB / 2 are gate columns, the others the up columns of the same outputs.  What is optional goes over the
 // accumulators in a pass of its own, so that a call pays for what it asks for and the code stays small.
-template <bool BF16, int MODE, bool GLU, int MB, int NB>
-__device__ __forceinline__ void store_tile(const LinearParams& p, const Tile& t, f32x4 (&acc)[MB][NB], int m_wave, int n_wave) {
+// patch: 4 KiB of LDS of this wave's own, through which bf16 values leave as whole 16-byte pieces, 8 (GLU: 4) of a row beside each
+// other, or null: 8 bytes a lane as they lie.
+template <bool BF16, int MODE, bool GLU, int MB, int NB, bool PATCH>
+__device__ __forceinline__ void store_tile(const LinearParams& p, const Tile& t, f32x4 (&acc)[MB][NB], int m_wave, int n_wave, unsigned char* patch) {
     constexpr int NO = GLU ? NB / 2 : NB;
-    const int lane = threadIdx.x & 63, l16 = lane & 15, kq = lane >> 4;
+    static_assert(!PATCH || (BF16 && MB % 2 == 0), "");
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));                       // (what depends on it is not worth registers of the loop over k-tiles)
+    const int l16 = lane & 15, kq = lane >> 4;
     const int limit = (MODE == WEIGHT ? p.M : t.count) - t.m0, n_first = t.n0 + n_wave + 4 * kq;
     // uniform start of the tile, 32-bit offsets in it (one register, made anew in each pass: the passes' common addresses kept across them
     // would not fit)
@@ -165,6 +173,39 @@ __device__ __forceinline__ void store_tile(const LinearParams& p, const Tile& t,
     };
     auto put = [&](void* to, auto&& of) {
         char* base = static_cast<char*>(to) + tile * (BF16 ? 2 : 4);
+        if constexpr (PATCH) {
+            constexpr int PR = 2 * NO, RP = 64 / PR;     // pieces of a row of the wave's columns; rows that 64 lanes have a piece each of
+            const int row_in = lane / PR, piece = lane % PR, n = t.n0 + n_wave + piece * 8;
+            const bool full = m_wave + MB * 16 <= limit && t.n0 + n_wave + NO * 16 <= p.N;      // (uniform)
+#pragma unroll
+            for (int ib = 0; ib < MB / 2; ++ib) {
+#pragma unroll
+                for (int bi = 0; bi < 2; ++bi)
+#pragma unroll
+                    for (int j = 0; j < NO; ++j) {
+                        const f32x4& v = of(2 * ib + bi, j);
+                        const int row = bi * 16 + l16;
+                        typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+                        *reinterpret_cast<u32x2*>(patch + row * PR * 16 + (((2 * j + (kq >> 1)) ^ (row & (PR - 1))) * 16) + (kq & 1) * 8) =
+                            u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+                    }
+                wave_sync();
+                piece_t out[32 / RP];
+#pragma unroll
+                for (int u = 0; u < 32 / RP; ++u) {
+                    const int row = u * RP + row_in;
+                    out[u] = *reinterpret_cast<const piece_t*>(patch + row * PR * 16 + ((piece ^ (row & (PR - 1))) * 16));
+                }
+                wave_sync();
+#pragma unroll
+                for (int u = 0; u < 32 / RP; ++u) {
+                    const int m = m_wave + ib * 32 + u * RP + row_in;
+                    if (full || (m < limit && n < p.N)) *reinterpret_cast<piece_t*>(base + (static_cast<uint32_t>(m) * p.N + n) * 2u) = out[u];
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            return;
+        }
         each([&](int i, int j, uint32_t at) {
             const f32x4& v = of(i, j);
             const float f[4] = {v[0], v[1], v[2], v[3]};
@@ -208,14 +249,25 @@ __device__ __forceinline__ void store_tile(const LinearParams& p, const Tile& t,
                 for (int j = 0; j < NO; ++j) asm volatile("" : "+v"(acc[i][j]));
             if (p.act == ETR_ACT_GELU) map([](float a, float) { return a * normal_cdf(a); });
         }
-        if (p.residual) {
+        if (p.residual) {                                // two rows of blocks at a time; past the ends the last row or columns again, not stored
             const char* base = static_cast<const char*>(p.residual) + tile * (BF16 ? 2 : 4);
-            each([&](int i, int j, uint32_t at) {
-                float r[4];
-                load4<BF16>(base, at, r);
+            constexpr int U = MB >= 2 ? 2 : 1;
 #pragma unroll
-                for (int v = 0; v < 4; ++v) acc[i][j][v] += r[v];
-            });
+            for (int ib = 0; ib < MB; ib += U) {
+                float r[U][NO][4];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int j = 0; j < NO; ++j)
+                        load4<BF16>(base, static_cast<uint32_t>(min(m_wave + (ib + u) * 16 + l16, limit - 1)) * p.N + min(n_first + j * 16, p.N - 4), r[u][j]);
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int j = 0; j < NO; ++j)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) acc[ib + u][j][v] += r[u][j][v];
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
     }
     put(p.C[MODE == WEIGHT ? t.half : 0], [&](int i, int j) -> const f32x4& { return acc[i][j]; });
@@ -363,7 +415,10 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
 #pragma unroll
             for (int jb = 0; jb < NB; ++jb) acc[i][jb] = f32x4{0.f, 0.f, 0.f, 0.f};
     };
-    auto store = [&]() { store_tile<BF16, MODE, GLU, MB, NB>(p, t, acc, wm * MB * 16, GLU ? wn * (NB / 2) * 16 : wn * NB * 16); };
+    constexpr bool DEEP = BF16 && MB == 8 && NB == 4 && NBUF == 2;
+    auto store = [&]() {
+        store_tile<BF16, MODE, GLU, MB, NB, DEEP>(p, t, acc, wm * MB * 16, GLU ? wn * (NB / 2) * 16 : wn * NB * 16, lds + NBUF * STAGE + wave * kPatch);
+    };
     auto next_tile = [&]() {
         j += gridDim.x >> 3;
         int unused;
@@ -375,7 +430,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
         asm volatile("" ::: "memory");
     };
     aim(t);
-    if constexpr (BF16 && MB == 8 && NB == 4 && NBUF == 2) {
+    if constexpr (DEEP) {
         // 128 rows x 64 columns to a wave, one workgroup to a CU: nothing else covers a wait, so the loop is written out.  A k-tile is four
         // substeps of 16 MFMAs: k-step 0 and 1 of row blocks 0 - 3 and 4 - 7.  Fragments are read a substep ahead; the barrier stands
         // before the last substep, when all reads of the buffer are done: behind it go the next k-tile's first reads (that it has landed is
@@ -696,7 +751,8 @@ long long tiles_at_most(const LinearParams& p, int mode, int BM, int out_n) {
 
 template <bool BF16, int BM, int BN, int WM, int WN, int NBUF, int MODE, bool GLU>
 hipError_t launch_tiles(LinearParams p, hipStream_t st) {
-    constexpr size_t lds = static_cast<size_t>(BM + BN) * 128 * NBUF;
+    constexpr bool large = BM * BN >= 256 * 256;
+    constexpr size_t lds = static_cast<size_t>(BM + BN) * 128 * NBUF + (large ? WM * WN * kPatch : 0);
     auto kern = linear_kernel<BF16, BM, BN, WM, WN, NBUF, MODE, GLU>;
     const hipError_t err = ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds);
     if (err != hipSuccess) return err;
@@ -704,7 +760,7 @@ hipError_t launch_tiles(LinearParams p, hipStream_t st) {
     const long long tiles = tiles_at_most(p, MODE, BM, GLU ? BN / 2 : BN);
     if (tiles > (1ll << 30)) return hipErrorInvalidValue;
     // one workgroup on each CU that walks the tiles, or (small tiles) one for each of them
-    const long long most = BM * BN >= 256 * 256 ? cu_count() / 8 : 1 << 17;
+    const long long most = large ? cu_count() / 8 : 1 << 17;
     const long long blocks = std::min((tiles + 7) / 8, most) * 8;
     hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(blocks)), dim3(WM * WN * 64), lds, st, p);
     return hipGetLastError();
