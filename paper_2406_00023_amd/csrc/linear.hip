@@ -215,16 +215,15 @@ __device__ __forceinline__ void store_tile(const LinearParams& p, const Tile& t,
     if constexpr (MODE == FORWARD) {
 #pragma unroll
         for (int h = 0; h < (GLU ? 2 : 1); ++h) {
-            if (p.bias[h]) {
+            // (added without a branch, zeros where there is none: around one, the accumulators of both ways would be kept)
 #pragma unroll
-                for (int j = 0; j < NO; ++j) {
-                    float b[4] = {0.f, 0.f, 0.f, 0.f};
-                    if (n_first + j * 16 < p.N) load4<false>(p.bias[h] + static_cast<size_t>(t.e) * p.N, n_first + j * 16, b);
+            for (int j = 0; j < NO; ++j) {
+                float b[4] = {0.f, 0.f, 0.f, 0.f};
+                if (p.bias[h] && n_first + j * 16 < p.N) load4<false>(p.bias[h] + static_cast<size_t>(t.e) * p.N, n_first + j * 16, b);
 #pragma unroll
-                    for (int i = 0; i < MB; ++i)
+                for (int i = 0; i < MB; ++i)
 #pragma unroll
-                        for (int v = 0; v < 4; ++v) acc[i][h * NO + j][v] += b[v];
-                }
+                    for (int v = 0; v < 4; ++v) acc[i][h * NO + j][v] += b[v];
             }
             if (p.pre[h]) put(p.pre[h], [&](int i, int j) -> const f32x4& { return acc[i][h * NO + j]; });
         }
@@ -435,147 +434,163 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
         // substeps of 16 MFMAs: k-step 0 and 1 of row blocks 0 - 3 and 4 - 7.  Fragments are read a substep ahead; the barrier stands
         // before the last substep, when all reads of the buffer are done: behind it go the next k-tile's first reads (that it has landed is
         // what was waited for), and the copies of the one after that into the buffer just left.
-        // Transposing reads are assembly: through the builtin each of them waits for all copies on their way, because it is taken to alias
-        // what they write.  A statement holds 8 MFMAs (two row blocks, four column blocks), behind the first of them the reads of up to
-        // four fragments, and its own wait at the end, so that they land under the other MFMAs and its outputs are ordinary registers.  What the
-        // compiler cannot see in it: two wait states between an ordinary write of an operand and the MFMA (the s_nop in front), and
-        // that an accumulator is not to be touched right behind (settle, before the epilogue).
-        Fragment fa[2][4], fb[2][4];
-        const int tr_q = l16 & 3, tr_j = l16 >> 2, tr_f = ((tr_j >> 1) & 1) | ((kq & 1) << 1);
-        uint32_t tr[4];                                  // this lane's place of the four 16-column blocks of a group
+        // MFMAs and the fragment reads beside them are assembly: a transposing read through the builtin waits for all copies on their way,
+        // because it is taken to alias what they write.  A statement holds 8 MFMAs (two row blocks, four column blocks), behind the first of
+        // them the reads of up to four fragments, and its own wait at the end, so that they land under the other MFMAs and its outputs are
+        // ordinary registers.  What the compiler cannot see in it: two wait states between an ordinary write of an operand and the
+        // MFMA (the s_nop in front), and that an accumulator is not to be touched right behind (settle, before the epilogue).
+        bf16x8 fa[2][4], fb[2][4];
+        // LDS addresses (buffer 0) of this lane's part of a fragment; columns: of the four 16-column blocks of the wave's first group, + 512: the
+        // k four further on, + 4096: the second k-step, + 8192: the next group; rows: of the two k-steps of the wave's first block, + 2048:
+        // the next block
+        const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr)lds));
+        uint32_t at_a[4], at_b[4];
+        {
+            const int q = l16 & 3, jj = l16 >> 2, f = ((jj >> 1) & 1) | ((kq & 1) << 1);
 #pragma unroll
-        for (int o = 0; o < 4; ++o)
-            tr[o] = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr)lds)) + (8 * kq + tr_j) * 128 + ((o ^ tr_f) * 32) + tr_q * 8;
-        const uint32_t tr_a = wm * 16384, tr_b = A_BYTES + wn * 8192;
-        auto read_a = [&](int b, int ks, int h, int i) { fa[h][i] = fragment(lds + b * STAGE, false, BM, wm * MB + 4 * h + i, ks); };
-        auto read_b = [&](int b, int ks, int i) { fb[ks][i] = fragment(lds + b * STAGE + A_BYTES, false, BN, b_block(i), ks); };
+            for (int o = 0; o < 4; ++o) {
+                const uint32_t columns = (8 * kq + jj) * 128 + ((o ^ f) * 32) + q * 8;
+                const uint32_t rows = l16 * 128 + ((4 * (o & 1) + kq) ^ ((l16 >> 1) & 7)) * 16;
+                at_a[o] = lds0 + (AT ? wm * 16384 + columns : wm * 16384 + rows);
+                at_b[o] = lds0 + A_BYTES + (BT ? wn * 8192 + columns : wn * (GLU ? 4096 : 8192) + rows);
+            }
+        }
 #define ETR_MF(C, B, A) "v_mfma_f32_16x16x32_bf16 %[c" #C "], %[b" #B "], %[a" #A "], %[c" #C "]\n\t"
 #define ETR_REST ETR_MF(1, 0, 1) ETR_MF(3, 1, 1) ETR_MF(2, 1, 0) ETR_MF(4, 2, 0) ETR_MF(5, 2, 1) ETR_MF(7, 3, 1) ETR_MF(6, 3, 0)
 #define ETR_TR(N) "ds_read_b64_tr_b16 %[x" #N "], %[p" #N "] offset:%c[o" #N "]\n\tds_read_b64_tr_b16 %[y" #N "], %[p" #N "] offset:%c[q" #N "]\n\t"
+#define ETR_RD(N) "ds_read_b128 %[r" #N "], %[p" #N "] offset:%c[o" #N "]\n\t"
 #define ETR_ACC [c0] "+v"(acc[I][0]), [c1] "+v"(acc[I + 1][0]), [c2] "+v"(acc[I][1]), [c3] "+v"(acc[I + 1][1]), [c4] "+v"(acc[I][2]), \
                 [c5] "+v"(acc[I + 1][2]), [c6] "+v"(acc[I][3]), [c7] "+v"(acc[I + 1][3])
 #define ETR_FRAGMENTS [a0] "v"(a[0]), [a1] "v"(a[1]), [b0] "v"(b[0]), [b1] "v"(b[1]), [b2] "v"(b[2]), [b3] "v"(b[3])
 #define ETR_OUT(N) [x##N] "=&v"(x[N]), [y##N] "=&v"(y[N])
-#define ETR_AT(N) [p##N] "v"(at + tr[F + N]), [o##N] "n"(OFF), [q##N] "n"(OFF + 512)
-        // acc[I], acc[I + 1] += a0[0..1] x b0[0..3]; R fragments from block F of the group at `at` + OFF on into `out`
-        auto mfma8 = [&](auto reads, auto block, const Fragment* a0, const Fragment* b0, Fragment* out, uint32_t at, auto from, auto offset) {
-            constexpr int R = decltype(reads)::value, I = decltype(block)::value, F = decltype(from)::value, OFF = decltype(offset)::value;
-            typedef int v2i __attribute__((ext_vector_type(2)));
-            bf16x8 a[2], b[4];
+#define ETR_ROW(N) [r##N] "=&v"(out[N])
+#define ETR_AT(N) [p##N] "v"(COLUMNS ? at[(F + N) & 3] + slot : at[KS] + slot), [o##N] "n"(offset(N)), [q##N] "n"(offset(N) + 512)
+        typedef int v2i __attribute__((ext_vector_type(2)));
+        auto join = [](v2i lo, v2i hi) -> bf16x8 {
+            typedef int v4i __attribute__((ext_vector_type(4)));
+            return __builtin_bit_cast(bf16x8, v4i{lo[0], lo[1], hi[0], hi[1]});
+        };
+        // acc[I], acc[I + 1] += a[0..1] x b[0..3] (I < 0: no products); R fragments of k-step KS from block F of half H of an operand (its
+        // kind, its addresses and whether it is B) on into `out`
+        auto step8 = [&](auto block, const bf16x8* a, const bf16x8* b, auto reads, auto columns_, auto is_b, const uint32_t* at, uint32_t slot, auto ks_, auto half,
+                         auto from, bf16x8* out) {
+            constexpr int I = decltype(block)::value < 0 ? 0 : decltype(block)::value, R = decltype(reads)::value, KS = decltype(ks_)::value,
+                          H = decltype(half)::value, F = decltype(from)::value;
+            constexpr bool NONE = decltype(block)::value < 0, COLUMNS = decltype(columns_)::value, OF_B = decltype(is_b)::value;
+            auto offset = [](int n) constexpr {
+                if (COLUMNS) return KS * 4096 + H * 8192;
+                if (OF_B && GLU) return ((F + n) >> 1) * 16384 + ((F + n) & 1) * 2048;       // the up rows lie 128 rows behind the gate rows
+                return (4 * H + F + n) * 2048;
+            };
             v2i x[4], y[4];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) a[i] = __builtin_bit_cast(bf16x8, a0[i]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) b[i] = __builtin_bit_cast(bf16x8, b0[i]);
-            if constexpr (R == 0)
-                asm volatile("s_nop 1\n\t" ETR_MF(0, 0, 0) ETR_REST : ETR_ACC : ETR_FRAGMENTS);
-            else if constexpr (R == 2)
+            if constexpr (NONE && COLUMNS)
+                asm volatile(ETR_TR(0) ETR_TR(1) ETR_TR(2) ETR_TR(3) "s_waitcnt lgkmcnt(0)"
+                             : ETR_OUT(0), ETR_OUT(1), ETR_OUT(2), ETR_OUT(3) : ETR_AT(0), ETR_AT(1), ETR_AT(2), ETR_AT(3) : "memory");
+            else if constexpr (NONE)
+                asm volatile(ETR_RD(0) ETR_RD(1) ETR_RD(2) ETR_RD(3) "s_waitcnt lgkmcnt(0)"
+                             : ETR_ROW(0), ETR_ROW(1), ETR_ROW(2), ETR_ROW(3) : ETR_AT(0), ETR_AT(1), ETR_AT(2), ETR_AT(3) : "memory");
+            else if constexpr (R == 2 && COLUMNS)
                 asm volatile("s_nop 1\n\t" ETR_MF(0, 0, 0) ETR_TR(0) ETR_TR(1) ETR_REST "s_waitcnt lgkmcnt(0)"
                              : ETR_ACC, ETR_OUT(0), ETR_OUT(1) : ETR_FRAGMENTS, ETR_AT(0), ETR_AT(1) : "memory");
-            else
+            else if constexpr (R == 2)
+                asm volatile("s_nop 1\n\t" ETR_MF(0, 0, 0) ETR_RD(0) ETR_RD(1) ETR_REST "s_waitcnt lgkmcnt(0)"
+                             : ETR_ACC, ETR_ROW(0), ETR_ROW(1) : ETR_FRAGMENTS, ETR_AT(0), ETR_AT(1) : "memory");
+            else if constexpr (COLUMNS)
                 asm volatile("s_nop 1\n\t" ETR_MF(0, 0, 0) ETR_TR(0) ETR_TR(1) ETR_TR(2) ETR_TR(3) ETR_REST "s_waitcnt lgkmcnt(0)"
                              : ETR_ACC, ETR_OUT(0), ETR_OUT(1), ETR_OUT(2), ETR_OUT(3)
                              : ETR_FRAGMENTS, ETR_AT(0), ETR_AT(1), ETR_AT(2), ETR_AT(3) : "memory");
-            typedef float v2f __attribute__((ext_vector_type(2)));
+            else
+                asm volatile("s_nop 1\n\t" ETR_MF(0, 0, 0) ETR_RD(0) ETR_RD(1) ETR_RD(2) ETR_RD(3) ETR_REST "s_waitcnt lgkmcnt(0)"
+                             : ETR_ACC, ETR_ROW(0), ETR_ROW(1), ETR_ROW(2), ETR_ROW(3)
+                             : ETR_FRAGMENTS, ETR_AT(0), ETR_AT(1), ETR_AT(2), ETR_AT(3) : "memory");
+            if constexpr (COLUMNS) {
 #pragma unroll
-            for (int i = 0; i < R; ++i) {
-                const v2f l = __builtin_bit_cast(v2f, x[i]), h = __builtin_bit_cast(v2f, y[i]);
-                out[i].f[0] = l[0]; out[i].f[1] = l[1]; out[i].f[2] = h[0]; out[i].f[3] = h[1];
+                for (int i = 0; i < (NONE ? 4 : R); ++i) out[i] = join(x[i], y[i]);
             }
         };
 #undef ETR_MF
 #undef ETR_REST
 #undef ETR_TR
+#undef ETR_RD
 #undef ETR_ACC
 #undef ETR_FRAGMENTS
 #undef ETR_OUT
+#undef ETR_ROW
 #undef ETR_AT
 #define ETR_INT(V) std::integral_constant<int, (V)>{}
-        // Substep (ks, h); then the next fragments: of A (NH, NKS) and, with NB_KS >= 0, of B, from buffer b.
-        auto substep = [&](auto ks_, auto h_, int b, auto nh_, auto nks_, auto nbks_, auto&& behind) {
+        // 64-row halves of this wave's 128 that have a row to store at all, none if its columns lie past the last: tiles at the end of an
+        // expert's rows multiply what they have, and the wave beside them on the SIMD has the matrix pipe for itself meanwhile
+        int live = 2;
+        auto count_live = [&]() {
+            const int rows_left = (MODE == WEIGHT ? p.M : t.count) - t.m0 - wm * 128;
+            live = t.n0 + (GLU ? wn * 32 : wn * 64) < p.N ? min(max((rows_left + 63) >> 6, 0), 2) : 0;
+        };
+        // Substep (ks, h); then the next fragments: of A (half nh, k-step nks) and, with nbks >= 0, of B, from buffer b.
+        auto substep = [&](auto live_, auto ks_, auto h_, int b, auto nh_, auto nks_, auto nbks_, auto&& behind) {
             constexpr int ks = decltype(ks_)::value, h = decltype(h_)::value, nh = decltype(nh_)::value, nks = decltype(nks_)::value,
-                          nbks = decltype(nbks_)::value;
+                          nbks = decltype(nbks_)::value, first = h >= decltype(live_)::value ? -1 : 4 * h, second = first < 0 ? -1 : first + 2;
             const uint32_t slot = static_cast<uint32_t>(b) * STAGE;
-            if constexpr (!BT) {
-#pragma unroll
-                for (int m = 0; m < 16; ++m) {           // neighbours share an operand, back and forth over the row blocks
-                    const int jb = m >> 2, i = jb & 1 ? 3 - (m & 3) : m & 3;
-                    acc[4 * h + i][jb] = multiply(fb[ks][jb], fa[h][i], acc[4 * h + i][jb]);
-                    __builtin_amdgcn_sched_barrier(0);
-                    if (m < 4) read_a(b, nks, nh, m);
-                    else if (m < 8 && nbks >= 0) read_b(b, nbks, m - 4);
-                    else if (m == 8) behind();
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            } else {
-                // first statement: the fragments of B (all four), or the first two of A; second: those of A that are left
-                if constexpr (nbks >= 0)
-                    mfma8(ETR_INT(4), ETR_INT(4 * h), fa[h], fb[ks], fb[nbks < 0 ? 0 : nbks], tr_b + slot, ETR_INT(0), ETR_INT(nbks * 4096));
-                else if constexpr (AT)
-                    mfma8(ETR_INT(2), ETR_INT(4 * h), fa[h], fb[ks], fa[nh], tr_a + slot, ETR_INT(0), ETR_INT(nks * 4096 + nh * 8192));
-                else
-                    mfma8(ETR_INT(0), ETR_INT(4 * h), fa[h], fb[ks], fa[nh], 0u, ETR_INT(0), ETR_INT(0));
-                behind();
-                __builtin_amdgcn_sched_barrier(0);
-                if constexpr (!AT) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) read_a(b, nks, nh, i);
-                    __builtin_amdgcn_sched_barrier(0);
-                    mfma8(ETR_INT(0), ETR_INT(4 * h + 2), fa[h] + 2, fb[ks], fa[nh], 0u, ETR_INT(0), ETR_INT(0));
-                } else if constexpr (nbks >= 0) {
-                    mfma8(ETR_INT(4), ETR_INT(4 * h + 2), fa[h] + 2, fb[ks], fa[nh], tr_a + slot, ETR_INT(0), ETR_INT(nks * 4096 + nh * 8192));
-                } else {
-                    mfma8(ETR_INT(2), ETR_INT(4 * h + 2), fa[h] + 2, fb[ks], fa[nh] + 2, tr_a + slot, ETR_INT(2), ETR_INT(nks * 4096 + nh * 8192));
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            // first statement: the fragments of B (all four), or the first two of A; second: those of A that are left.  Without products
+            // (nothing of these 64 rows is stored): four at a time
+            if constexpr (nbks >= 0)
+                step8(ETR_INT(first), fa[h], fb[ks], ETR_INT(4), ETR_INT(BT), ETR_INT(1), at_b, slot, ETR_INT(nbks < 0 ? 0 : nbks), ETR_INT(0), ETR_INT(0), fb[nbks < 0 ? 0 : nbks]);
+            else if constexpr (first >= 0)
+                step8(ETR_INT(first), fa[h], fb[ks], ETR_INT(2), ETR_INT(AT), ETR_INT(0), at_a, slot, ETR_INT(nks), ETR_INT(nh), ETR_INT(0), fa[nh]);
+            __builtin_amdgcn_sched_barrier(0);
+            behind();
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (nbks >= 0 || first < 0)
+                step8(ETR_INT(second), fa[h] + 2, fb[ks], ETR_INT(4), ETR_INT(AT), ETR_INT(0), at_a, slot, ETR_INT(nks), ETR_INT(nh), ETR_INT(0), fa[nh]);
+            else
+                step8(ETR_INT(second), fa[h] + 2, fb[ks], ETR_INT(2), ETR_INT(AT), ETR_INT(0), at_a, slot, ETR_INT(nks), ETR_INT(nh), ETR_INT(2), fa[nh] + 2);
+            __builtin_amdgcn_sched_barrier(0);
         };
         auto settle = [&]() {                            // nothing behind this reads an accumulator sooner than its MFMA has written it
-            if constexpr (BT) {
-                asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+            asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
 #pragma unroll
-                for (int i = 0; i < MB; ++i)
+            for (int i = 0; i < MB; ++i)
 #pragma unroll
-                    for (int jb = 0; jb < NB; ++jb) asm volatile("" : "+v"(acc[i][jb]));
-            }
-        };
-        auto read_first = [&]() {
-            typedef int v2i __attribute__((ext_vector_type(2)));
-            typedef float v2f __attribute__((ext_vector_type(2)));
-            auto columns = [&](uint32_t at) -> Fragment {
-                v2i x, y;
-                asm volatile("ds_read_b64_tr_b16 %0, %2\n\tds_read_b64_tr_b16 %1, %2 offset:512\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x), "=&v"(y) : "v"(at) : "memory");
-                const v2f l = __builtin_bit_cast(v2f, x), h = __builtin_bit_cast(v2f, y);
-                return Fragment{{l[0], l[1], h[0], h[1]}};
-            };
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (AT) fa[0][i] = columns(tr_a + tr[i]);
-                else read_a(0, 0, 0, i);
-                if constexpr (BT) fb[0][i] = columns(tr_b + tr[i]);
-                else read_b(0, 0, i);
-            }
+                for (int jb = 0; jb < NB; ++jb) asm volatile("" : "+v"(acc[i][jb]));
         };
         issue(0); advance();
         issue(1); advance();
         wait_copies<CA + CB>();
         barrier();
-        read_first();
+        step8(ETR_INT(-1), nullptr, nullptr, ETR_INT(4), ETR_INT(AT), ETR_INT(0), at_a, 0u, ETR_INT(0), ETR_INT(0), ETR_INT(0), fa[0]);
+        step8(ETR_INT(-1), nullptr, nullptr, ETR_INT(4), ETR_INT(BT), ETR_INT(1), at_b, 0u, ETR_INT(0), ETR_INT(0), ETR_INT(0), fb[0]);
         int buf = 0;
         do {
             clear();
+            count_live();
             const int KT = half_tiles(t) * two;
-            for (int kt = 0; kt < KT; ++kt) {
-                substep(ETR_INT(0), ETR_INT(0), buf, ETR_INT(1), ETR_INT(0), ETR_INT(1), [&]() {});
-                substep(ETR_INT(0), ETR_INT(1), buf, ETR_INT(0), ETR_INT(1), ETR_INT(-1), [&]() {});
-                substep(ETR_INT(1), ETR_INT(0), buf, ETR_INT(1), ETR_INT(1), ETR_INT(-1), [&]() {});
-                __builtin_amdgcn_s_waitcnt(0x0070);      // vmcnt(0), lgkmcnt(0): the next k-tile is here, this wave's reads are done
-                barrier();
-                __builtin_amdgcn_sched_barrier(0);
-                substep(ETR_INT(1), ETR_INT(1), buf ^ 1, ETR_INT(0), ETR_INT(0), ETR_INT(0), [&]() { issue(buf); });
-                advance();
-                buf ^= 1;
-            }
+            auto k_loop = [&](auto n) {
+                for (int kt = 0; kt < KT; ++kt) {
+                    substep(n, ETR_INT(0), ETR_INT(0), buf, ETR_INT(1), ETR_INT(0), ETR_INT(1), [&]() {});
+                    substep(n, ETR_INT(0), ETR_INT(1), buf, ETR_INT(0), ETR_INT(1), ETR_INT(-1), [&]() {});
+                    substep(n, ETR_INT(1), ETR_INT(0), buf, ETR_INT(1), ETR_INT(1), ETR_INT(-1), [&]() {});
+                    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0), lgkmcnt(0): the next k-tile is here, this wave's reads are done
+                    barrier();
+                    __builtin_amdgcn_sched_barrier(0);
+                    substep(n, ETR_INT(1), ETR_INT(1), buf ^ 1, ETR_INT(0), ETR_INT(0), ETR_INT(0), [&]() { issue(buf); });
+                    advance();
+                    buf ^= 1;
+                }
+            };
+            // (the empty statements: what the three ways leave behind is one set of registers, not merged by copies)
+            auto pin = [&]() {
+#pragma unroll
+                for (int i = 0; i < MB; ++i)
+#pragma unroll
+                    for (int jb = 0; jb < NB; ++jb) asm volatile("" : "+v"(acc[i][jb]));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(fa[0][i]), "+v"(fb[0][i]));
+            };
+            if (live == 2) k_loop(ETR_INT(2));
+            pin();
+            if (live == 1) k_loop(ETR_INT(1));
+            pin();
+            if (live == 0) k_loop(ETR_INT(0));
+            pin();
             settle();
             store();
         } while (next_tile());
