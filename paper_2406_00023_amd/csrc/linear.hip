@@ -67,12 +67,15 @@ struct Groups {
     }
 };
 
-struct Tile { int e, first, m0, n0, count, half; };      // half: WEIGHT with SwiGLU, which of the two outputs
+// count: rows of the group; limit: the tile stores rows below it; half: WEIGHT with SwiGLU, which of the two outputs
+struct Tile { int e, first, m0, n0, count, limit, half; };
 
 // The tile list: groups one after the other; inside a group bands of 8 row tiles, in a band the row tiles of a column tile next to
 // each other.  Each XCD (workgroups go round them) has an equal contiguous part of the list, so its 32 CUs work on some 8 x 4 tiles at
 // once and share 8 + 4 operand slabs in its L2.
-template <int MODE>
+// SPLIT (large tiles, one workgroup to a CU): where the last round over an XCD's CUs would keep half of them or fewer busy, its tiles go in
+// halves or quarters of their rows to as many workgroups.
+template <int MODE, bool SPLIT>
 __device__ __forceinline__ bool find_tile(const LinearParams& p, const Groups& g, int BM, int BN, int j, int& share, Tile& t) {
     int total, MTw = 0;
     if (MODE == WEIGHT) {
@@ -82,6 +85,15 @@ __device__ __forceinline__ bool find_tile(const LinearParams& p, const Groups& g
         total = __builtin_amdgcn_readlane(g.tiles_incl, 63) * p.NT;
     }
     share = (total + 7) >> 3;
+    int part = 0, parts_log = 0;
+    if constexpr (SPLIT) {
+        const int W = gridDim.x >> 3, full = share / W * W, rest = share - full;
+        if (j >= full) {
+            parts_log = rest * 4 <= W ? 2 : rest * 2 <= W ? 1 : 0;
+            part = (j - full) & ((1 << parts_log) - 1);
+            j = full + ((j - full) >> parts_log);
+        }
+    }
     const int q = (blockIdx.x & 7) * share + j;
     if (j >= share || q >= total) return false;
     int in, rows;
@@ -101,6 +113,12 @@ __device__ __forceinline__ bool find_tile(const LinearParams& p, const Groups& g
     t.half = MODE == WEIGHT && mt >= MTw ? 1 : 0;
     t.m0 = (mt - t.half * MTw) * BM;
     t.n0 = nt * BN;
+    t.limit = MODE == WEIGHT ? p.M : t.count;
+    if (SPLIT && parts_log) {                            // (a part past the last row stores nothing: it stays at the tile's start)
+        const int height = BM >> parts_log, m0 = t.m0 + part * height;
+        t.limit = m0 < t.limit ? min(t.limit, m0 + height) : t.m0;
+        t.m0 = t.limit > t.m0 ? m0 : t.m0;
+    }
     return true;
 }
 
@@ -155,7 +173,7 @@ __device__ __forceinline__ void store_tile(const LinearParams& p, const Tile& t,
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));                       // (what depends on it is not worth registers of the loop over k-tiles)
     const int l16 = lane & 15, kq = lane >> 4;
-    const int limit = (MODE == WEIGHT ? p.M : t.count) - t.m0, n_first = t.n0 + n_wave + 4 * kq;
+    const int limit = t.limit - t.m0, n_first = t.n0 + n_wave + 4 * kq;
     // uniform start of the tile, 32-bit offsets in it (one register, made anew in each pass: the passes' common addresses kept across them
     // would not fit)
     const size_t tile = ((MODE == WEIGHT ? static_cast<size_t>(t.e) * p.M : static_cast<size_t>(t.first)) + t.m0) * p.N;
@@ -258,7 +276,7 @@ __device__ __forceinline__ void store_tile(const LinearParams& p, const Tile& t,
                 for (int u = 0; u < U; ++u)
 #pragma unroll
                     for (int j = 0; j < NO; ++j)
-                        load4<BF16>(base, static_cast<uint32_t>(min(m_wave + (ib + u) * 16 + l16, limit - 1)) * p.N + min(n_first + j * 16, p.N - 4), r[u][j]);
+                        load4<BF16>(base, static_cast<uint32_t>(max(min(m_wave + (ib + u) * 16 + l16, limit - 1), 0)) * p.N + min(n_first + j * 16, p.N - 4), r[u][j]);
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -290,6 +308,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
     constexpr int CA = BM / 8 / NW, CB = BN / 8 / NW;    // copies of 64 pieces per wave, operand and k-tile
     static_assert(CA * NW * 8 == BM && CB * NW * 8 == BN, "whole copies for every wave");
     static_assert((!AT || BM % 64 == 0) && (!BT || BN % 64 == 0), "columns come in groups of 64");
+    constexpr bool DEEP = BF16 && MB == 8 && NB == 4 && NBUF == 2;       // one workgroup to a CU, which walks the tiles
     constexpr int A_BYTES = BM * 128, STAGE = (BM + BN) * 128, OUT_N = GLU ? BN / 2 : BN;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int lane = threadIdx.x & 63, l16 = lane & 15, kq = lane >> 4;
@@ -300,7 +319,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
     int share;
     Tile t;
     int j = blockIdx.x >> 3;
-    if (!find_tile<MODE>(p, groups, BM, OUT_N, j, share, t)) return;
+    if (!find_tile<MODE, DEEP>(p, groups, BM, OUT_N, j, share, t)) return;
 
     // k-tiles of a tile, of each half of a contraction in two halves (INPUT of SwiGLU)
     const int two = MODE == INPUT && p.glu ? 2 : 1;
@@ -371,7 +390,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
         jn += gridDim.x >> 3;
         Tile n;
         int unused;
-        if (find_tile<MODE>(p, groups, BM, OUT_N, jn, unused, n)) aim(n);
+        if (find_tile<MODE, DEEP>(p, groups, BM, OUT_N, jn, unused, n)) aim(n);
         else more = false;
     };
 
@@ -414,14 +433,13 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
 #pragma unroll
             for (int jb = 0; jb < NB; ++jb) acc[i][jb] = f32x4{0.f, 0.f, 0.f, 0.f};
     };
-    constexpr bool DEEP = BF16 && MB == 8 && NB == 4 && NBUF == 2;
     auto store = [&]() {
         store_tile<BF16, MODE, GLU, MB, NB, DEEP>(p, t, acc, wm * MB * 16, GLU ? wn * (NB / 2) * 16 : wn * NB * 16, lds + NBUF * STAGE + wave * kPatch);
     };
     auto next_tile = [&]() {
         j += gridDim.x >> 3;
         int unused;
-        return find_tile<MODE>(p, groups, BM, OUT_N, j, unused, t);
+        return find_tile<MODE, DEEP>(p, groups, BM, OUT_N, j, unused, t);
     };
     auto barrier = [&]() {
         asm volatile("" ::: "memory");
@@ -522,7 +540,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
         // expert's rows multiply what they have, and the wave beside them on the SIMD has the matrix pipe for itself meanwhile
         int live = 2;
         auto count_live = [&]() {
-            const int rows_left = (MODE == WEIGHT ? p.M : t.count) - t.m0 - wm * 128;
+            const int rows_left = t.limit - t.m0 - wm * 128;
             live = t.n0 + (GLU ? wn * 32 : wn * 64) < p.N ? min(max((rows_left + 63) >> 6, 0), 2) : 0;
         };
         // Substep (ks, h); then the next fragments: of A (half nh, k-step nks) and, with nbks >= 0, of B, from buffer b.
@@ -775,8 +793,8 @@ hipError_t launch_tiles(LinearParams p, hipStream_t st) {
     const long long tiles = tiles_at_most(p, MODE, BM, GLU ? BN / 2 : BN);
     if (tiles > (1ll << 30)) return hipErrorInvalidValue;
     // one workgroup on each CU that walks the tiles, or (small tiles) one for each of them
-    const long long most = large ? cu_count() / 8 : 1 << 17;
-    const long long blocks = std::min((tiles + 7) / 8, most) * 8;
+    const long long most = large ? cu_count() / 8 : 1 << 17, wanted = (tiles + 7) / 8 * (large ? 4 : 1);      // (up to four parts of a tile)
+    const long long blocks = std::min(wanted, most) * 8;
     hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(blocks)), dim3(WM * WN * 64), lds, st, p);
     return hipGetLastError();
 }
