@@ -16,7 +16,6 @@ namespace {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((address_space(3))) void* lds_ptr;
 
 enum Product { FORWARD = 0, INPUT = 1, WEIGHT = 2 };     // y, dx, dw
@@ -76,7 +75,7 @@ struct Tile { int e, first, m0, n0, count, limit, half; };
 // SPLIT (large tiles, one workgroup to a CU): where the last round over an XCD's CUs would keep half of them or fewer busy, its tiles go in
 // halves or quarters of their rows to as many workgroups.
 template <int MODE, bool SPLIT>
-__device__ __forceinline__ bool find_tile(const LinearParams& p, const Groups& g, int BM, int BN, int j, int& share, Tile& t) {
+__device__ __forceinline__ bool find_tile(const LinearParams& p, const Groups& g, int BM, int BN, int bid, int grid, int j, Tile& t) {
     int total, MTw = 0;
     if (MODE == WEIGHT) {
         MTw = (p.M + BM - 1) / BM;
@@ -84,17 +83,17 @@ __device__ __forceinline__ bool find_tile(const LinearParams& p, const Groups& g
     } else {
         total = __builtin_amdgcn_readlane(g.tiles_incl, 63) * p.NT;
     }
-    share = (total + 7) >> 3;
+    const int share = (total + 7) >> 3;
     int part = 0, parts_log = 0;
     if constexpr (SPLIT) {
-        const int W = gridDim.x >> 3, full = share / W * W, rest = share - full;
+        const int W = grid >> 3, full = share / W * W, rest = share - full;
         if (j >= full) {
             parts_log = rest * 4 <= W ? 2 : rest * 2 <= W ? 1 : 0;
             part = (j - full) & ((1 << parts_log) - 1);
             j = full + ((j - full) >> parts_log);
         }
     }
-    const int q = (blockIdx.x & 7) * share + j;
+    const int q = (bid & 7) * share + j;
     if (j >= share || q >= total) return false;
     int in, rows;
     if (MODE == WEIGHT) {
@@ -299,31 +298,38 @@ __device__ __forceinline__ void store_tile(const LinearParams& p, const Tile& t,
 //                 k and twice bit 3, for the transposing reads; fp32: [k][columns], the piece at place s of a k row is s ^ 4 (k / 4 % 4)
 // A workgroup of WM x WN waves has a BM x BN tile at a time; NBUF buffers, of which all but one are on their way.
 // The MFMAs take the columns' fragment first, so that a lane ends up with four neighbouring columns of one row.
-template <bool BF16, int BM, int BN, int WM, int WN, int NBUF, int MODE, bool GLU>
-__global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) {
+// KS > 1: as many such groups of waves to a workgroup, which has one tile: group g takes the k-tiles g, g + KS, ... into buffers of its
+// own, and the first one adds the others' sums to its own, in their order.  For products with fewer tiles than CUs.
+// bid, grid: the workgroup's number among those of this product, and theirs (a multiple of 8).
+template <bool BF16, int BM, int BN, int WM, int WN, int NBUF, int KS, int MODE, bool GLU>
+__device__ __forceinline__ void linear_tiles(const LinearParams& p, int bid, int grid) {
     constexpr bool AT = MODE == WEIGHT, BT = MODE != FORWARD;
     static_assert(!GLU || MODE == FORWARD, "two weights side by side: the forward product only");
     constexpr int ES = BF16 ? 2 : 4, KE = 128 / ES, PE = 16 / ES;        // bytes of an element; elements of a k-tile, of a piece
     constexpr int NW = WM * WN, MB = BM / WM / 16, NB = BN / WN / 16;
+    constexpr bool DEEP = BF16 && MB == 8 && NB == 4 && NBUF == 2;       // one workgroup to a CU, which walks the tiles
     constexpr int CA = BM / 8 / NW, CB = BN / 8 / NW;    // copies of 64 pieces per wave, operand and k-tile
+    constexpr int A_BYTES = BM * 128, STAGE = (BM + BN) * 128;
     static_assert(CA * NW * 8 == BM && CB * NW * 8 == BN, "whole copies for every wave");
     static_assert((!AT || BM % 64 == 0) && (!BT || BN % 64 == 0), "columns come in groups of 64");
-    constexpr bool DEEP = BF16 && MB == 8 && NB == 4 && NBUF == 2;       // one workgroup to a CU, which walks the tiles
-    constexpr int A_BYTES = BM * 128, STAGE = (BM + BN) * 128, OUT_N = GLU ? BN / 2 : BN;
-    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    static_assert(KS == 1 || (!DEEP && BM * BN * 4 <= NBUF * STAGE), "a group's sums fit its buffers");
+    static_assert(DEEP || !BF16 || ((!AT || MB == 2 || MB == 4) && (!BT || NB == 2 || NB == 4)), "see column_fragments");
+    constexpr int OUT_N = GLU ? BN / 2 : BN;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds_all[];
     const int lane = threadIdx.x & 63, l16 = lane & 15, kq = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
+    const int wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = wave_all % NW, group = wave_all / NW, wm = wave / WN, wn = wave % WN;
+    unsigned char* lds = lds_all + group * NBUF * STAGE;
 
     Groups groups;
     groups.load(p, BM);
-    int share;
     Tile t;
-    int j = blockIdx.x >> 3;
-    if (!find_tile<MODE, DEEP>(p, groups, BM, OUT_N, j, share, t)) return;
+    int j = bid >> 3;
+    if (!find_tile<MODE, DEEP>(p, groups, BM, OUT_N, bid, grid, j, t)) return;
 
     // k-tiles of a tile, of each half of a contraction in two halves (INPUT of SwiGLU)
     const int two = MODE == INPUT && p.glu ? 2 : 1;
     auto half_tiles = [&](const Tile& x) { return MODE == WEIGHT ? max((x.count + KE - 1) / KE, 1) : (p.K + KE - 1) / KE; };
+    auto steps = [&](const Tile& x) { return (half_tiles(x) * two + KS - 1) / KS; };         // of each group
 
     // ---- the copy side: a tile and a k-tile of its own, ahead of the products
     // copy c of an operand: 64 pieces, lane after lane; the k (columns kind) or first k (rows kind) of a lane's piece in its k-tile, and
@@ -341,7 +347,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
     auto aim = [&](const Tile& x) {
         s.KTh = half_tiles(x);
         s.length = MODE == WEIGHT ? x.count : p.K;
-        s.kt = 0;
+        s.kt = group;
         if constexpr (AT) s.A = reinterpret_cast<uint64_t>(p.A[x.half]) + static_cast<uint64_t>(x.first) * p.lda * ES;
         else s.A = static_cast<uint64_t>(x.first + x.m0) * p.lda * ES;                                   // + the half's array
         const uint64_t group = MODE == WEIGHT ? static_cast<uint64_t>(x.first) * p.ldb * ES
@@ -367,7 +373,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
     };
     auto issue = [&](int buf) {
         const int h = s.kt >= s.KTh ? 1 : 0, kt = s.kt - h * s.KTh;
-        const int left = s.length - kt * KE;             // of the contraction, from this k-tile on
+        const int left = KS > 1 && s.kt >= s.KTh * two ? 0 : s.length - kt * KE;             // of the contraction, from this k-tile on
         const uint64_t a = AT ? s.A + static_cast<uint64_t>(kt) * KE * ES * p.lda
                               : s.A + reinterpret_cast<uint64_t>(p.A[h]) + static_cast<uint64_t>(kt) * 128;
         unsigned char* dst = lds + buf * STAGE;
@@ -386,11 +392,10 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
     int jn = j;
     auto advance = [&]() {                               // (a source past the last tile goes on copying its last k-tile)
         if (!more) return;
-        if (s.kt + 1 < s.KTh * two) { ++s.kt; return; }
-        jn += gridDim.x >> 3;
+        if (s.kt - group + KS < s.KTh * two) { s.kt += KS; return; }
+        jn += grid >> 3;
         Tile n;
-        int unused;
-        if (find_tile<MODE, DEEP>(p, groups, BM, OUT_N, jn, unused, n)) aim(n);
+        if (find_tile<MODE, DEEP>(p, groups, BM, OUT_N, bid, grid, jn, n)) aim(n);
         else more = false;
     };
 
@@ -402,15 +407,6 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
             const int row = block * 16 + l16;
             const f32x4 v = *reinterpret_cast<const f32x4*>(op + row * 128 + ((4 * ks + kq) ^ ((row >> 1) & 7)) * 16);
             r.f[0] = v[0]; r.f[1] = v[1]; r.f[2] = v[2]; r.f[3] = v[3];
-        } else if constexpr (BF16) {
-            const int q = l16 & 3, jj = l16 >> 2, f = ((jj >> 1) & 1) | ((kq & 1) << 1);
-            const unsigned char* at = op + (block >> 2) * 8192 + (32 * ks + 8 * kq + jj) * 128 + (((block & 3) ^ f) * 32) + q * 8;
-            typedef __attribute__((address_space(3))) s16x4* tr_ptr;
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)at);
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(at + 512));
-            typedef __attribute__((ext_vector_type(2))) float f32x2;
-            const f32x2 l = __builtin_bit_cast(f32x2, lo), h = __builtin_bit_cast(f32x2, hi);
-            r.f[0] = l[0]; r.f[1] = l[1]; r.f[2] = h[0]; r.f[3] = h[1];
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -422,6 +418,37 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
     };
     auto multiply = [&](const Fragment& b, const Fragment& a, f32x4 c) -> f32x4 {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
+    };
+    // bf16, columns kind: all of a wave's fragments of a k-step (2 or 4: neighbouring blocks of one group of 64 columns) in one statement with
+    // its own wait; through the builtin a transposing read waits for all copies on their way, because it is taken to alias what they write
+    typedef int v2i __attribute__((ext_vector_type(2)));
+    auto join = [](v2i lo, v2i hi) -> bf16x8 {
+        typedef int v4i __attribute__((ext_vector_type(4)));
+        return __builtin_bit_cast(bf16x8, v4i{lo[0], lo[1], hi[0], hi[1]});
+    };
+    const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr)lds));
+    // LDS address, in the operand's first k-step, of this lane's part of a 16-column block
+    auto columns_address = [&](int block) -> uint32_t {
+        const int jj = l16 >> 2, f = ((jj >> 1) & 1) | ((kq & 1) << 1);
+        return (block >> 2) * 8192 + (8 * kq + jj) * 128 + (((block & 3) ^ f) * 32) + (l16 & 3) * 8;
+    };
+    auto column_fragments = [&](auto n_, uint32_t at, int first, Fragment* out) {
+        constexpr int N = decltype(n_)::value;
+        v2i x[4], y[4];
+        if constexpr (N == 2)
+            asm volatile("ds_read_b64_tr_b16 %0, %4\n\tds_read_b64_tr_b16 %1, %4 offset:512\n\tds_read_b64_tr_b16 %2, %5\n\t"
+                         "ds_read_b64_tr_b16 %3, %5 offset:512\n\ts_waitcnt lgkmcnt(0)"
+                         : "=&v"(x[0]), "=&v"(y[0]), "=&v"(x[1]), "=&v"(y[1])
+                         : "v"(at + columns_address(first)), "v"(at + columns_address(first + 1)) : "memory");
+        else
+            asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:512\n\tds_read_b64_tr_b16 %2, %9\n\t"
+                         "ds_read_b64_tr_b16 %3, %9 offset:512\n\tds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:512\n\t"
+                         "ds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:512\n\ts_waitcnt lgkmcnt(0)"
+                         : "=&v"(x[0]), "=&v"(y[0]), "=&v"(x[1]), "=&v"(y[1]), "=&v"(x[2]), "=&v"(y[2]), "=&v"(x[3]), "=&v"(y[3])
+                         : "v"(at + columns_address(first)), "v"(at + columns_address(first + 1)), "v"(at + columns_address(first + 2)),
+                           "v"(at + columns_address(first + 3)) : "memory");
+#pragma unroll
+        for (int i = 0; i < N; ++i) out[i] = __builtin_bit_cast(Fragment, join(x[i], y[i]));
     };
     // GLU: the first half of the staged weight rows are gate rows, the second the up rows of the same outputs
     auto b_block = [&](int jb) { return GLU ? (jb >= NB / 2 ? BN / 32 : 0) + wn * (NB / 2) + (jb >= NB / 2 ? jb - NB / 2 : jb) : wn * NB + jb; };
@@ -437,9 +464,8 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
         store_tile<BF16, MODE, GLU, MB, NB, DEEP>(p, t, acc, wm * MB * 16, GLU ? wn * (NB / 2) * 16 : wn * NB * 16, lds + NBUF * STAGE + wave * kPatch);
     };
     auto next_tile = [&]() {
-        j += gridDim.x >> 3;
-        int unused;
-        return find_tile<MODE, DEEP>(p, groups, BM, OUT_N, j, unused, t);
+        j += grid >> 3;
+        return find_tile<MODE, DEEP>(p, groups, BM, OUT_N, bid, grid, j, t);
     };
     auto barrier = [&]() {
         asm volatile("" ::: "memory");
@@ -456,22 +482,18 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
         // because it is taken to alias what they write.  A statement holds 8 MFMAs (two row blocks, four column blocks), behind the first of
         // them the reads of up to four fragments, and its own wait at the end, so that they land under the other MFMAs and its outputs are
         // ordinary registers.  What the compiler cannot see in it: two wait states between an ordinary write of an operand and the
-        // MFMA (the s_nop in front), and that an accumulator is not to be touched right behind (settle, before the epilogue).
+        // MFMA (the s_nop in front), and that an accumulator is not to be touched right behind (the s_nops at the end of the
+        // loop; inside it nothing else uses one).
         bf16x8 fa[2][4], fb[2][4];
         // LDS addresses (buffer 0) of this lane's part of a fragment; columns: of the four 16-column blocks of the wave's first group, + 512: the
         // k four further on, + 4096: the second k-step, + 8192: the next group; rows: of the two k-steps of the wave's first block, + 2048:
         // the next block
-        const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr)lds));
         uint32_t at_a[4], at_b[4];
-        {
-            const int q = l16 & 3, jj = l16 >> 2, f = ((jj >> 1) & 1) | ((kq & 1) << 1);
 #pragma unroll
-            for (int o = 0; o < 4; ++o) {
-                const uint32_t columns = (8 * kq + jj) * 128 + ((o ^ f) * 32) + q * 8;
-                const uint32_t rows = l16 * 128 + ((4 * (o & 1) + kq) ^ ((l16 >> 1) & 7)) * 16;
-                at_a[o] = lds0 + (AT ? wm * 16384 + columns : wm * 16384 + rows);
-                at_b[o] = lds0 + A_BYTES + (BT ? wn * 8192 + columns : wn * (GLU ? 4096 : 8192) + rows);
-            }
+        for (int o = 0; o < 4; ++o) {
+            const uint32_t columns = columns_address(o), rows = l16 * 128 + ((4 * (o & 1) + kq) ^ ((l16 >> 1) & 7)) * 16;
+            at_a[o] = lds0 + wm * 16384 + (AT ? columns : rows);
+            at_b[o] = lds0 + A_BYTES + (BT ? wn * 8192 + columns : wn * (GLU ? 4096 : 8192) + rows);
         }
 #define ETR_MF(C, B, A) "v_mfma_f32_16x16x32_bf16 %[c" #C "], %[b" #B "], %[a" #A "], %[c" #C "]\n\t"
 #define ETR_REST ETR_MF(1, 0, 1) ETR_MF(3, 1, 1) ETR_MF(2, 1, 0) ETR_MF(4, 2, 0) ETR_MF(5, 2, 1) ETR_MF(7, 3, 1) ETR_MF(6, 3, 0)
@@ -482,21 +504,16 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
 #define ETR_FRAGMENTS [a0] "v"(a[0]), [a1] "v"(a[1]), [b0] "v"(b[0]), [b1] "v"(b[1]), [b2] "v"(b[2]), [b3] "v"(b[3])
 #define ETR_OUT(N) [x##N] "=&v"(x[N]), [y##N] "=&v"(y[N])
 #define ETR_ROW(N) [r##N] "=&v"(out[N])
-#define ETR_AT(N) [p##N] "v"(COLUMNS ? at[(F + N) & 3] + slot : at[KS] + slot), [o##N] "n"(offset(N)), [q##N] "n"(offset(N) + 512)
-        typedef int v2i __attribute__((ext_vector_type(2)));
-        auto join = [](v2i lo, v2i hi) -> bf16x8 {
-            typedef int v4i __attribute__((ext_vector_type(4)));
-            return __builtin_bit_cast(bf16x8, v4i{lo[0], lo[1], hi[0], hi[1]});
-        };
-        // acc[I], acc[I + 1] += a[0..1] x b[0..3] (I < 0: no products); R fragments of k-step KS from block F of half H of an operand (its
+#define ETR_AT(N) [p##N] "v"(COLUMNS ? at[(F + N) & 3] + slot : at[KSTEP] + slot), [o##N] "n"(offset(N)), [q##N] "n"(offset(N) + 512)
+        // acc[I], acc[I + 1] += a[0..1] x b[0..3] (I < 0: no products); R fragments of k-step KSTEP from block F of half H of an operand (its
         // kind, its addresses and whether it is B) on into `out`
         auto step8 = [&](auto block, const bf16x8* a, const bf16x8* b, auto reads, auto columns_, auto is_b, const uint32_t* at, uint32_t slot, auto ks_, auto half,
                          auto from, bf16x8* out) {
-            constexpr int I = decltype(block)::value < 0 ? 0 : decltype(block)::value, R = decltype(reads)::value, KS = decltype(ks_)::value,
+            constexpr int I = decltype(block)::value < 0 ? 0 : decltype(block)::value, R = decltype(reads)::value, KSTEP = decltype(ks_)::value,
                           H = decltype(half)::value, F = decltype(from)::value;
             constexpr bool NONE = decltype(block)::value < 0, COLUMNS = decltype(columns_)::value, OF_B = decltype(is_b)::value;
             auto offset = [](int n) constexpr {
-                if (COLUMNS) return KS * 4096 + H * 8192;
+                if (COLUMNS) return KSTEP * 4096 + H * 8192;
                 if (OF_B && GLU) return ((F + n) >> 1) * 16384 + ((F + n) & 1) * 2048;       // the up rows lie 128 rows behind the gate rows
                 return (4 * H + F + n) * 2048;
             };
@@ -563,13 +580,6 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
                 step8(ETR_INT(second), fa[h] + 2, fb[ks], ETR_INT(2), ETR_INT(AT), ETR_INT(0), at_a, slot, ETR_INT(nks), ETR_INT(nh), ETR_INT(2), fa[nh] + 2);
             __builtin_amdgcn_sched_barrier(0);
         };
-        auto settle = [&]() {                            // nothing behind this reads an accumulator sooner than its MFMA has written it
-            asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
-#pragma unroll
-            for (int i = 0; i < MB; ++i)
-#pragma unroll
-                for (int jb = 0; jb < NB; ++jb) asm volatile("" : "+v"(acc[i][jb]));
-        };
         issue(0); advance();
         issue(1); advance();
         wait_copies<CA + CB>();
@@ -593,6 +603,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
                     advance();
                     buf ^= 1;
                 }
+                asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");         // the last products are written before anything reads them
             };
             // (the empty statements: what the three ways leave behind is one set of registers, not merged by copies)
             auto pin = [&]() {
@@ -609,7 +620,6 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
             pin();
             if (live == 0) k_loop(ETR_INT(0));
             pin();
-            settle();
             store();
         } while (next_tile());
 #undef ETR_INT
@@ -619,7 +629,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
         int buf = 0;
         for (;;) {
             clear();
-            const int KT = half_tiles(t) * two;
+            const int KT = steps(t);
             for (int kt = 0; kt < KT; ++kt) {
                 wait_copies<(NBUF - 2) * (CA + CB)>();   // this wave's part of the k-tile has landed
                 barrier();                               // ... and everybody's; and everybody is done with the buffer before it
@@ -628,20 +638,26 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
                 const unsigned char* op = lds + buf * STAGE;
 #pragma unroll
                 for (int ks = 0; ks < 2; ++ks) {
-                    Fragment fb[NB];
+                    const uint32_t at = lds0 + buf * STAGE + ks * 4096;
+                    Fragment fa[MB], fb[NB];
+                    if constexpr (BF16 && BT) {
+                        column_fragments(std::integral_constant<int, NB>{}, at + A_BYTES, wn * NB, fb);
+                    } else {
 #pragma unroll
-                    for (int jb = 0; jb < NB; ++jb) fb[jb] = fragment(op + A_BYTES, BT, BN, b_block(jb), ks);
-                    if constexpr (BF16) {
-#pragma unroll
-                        for (int i = 0; i < MB; ++i) {
-                            const Fragment fa = fragment(op, AT, BM, wm * MB + i, ks);
-#pragma unroll
-                            for (int jb = 0; jb < NB; ++jb) acc[i][jb] = multiply(fb[jb], fa, acc[i][jb]);
-                        }
-                    } else {                             // four MFMAs to a pair of fragments: not one behind the other
-                        Fragment fa[MB];
+                        for (int jb = 0; jb < NB; ++jb) fb[jb] = fragment(op + A_BYTES, BT, BN, b_block(jb), ks);
+                    }
+                    if constexpr (BF16 && AT) {
+                        column_fragments(std::integral_constant<int, MB>{}, at, wm * MB, fa);
+                    } else {
 #pragma unroll
                         for (int i = 0; i < MB; ++i) fa[i] = fragment(op, AT, BM, wm * MB + i, ks);
+                    }
+                    if constexpr (BF16) {
+#pragma unroll
+                        for (int i = 0; i < MB; ++i)
+#pragma unroll
+                            for (int jb = 0; jb < NB; ++jb) acc[i][jb] = multiply(fb[jb], fa[i], acc[i][jb]);
+                    } else {                             // four MFMAs to a pair of fragments: not one behind the other
 #pragma unroll
                         for (int v = 0; v < 4; ++v)
 #pragma unroll
@@ -653,12 +669,44 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_kernel(LinearParams p) 
                 }
                 buf = buf + 1 == NBUF ? 0 : buf + 1;
             }
+            if constexpr (KS > 1) {
+                wait_copies<0>();                        // nothing is on its way into the buffers any more
+                barrier();
+                f32x4* sums = reinterpret_cast<f32x4*>(lds) + (threadIdx.x % (NW * 64));
+                if (group > 0) {
+#pragma unroll
+                    for (int i = 0; i < MB; ++i)
+#pragma unroll
+                        for (int jb = 0; jb < NB; ++jb) sums[(i * NB + jb) * NW * 64] = acc[i][jb];
+                }
+                __syncthreads();
+                if (group > 0) return;
+#pragma unroll
+                for (int g = 1; g < KS; ++g)
+#pragma unroll
+                    for (int i = 0; i < MB; ++i)
+#pragma unroll
+                        for (int jb = 0; jb < NB; ++jb) acc[i][jb] += sums[g * (NBUF * STAGE / 16) + (i * NB + jb) * NW * 64];
+                store();
+                return;
+            }
             store();
             if (!next_tile()) break;
             wait_copies<0>();                            // (the stores too: the counted waits are for copies alone)
         }
     }
     wait_copies<0>();                                    // the copies that nobody needed
+}
+
+template <bool BF16, int BM, int BN, int WM, int WN, int NBUF, int KS, int MODE, bool GLU>
+__global__ __launch_bounds__(WM* WN * KS * 64, KS > 1 ? 4 : 2) void linear_kernel(LinearParams p) {
+    linear_tiles<BF16, BM, BN, WM, WN, NBUF, KS, MODE, GLU>(p, blockIdx.x, gridDim.x);
+}
+// dx and dw in one launch, where both take the small tiles: the first `n_input` workgroups (a multiple of 8) are dx's
+template <bool BF16, int BM, int BN, int WM, int WN, int NBUF, int KS>
+__global__ __launch_bounds__(WM* WN * KS * 64, KS > 1 ? 4 : 2) void linear_backward_kernel(LinearParams input, LinearParams weight, int n_input) {
+    if (static_cast<int>(blockIdx.x) < n_input) linear_tiles<BF16, BM, BN, WM, WN, NBUF, KS, INPUT, false>(input, blockIdx.x, n_input);
+    else linear_tiles<BF16, BM, BN, WM, WN, NBUF, KS, WEIGHT, false>(weight, blockIdx.x - n_input, gridDim.x - n_input);
 }
 
 // ---- the element-wise middle of the backward ----------------------------------------------------------------------------
@@ -670,6 +718,7 @@ constexpr int kChunk = 32;
 struct MiddleParams {
     const piece_t* pre; const piece_t* pre_up; const piece_t* dy; piece_t* da; piece_t* db;
     float* part;            // [2 with SwiGLU][chunks][N], optional
+    float* dbias[2];        // [E][N]; where no expert has more than a chunk of rows: the sums go here at once (a workgroup per expert)
     const int32_t* offsets;
     int rows, E, N, pieces, act, chunks;
 };
@@ -683,9 +732,10 @@ __global__ __launch_bounds__(256) void linear_middle_kernel(MiddleParams p) {
     Groups g;
     g.load(q, kChunk);
     const int chunk = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (chunk >= __builtin_amdgcn_readlane(g.tiles_incl, 63)) return;
-    const int e = __builtin_ctzll(__ballot(g.tiles_incl > chunk));
-    const int in_group = chunk - (__builtin_amdgcn_readlane(g.tiles_incl, e) - __builtin_amdgcn_readlane(g.tiles, e));
+    const bool direct = p.dbias[0] != nullptr;
+    if (!direct && chunk >= __builtin_amdgcn_readlane(g.tiles_incl, 63)) return;
+    const int e = direct ? chunk : __builtin_ctzll(__ballot(g.tiles_incl > chunk));
+    const int in_group = direct ? 0 : chunk - (__builtin_amdgcn_readlane(g.tiles_incl, e) - __builtin_amdgcn_readlane(g.tiles, e));
     const int first = __builtin_amdgcn_readlane(g.first, e) + in_group * kChunk;
     const int n_rows = min(kChunk, __builtin_amdgcn_readlane(g.count, e) - in_group * kChunk);
     const int c = blockIdx.y * 64 + lane;
@@ -734,18 +784,20 @@ __global__ __launch_bounds__(256) void linear_middle_kernel(MiddleParams p) {
             for (int i = 0; i < V; ++i) { sa[i] += a[i]; sb[i] += glu ? b[i] : 0.f; }
         }
     }
-    if (!p.part) return;
+    if (!p.part && !direct) return;
     if (wave > 0) {
 #pragma unroll
         for (int i = 0; i < V; ++i) { sums[wave - 1][lane][i] = sa[i]; sums[wave - 1][lane][V + i] = sb[i]; }
     }
     __syncthreads();
     if (wave > 0 || !in) return;
-    float* out = p.part + static_cast<size_t>(chunk) * p.N + static_cast<size_t>(c) * V;
+    const size_t at = static_cast<size_t>(chunk) * p.N + static_cast<size_t>(c) * V;
+    float* out = (direct ? p.dbias[0] : p.part) + at;
+    float* out_up = direct ? p.dbias[1] + at : out + static_cast<size_t>(p.chunks) * p.N;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         out[i] = ((sa[i] + sums[0][lane][i]) + sums[1][lane][i]) + sums[2][lane][i];
-        if (glu) out[static_cast<size_t>(p.chunks) * p.N + i] = ((sb[i] + sums[0][lane][V + i]) + sums[1][lane][V + i]) + sums[2][lane][V + i];
+        if (glu) out_up[i] = ((sb[i] + sums[0][lane][V + i]) + sums[1][lane][V + i]) + sums[2][lane][V + i];
     }
 }
 
@@ -782,41 +834,75 @@ long long tiles_at_most(const LinearParams& p, int mode, int BM, int out_n) {
     return columns * (p.rows / BM + std::min(p.E, p.rows));
 }
 
-template <bool BF16, int BM, int BN, int WM, int WN, int NBUF, int MODE, bool GLU>
+template <int BM, int BN, bool GLU> long long plan_tiles(LinearParams& p, int mode) {          // fills NT; the tiles at most
+    p.NT = (p.N + (GLU ? BN / 2 : BN) - 1) / (GLU ? BN / 2 : BN);
+    return tiles_at_most(p, mode, BM, GLU ? BN / 2 : BN);
+}
+template <bool BF16, int BM, int BN, int WM, int WN, int NBUF, int KS, int MODE, bool GLU>
 hipError_t launch_tiles(LinearParams p, hipStream_t st) {
     constexpr bool large = BM * BN >= 256 * 256;
-    constexpr size_t lds = static_cast<size_t>(BM + BN) * 128 * NBUF + (large ? WM * WN * kPatch : 0);
-    auto kern = linear_kernel<BF16, BM, BN, WM, WN, NBUF, MODE, GLU>;
+    constexpr size_t lds = static_cast<size_t>(BM + BN) * 128 * NBUF * KS + (large ? WM * WN * kPatch : 0);
+    auto kern = linear_kernel<BF16, BM, BN, WM, WN, NBUF, KS, MODE, GLU>;
     const hipError_t err = ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds);
     if (err != hipSuccess) return err;
-    p.NT = (p.N + (GLU ? BN / 2 : BN) - 1) / (GLU ? BN / 2 : BN);
-    const long long tiles = tiles_at_most(p, MODE, BM, GLU ? BN / 2 : BN);
-    if (tiles > (1ll << 30)) return hipErrorInvalidValue;
-    // one workgroup on each CU that walks the tiles, or (small tiles) one for each of them
-    const long long most = large ? cu_count() / 8 : 1 << 17, wanted = (tiles + 7) / 8 * (large ? 4 : 1);      // (up to four parts of a tile)
+    const long long tiles = plan_tiles<BM, BN, GLU>(p, MODE);
+    // one workgroup on each CU that walks the tiles (up to four parts of one), or (small tiles) one for each of them
+    const long long most = large ? cu_count() / 8 : 1 << 17, wanted = (tiles + 7) / 8 * (large ? 4 : 1);
+    if (KS > 1 && wanted > most) return hipErrorInvalidValue;
     const long long blocks = std::min(wanted, most) * 8;
-    hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(blocks)), dim3(WM * WN * 64), lds, st, p);
+    hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(blocks)), dim3(WM * WN * KS * 64), lds, st, p);
+    return hipGetLastError();
+}
+template <bool BF16, int NBUF, int KS>
+hipError_t launch_small_backward(LinearParams input, LinearParams weight, hipStream_t st) {
+    constexpr size_t lds = 128 * 128 * NBUF * KS;
+    auto kern = linear_backward_kernel<BF16, 64, 64, 2, 2, NBUF, KS>;
+    const hipError_t err = ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds);
+    if (err != hipSuccess) return err;
+    const long long most = 1 << 17, tiles_input = plan_tiles<64, 64, false>(input, INPUT), tiles_weight = plan_tiles<64, 64, false>(weight, WEIGHT);
+    const long long n_input = std::min((tiles_input + 7) / 8, most) * 8, n_weight = std::min((tiles_weight + 7) / 8, most) * 8;
+    if (KS > 1 && std::max(tiles_input, tiles_weight) > 8 * most) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(n_input + n_weight)), dim3(256 * KS), lds, st, input, weight, static_cast<int>(n_input));
     return hipGetLastError();
 }
 
+// Tiles of a product: the largest that give every CU one (two of the 128 x 128 ones, which share a CU), for the fewer bytes that they
+// read from LDS and L2 per product; few rows: 32, whose weights stream.  deep: fewer of these tiles than CUs and a contraction of eight k-tiles or
+// more, so that four groups of waves share a tile's contraction.
+enum class Tiles { ROWS32, T64, T128, T256 };
+struct Choice { Tiles tiles; bool deep; };
 template <int MODE, bool GLU>
-hipError_t launch_product(const LinearParams& p, bool bf16, hipStream_t st) {
-    const int out256 = GLU ? 128 : 256;
+Choice choose_tiles(const LinearParams& p, bool bf16) {
     const int rows_each = MODE == WEIGHT ? p.M : (p.rows + p.E - 1) / p.E;           // rows of a group, on average
     const long long groups = MODE == WEIGHT ? p.E * (p.glu ? 2 : 1) : std::min(p.E, p.rows);
     auto tiles = [&](int BM, int BN) { return groups * ((rows_each + BM - 1) / BM) * ((p.N + BN - 1) / BN); };
-    if (!bf16) {
-        if (tiles(128, out256 / 2) >= 2ll * cu_count()) return launch_tiles<false, 128, 128, 2, 2, 2, MODE, GLU>(p, st);
-        return launch_tiles<false, 64, 64, 2, 2, 3, MODE, GLU>(p, st);
-    }
+    const long long cus = cu_count();
+    const int k_tiles = ((MODE == WEIGHT ? (p.rows + p.E - 1) / p.E : p.K * (MODE == INPUT && p.glu ? 2 : 1)) + (bf16 ? 63 : 31)) / (bf16 ? 64 : 32);
+    if (MODE != WEIGHT && rows_each <= 32) return {Tiles::ROWS32, k_tiles >= 8 && tiles(32, MODE == FORWARD ? 64 : 128) <= cus};
+    if (bf16 && tiles(256, GLU ? 128 : 256) >= cus / 2) return {Tiles::T256, false};
+    if (tiles(128, GLU ? 64 : 128) >= (bf16 ? cus : 2 * cus)) return {Tiles::T128, false};
+    return {Tiles::T64, k_tiles >= 8 && tiles(64, GLU ? 32 : 64) <= cus};
+}
+template <bool BF16, int MODE, bool GLU>
+hipError_t launch_typed(const LinearParams& p, hipStream_t st) {
+    const Choice c = choose_tiles<MODE, GLU>(p, BF16);
     if constexpr (MODE != WEIGHT) {
-        if (rows_each <= 32) {
-            if constexpr (GLU || MODE == INPUT) return launch_tiles<true, 32, 128, 1, 4, 4, MODE, GLU>(p, st);
-            else return launch_tiles<true, 32, 64, 1, 4, 4, MODE, GLU>(p, st);
+        if (c.tiles == Tiles::ROWS32) {
+            if constexpr (GLU || MODE == INPUT)
+                return c.deep ? launch_tiles<BF16, 32, 128, 1, 4, 2, 4, MODE, GLU>(p, st) : launch_tiles<BF16, 32, 128, 1, 4, 4, 1, MODE, GLU>(p, st);
+            else
+                return c.deep ? launch_tiles<BF16, 32, 64, 1, 4, 3, 4, MODE, GLU>(p, st) : launch_tiles<BF16, 32, 64, 1, 4, 4, 1, MODE, GLU>(p, st);
         }
     }
-    if (tiles(256, out256) >= cu_count() / 2) return launch_tiles<true, 256, 256, 2, 4, 2, MODE, GLU>(p, st);
-    return launch_tiles<true, 128, 128, 2, 2, 2, MODE, GLU>(p, st);
+    if constexpr (BF16) {
+        if (c.tiles == Tiles::T256) return launch_tiles<true, 256, 256, 2, 4, 2, 1, MODE, GLU>(p, st);
+    }
+    if (c.tiles == Tiles::T128) return launch_tiles<BF16, 128, 128, 2, 2, 2, 1, MODE, GLU>(p, st);
+    return c.deep ? launch_tiles<BF16, 64, 64, 2, 2, 2, 4, MODE, GLU>(p, st) : launch_tiles<BF16, 64, 64, 2, 2, BF16 ? 4 : 2, 1, MODE, GLU>(p, st);
+}
+template <int MODE, bool GLU>
+hipError_t launch_product(const LinearParams& p, bool bf16, hipStream_t st) {
+    return bf16 ? launch_typed<true, MODE, GLU>(p, st) : launch_typed<false, MODE, GLU>(p, st);
 }
 
 int chunks_at_most(const etr_linear_config& c) { return c.rows / kChunk + std::min(c.E, c.rows); }
@@ -848,34 +934,40 @@ hipError_t launch_expert_linear_backward(const etr_linear_config& c, const void*
     const size_t middle = middle_bytes(c);
     void* da = c.act == ETR_ACT_NONE ? nullptr : at;
     void* db = glu ? at + middle : nullptr;
+    const bool direct = dbias && c.rows <= kChunk;
     const MiddleParams m{static_cast<const piece_t*>(pre), static_cast<const piece_t*>(pre_up), static_cast<const piece_t*>(dy), static_cast<piece_t*>(da),
-                         static_cast<piece_t*>(db), dbias ? reinterpret_cast<float*>(at + (glu ? 2 : 1) * middle) : nullptr, offsets, c.rows, c.E, c.N,
+                         static_cast<piece_t*>(db), dbias && !direct ? reinterpret_cast<float*>(at + (glu ? 2 : 1) * middle) : nullptr,
+                         {direct ? dbias : nullptr, direct ? dbias_up : nullptr}, offsets, c.rows, c.E, c.N,
                          static_cast<int>(static_cast<size_t>(c.N) * elt_bytes(c.dtype) / 16), c.act, chunks_at_most(c)};
     hipError_t err;
     if (da || dbias) {
-        const dim3 grid(m.chunks, (m.pieces + 63) / 64);
+        const dim3 grid(direct ? c.E : m.chunks, (m.pieces + 63) / 64);
         if (bf16) hipLaunchKernelGGL(linear_middle_kernel<true>, grid, dim3(256), 0, st, m);
         else hipLaunchKernelGGL(linear_middle_kernel<false>, grid, dim3(256), 0, st, m);
         if ((err = hipGetLastError()) != hipSuccess) return err;
     }
-    if (dbias) {
+    if (dbias && !direct) {
         hipLaunchKernelGGL(linear_bias_kernel, dim3((c.N + 63) / 64, c.E, glu ? 2 : 1), dim3(1024), 0, st, m, dbias, dbias_up);
         if ((err = hipGetLastError()) != hipSuccess) return err;
     }
     LinearParams p{};
     p.offsets = offsets; p.rows = c.rows; p.E = c.E; p.glu = glu;
     p.A[0] = da ? da : dy; p.A[1] = db;
-    if (dx) {
-        p.B[0] = w; p.B[1] = w_up; p.C[0] = dx;
-        p.N = c.K; p.K = c.N; p.lda = c.N; p.ldb = c.K;
-        if ((err = launch_product<INPUT, false>(p, bf16, st)) != hipSuccess) return err;
+    LinearParams q = p;
+    p.B[0] = w; p.B[1] = w_up; p.C[0] = dx;
+    p.N = c.K; p.K = c.N; p.lda = c.N; p.ldb = c.K;
+    q.B[0] = x; q.C[0] = dw; q.C[1] = dw_up;
+    q.M = c.N; q.N = c.K; q.K = c.rows; q.lda = c.N; q.ldb = c.K;
+    if (dx && dw) {
+        const Choice ci = choose_tiles<INPUT, false>(p, bf16), cw = choose_tiles<WEIGHT, false>(q, bf16);
+        if (cw.tiles == Tiles::T64 && (ci.tiles == Tiles::T64 || ci.tiles == Tiles::ROWS32)) {
+            if (ci.deep && tiles_at_most(q, WEIGHT, 64, 64) <= cu_count())
+                return bf16 ? launch_small_backward<true, 2, 4>(p, q, st) : launch_small_backward<false, 2, 4>(p, q, st);
+            return bf16 ? launch_small_backward<true, 4, 1>(p, q, st) : launch_small_backward<false, 2, 1>(p, q, st);
+        }
     }
-    if (dw) {
-        p.B[0] = x; p.B[1] = nullptr; p.C[0] = dw; p.C[1] = dw_up;
-        p.M = c.N; p.N = c.K; p.K = c.rows; p.lda = c.N; p.ldb = c.K;
-        if ((err = launch_product<WEIGHT, false>(p, bf16, st)) != hipSuccess) return err;
-    }
-    return hipSuccess;
+    if (dx && (err = launch_product<INPUT, false>(p, bf16, st)) != hipSuccess) return err;
+    return dw ? launch_product<WEIGHT, false>(q, bf16, st) : hipSuccess;
 }
 
 }  // namespace etr

@@ -48,8 +48,9 @@ __device__ __forceinline__ float score_gradient(const RouteBackwardParams& p, si
     return ds;
 }
 
-// Groups of whole 16-byte pieces (D a multiple of a piece; POOLED: as many pieces to a group as a power of two).
-template <bool BF16, int NV>
+// Groups of whole 16-byte pieces (D a multiple of a piece; POOLED: as many pieces to a group as a power of two).  A row of up to 64 NV
+// pieces stays in registers; with WIDE it comes in parts of that size, twice.
+template <bool BF16, int NV, bool WIDE>
 __global__ __launch_bounds__(1024) void route_backward_kernel(RouteBackwardParams p) {
     using R = Piece<BF16>;
     constexpr int V = R::kN;
@@ -62,35 +63,43 @@ __global__ __launch_bounds__(1024) void route_backward_kernel(RouteBackwardParam
     const piece_t* add = static_cast<const piece_t*>(p.dx_add);
     const piece_t zero = {0u, 0u, 0u, 0u};
     const int waves = blockDim.x >> 6;
+    auto group_sum = [&](float s) {                          // over the lanes that share a group
+        for (int o = 1; o < per_group; o <<= 1) s += __shfl_xor(s, o, 64);
+        return s;
+    };
     for (long long t = static_cast<long long>(blockIdx.x) * waves + (threadIdx.x >> 6); t < p.T; t += static_cast<long long>(gridDim.x) * waves) {
         const size_t row = static_cast<size_t>(t) * p.pieces;
         piece_t xv[NV], av[NV];
+        auto load = [&](piece_t (&v)[NV], const piece_t* from, int c0) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) xv[i] = lane + i * 64 < p.pieces ? x[row + lane + i * 64] : zero;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) av[i] = add && lane + i * 64 < p.pieces ? add[row + lane + i * 64] : zero;
+            for (int i = 0; i < NV; ++i) v[i] = from && c0 + lane + i * 64 < p.pieces ? from[row + c0 + lane + i * 64] : zero;
+        };
+        load(xv, x, 0);
+        if (!WIDE) load(av, add, 0);
         float b;
         const float ds = score_gradient(p, t, lane, b);
         for (int q = lane; q < p.P; q += 64) {
             float s = 0.f;
-#pragma unroll 8
+#pragma unroll 4
             for (int e = 0; e < p.E; ++e) s = fmaf(lane_value(ds, e), unit[e * p.P + q], s);
             u[q] = s;
         }
         float square = 0.f, mean[NV];
+        for (int c0 = 0; c0 < (WIDE ? p.pieces : 1); c0 += 64 * NV) {
+            if (WIDE && c0) load(xv, x, c0);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            float f[V], s = 0.f;
-            R::unpack(xv[i], f);
+            for (int i = 0; i < NV; ++i) {
+                float f[V], s = 0.f;
+                R::unpack(xv[i], f);
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                if (p.full) square = fmaf(f[j], f[j], square);
-                else s += f[j];
-            }
-            if (!p.full) {
-                for (int o = 1; o < per_group; o <<= 1) s += __shfl_xor(s, o, 64);
-                mean[i] = s / p.D;
-                square = fmaf(mean[i], mean[i], square);     // (counted by each of the group's lanes)
+                for (int j = 0; j < V; ++j) {
+                    if (p.full) square = fmaf(f[j], f[j], square);
+                    else s += f[j];
+                }
+                if (!p.full) {
+                    mean[i] = group_sum(s) / p.D;
+                    square = fmaf(mean[i], mean[i], square);                 // (counted by each of the group's lanes)
+                }
             }
         }
         square = wave_sum(square);
@@ -99,17 +108,29 @@ __global__ __launch_bounds__(1024) void route_backward_kernel(RouteBackwardParam
         const float cu = p.full ? inv / sqrtf(static_cast<float>(p.D)) : inv / p.D;
         const float cx = square > 0.f ? b / square * (p.full ? 1.0f : 1.0f / p.D) : 0.f;
         wave_sync();
+        for (int c0 = 0; c0 < (WIDE ? p.pieces : 1); c0 += 64 * NV) {
+            if (WIDE) {
+                load(xv, x, c0);
+                load(av, add, c0);
+            }
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = lane + i * 64;
-            if (c >= p.pieces) continue;
-            float f[V], a[V];
-            R::unpack(xv[i], f);
-            R::unpack(av[i], a);
-            const float uc = u[c / per_group] * cu;
+            for (int i = 0; i < NV; ++i) {
+                const int c = c0 + lane + i * 64;
+                float f[V], a[V];
+                R::unpack(xv[i], f);
+                R::unpack(av[i], a);
+                if (WIDE && !p.full) {
+                    float s = 0.f;
 #pragma unroll
-            for (int j = 0; j < V; ++j) a[j] += uc - cx * (p.full ? f[j] : mean[i]);
-            __builtin_nontemporal_store(R::pack(a), static_cast<piece_t*>(p.dx) + row + c);
+                    for (int j = 0; j < V; ++j) s += f[j];
+                    mean[i] = group_sum(s) / p.D;
+                }
+                if (c >= p.pieces) continue;
+                const float uc = u[c / per_group] * cu;
+#pragma unroll
+                for (int j = 0; j < V; ++j) a[j] += uc - cx * (p.full ? f[j] : mean[i]);
+                __builtin_nontemporal_store(R::pack(a), static_cast<piece_t*>(p.dx) + row + c);
+            }
         }
         wave_sync();                                         // u is written again by the next token
     }
@@ -166,15 +187,15 @@ __global__ __launch_bounds__(256) void route_backward_groups_kernel(RouteBackwar
     }
 }
 
-template <bool BF16, int NV>
+template <bool BF16, int NV, bool WIDE = false>
 hipError_t launch_pieces(const RouteBackwardParams& p, int waves, size_t lds, hipStream_t st) {
-    const void* kern = reinterpret_cast<const void*>(route_backward_kernel<BF16, NV>);
+    const void* kern = reinterpret_cast<const void*>(route_backward_kernel<BF16, NV, WIDE>);
     const hipError_t err = ensure_dynamic_lds(kern, lds);
     if (err != hipSuccess) return err;
     // as many workgroups as are resident together (16 waves to a CU at this kernel's registers, or what the LDS holds)
     const long long resident = static_cast<long long>(cu_count()) * std::max<long long>(1, std::min<long long>(16 / waves, (160 * 1024) / static_cast<long long>(lds)));
     const long long blocks = std::min(resident, (static_cast<long long>(p.T) + waves - 1) / waves);
-    hipLaunchKernelGGL((route_backward_kernel<BF16, NV>), dim3(static_cast<unsigned>(blocks)), dim3(waves * 64), lds, st, p);
+    hipLaunchKernelGGL((route_backward_kernel<BF16, NV, WIDE>), dim3(static_cast<unsigned>(blocks)), dim3(waves * 64), lds, st, p);
     return hipGetLastError();
 }
 template <bool BF16>
@@ -186,12 +207,13 @@ hipError_t launch_typed(const RouteBackwardParams& p, hipStream_t st) {
     int waves = embeddings > 64 * 1024 ? 16 : embeddings > 32 * 1024 ? 8 : 4;
     while (waves > 1 && embeddings + waves * row > 160 * 1024) waves /= 2;
     const bool whole = p.D % V == 0 && (p.full || (per_group <= 64 && (per_group & (per_group - 1)) == 0));
-    if (whole && p.pieces <= 64 * 8 && embeddings + waves * row <= 160 * 1024) {
+    if (whole && embeddings + waves * row <= 160 * 1024) {
         const size_t lds = embeddings + waves * row;
         if (p.pieces <= 64) return launch_pieces<BF16, 1>(p, waves, lds, st);
         if (p.pieces <= 128) return launch_pieces<BF16, 2>(p, waves, lds, st);
         if (p.pieces <= 256) return launch_pieces<BF16, 4>(p, waves, lds, st);
-        return launch_pieces<BF16, 8>(p, waves, lds, st);
+        if (p.pieces <= 512) return launch_pieces<BF16, 8>(p, waves, lds, st);
+        return launch_pieces<BF16, 8, true>(p, waves, lds, st);
     }
     const hipError_t err = ensure_dynamic_lds(reinterpret_cast<const void*>(route_backward_groups_kernel<BF16>), embeddings);
     if (err != hipSuccess) return err;

@@ -14,7 +14,9 @@ namespace etr {
 namespace {
 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
-constexpr int kMaxSortBlocks = 256, kMinPairs = 4096;      // pairs per workgroup: at least this many, and at most 256 workgroups
+// One workgroup for up to kOnePairs pairs; else kMinPairs or more to a workgroup, and at most 256 workgroups.
+constexpr int kMaxSortBlocks = 256, kMinPairs = 1024, kOnePairs = 4096;
+constexpr int kHeld = kOnePairs / kSortThreads;            // pairs of a thread that stay in registers between counting and placing
 constexpr int kMaxExperts = 64;
 
 struct SortParams {
@@ -43,22 +45,38 @@ __device__ __forceinline__ uint64_t same_expert(int e, int bits) {
     return same;
 }
 
-// Pairs of each expert in each wave's part of the workgroup's share: the wave's own row of LDS, so no atomics.
-__device__ __forceinline__ void count_pairs(const SortParams& p, int first, int end, int (*cnt)[kMaxExperts + 1]) {
+// Experts of N groups of 64 pairs from q on, all requested before the first is used.
+template <int N>
+__device__ __forceinline__ void load_experts(const SortParams& p, int q, int end, int (&e)[N]) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < N; ++i) e[i] = p.E;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (q + i * 64 < end) e[i] = pair_expert(p, q + i * 64 + lane, end);
+}
+// Pairs of each expert in each wave's part of the workgroup's share: the wave's own row of LDS, so no atomics.  e: the experts of its last
+// N groups of 64 pairs (all of them where it has no more).
+template <int N>
+__device__ __forceinline__ void count_pairs(const SortParams& p, int first, int end, int (*cnt)[kMaxExperts + 1], int (&e)[N]) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    for (int e = lane; e <= kMaxExperts; e += 64) cnt[wave][e] = 0;
+    for (int i = lane; i <= kMaxExperts; i += 64) cnt[wave][i] = 0;
     wave_sync();
-    for (int q = first; q < end; q += 64) {                  // (uniform over the wave)
-        const int e = pair_expert(p, q + lane, end);
-        const uint64_t same = same_expert(e, p.bits);
-        if (__builtin_ctzll(same) == lane) cnt[wave][e] += __popcll(same);
-        wave_sync();
+    for (int q = first; q < end; q += 64 * N) {              // (uniform over the wave)
+        load_experts(p, q, end, e);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (q + i * 64 >= end) continue;
+            const uint64_t same = same_expert(e[i], p.bits);
+            if (__builtin_ctzll(same) == lane) cnt[wave][e[i]] += __popcll(same);
+            wave_sync();
+        }
     }
 }
 
 // this wave's part of the workgroup's share of the pairs
 __device__ __forceinline__ void wave_part(const SortParams& p, int& first, int& end) {
-    const int begin = blockIdx.x * p.per_block, stop = min(begin + p.per_block, p.pairs), part = p.per_block / kSortWaves;
+    const int begin = min(static_cast<int>(blockIdx.x) * p.per_block, p.pairs), stop = min(begin + p.per_block, p.pairs), part = p.per_block / kSortWaves;
     first = min(begin + static_cast<int>(threadIdx.x >> 6) * part, stop);
     end = min(first + part, stop);
 }
@@ -67,7 +85,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortParams p) 
     __shared__ int cnt[kSortWaves][kMaxExperts + 1];
     int first, end;
     wave_part(p, first, end);
-    count_pairs(p, first, end, cnt);
+    int e[4];
+    count_pairs(p, first, end, cnt, e);
     __syncthreads();
     if (static_cast<int>(threadIdx.x) < p.E) {
         int s = 0;
@@ -100,7 +119,9 @@ __global__ __launch_bounds__(kSortThreads) void sort_rank_kernel(SortParams p) {
             atomicAdd(&total[e], sum);
         }
     }
-    count_pairs(p, first, end, cnt);
+    constexpr int N = ONE ? kHeld : 4;
+    int e[N];
+    count_pairs(p, first, end, cnt, e);
     __syncthreads();
     if (wave == 0) {                                         // lane = expert: rows before each expert, then before each wave
         int all = 0;
@@ -126,19 +147,24 @@ __global__ __launch_bounds__(kSortThreads) void sort_rank_kernel(SortParams p) {
     }
     __syncthreads();
     const int used = base[0];
-    for (int q = first; q < end; q += 64) {
-        const int e = pair_expert(p, q + lane, end);
-        const uint64_t same = same_expert(e, p.bits);
-        const int rank = __popcll(same & ((1ull << lane) - 1ull));
-        const bool in = e < p.E;
-        const int row = in ? cnt[wave][e] + rank : -1;
-        wave_sync();
-        if (in && rank == 0) cnt[wave][e] += __popcll(same);
-        wave_sync();
-        if (q + lane < end) {
-            p.row_of[q + lane] = row;
-            if (in) p.pair_of[row] = q + lane;
-            if (q + lane >= used) p.pair_of[q + lane] = -1;  // (no pair's row lies there)
+    for (int q0 = first; q0 < end; q0 += 64 * N) {
+        if (end - first > 64 * N) load_experts(p, q0, end, e);              // (else they are still there)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int q = q0 + i * 64;
+            if (q >= end) continue;
+            const uint64_t same = same_expert(e[i], p.bits);
+            const int rank = __popcll(same & ((1ull << lane) - 1ull));
+            const bool in = e[i] < p.E;
+            const int row = in ? cnt[wave][e[i]] + rank : -1;
+            wave_sync();
+            if (in && rank == 0) cnt[wave][e[i]] += __popcll(same);
+            wave_sync();
+            if (q + lane < end) {
+                p.row_of[q + lane] = row;
+                if (in) p.pair_of[row] = q + lane;
+                if (q + lane >= used) p.pair_of[q + lane] = -1;             // (no pair's row lies there)
+            }
         }
     }
 }
@@ -334,6 +360,7 @@ int pieces_of(const etr_sort_config& c) { return static_cast<int>(static_cast<si
 
 int pairs_per_block(const etr_sort_config& c) {
     const int pairs = c.T * c.k;
+    if (pairs <= kOnePairs) return kOnePairs;
     const int even = (pairs + kMaxSortBlocks - 1) / kMaxSortBlocks;
     return (std::max(even, kMinPairs) + kSortThreads - 1) / kSortThreads * kSortThreads;
 }
