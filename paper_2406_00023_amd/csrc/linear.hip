@@ -866,22 +866,69 @@ hipError_t launch_small_backward(LinearParams input, LinearParams weight, hipStr
     return hipGetLastError();
 }
 
-// Tiles of a product: the largest that give every CU one (two of the 128 x 128 ones, which share a CU), for the fewer bytes that they
-// read from LDS and L2 per product; few rows: 32, whose weights stream.  deep: fewer of these tiles than CUs and a contraction of eight k-tiles or
-// more, so that four groups of waves share a tile's contraction.
+// The tiles of a product, by estimate.  ROWS32: 32 rows x 64 weight rows (128 for SwiGLU and dx); deep: four groups of waves share a tile's
+// contraction.
 enum class Tiles { ROWS32, T64, T128, T256 };
 struct Choice { Tiles tiles; bool deep; };
+// Estimated microseconds: rounds of tiles over the places that they have on the chip, each a time per k-tile (alone ... chip full) and a time
+// besides, and at least the operands at the rate of memory.  In microseconds per 64-deep bf16 k-tile, from 33 products of 1 to 64 groups of 32 to
+// 32768 rows, contractions of 128 to 5632:
+//   T256    one to a CU    0.94 ... 1.69 (the power limit), 5 besides; a last round of half the CUs or fewer goes in parts
+//   T128    two to a CU    0.67 ... 1.2, 5
+//   T64     two to a CU    0.33 ... 0.5, 2.5; deep: one to a CU, 1.05 per four k-tiles, 3
+//   ROWS32  three (of 64 columns) or two to a CU, 0.25 ... 0.45 or 0.38 ... 0.6, 2; deep: one to a CU, 0.65 or 1.2 per four, 3
+// 2048 rows in 16 groups, 2048 x 2048: T256 46, T128 33, T64 40 us; 4096 rows: 48, 57, 68; 512 rows dense, 4096 x 4096: 61, 43, 29.
+// fp32, per 32-deep k-tile, where the CU's matrix pipes set the time as soon as two 64 x 64 tiles share it: T128 2.0 or 1.87 per tile on the
+// CU, T64 0.7 or 0.47, ROWS32 half of it (of 128 columns: all of it); deep: a quarter of the k-tiles, 4.5 times the work in each.
+double estimate_us(Choice c, double tiles, double k_tiles, bool wide, bool bf16) {
+    const double cus = cu_count();
+    const double steps = c.deep ? std::ceil(k_tiles / 4) : k_tiles;
+    if (!bf16) {
+        const double alone = c.tiles == Tiles::T128 ? 2.0 : c.tiles == Tiles::T64 || wide ? 0.7 : 0.45, each = c.tiles == Tiles::T128 ? 1.87 : c.tiles == Tiles::T64 || wide ? 0.47 : 0.25;
+        return steps * std::max(c.deep ? 1.7 * alone : alone, each * (c.deep ? 4.5 : 1.0) * std::max(1.0, tiles / cus)) + (c.deep ? 5.0 : 4.0);
+    }
+    double places = 2, alone = 0, full = 0, besides = 0;
+    switch (c.tiles) {
+        case Tiles::T256: places = 1; alone = 0.94; full = 1.69; besides = 5.0; break;
+        case Tiles::T128: alone = 0.67; full = 1.2; besides = 5.0; break;
+        case Tiles::T64: alone = 0.33; full = 0.5; besides = 2.5; break;
+        case Tiles::ROWS32: places = wide ? 2 : 3; alone = wide ? 0.38 : 0.25; full = wide ? 0.6 : 0.45; besides = 2.0; break;
+    }
+    if (c.deep) { places = 1; alone = full = c.tiles == Tiles::T64 ? 1.05 : wide ? 1.2 : 0.65; besides = 3.0; }
+    const double r = tiles / (places * cus), rest = r - std::floor(r);
+    double rounds = r <= 1 ? 1.0 : c.tiles == Tiles::T256 ? std::ceil(r) : r < 4 ? std::ceil(2 * r) / 2 : r + 0.25;
+    if (c.tiles == Tiles::T256 && r > 1 && rest > 0) rounds = std::floor(r) + (rest <= 0.25 ? 0.55 : rest <= 0.5 ? 0.7 : 1.0);
+    return rounds * (steps * (alone + (full - alone) * std::min(1.0, r)) + besides);
+}
 template <int MODE, bool GLU>
 Choice choose_tiles(const LinearParams& p, bool bf16) {
-    const int rows_each = MODE == WEIGHT ? p.M : (p.rows + p.E - 1) / p.E;           // rows of a group, on average
-    const long long groups = MODE == WEIGHT ? p.E * (p.glu ? 2 : 1) : std::min(p.E, p.rows);
-    auto tiles = [&](int BM, int BN) { return groups * ((rows_each + BM - 1) / BM) * ((p.N + BN - 1) / BN); };
-    const long long cus = cu_count();
-    const int k_tiles = ((MODE == WEIGHT ? (p.rows + p.E - 1) / p.E : p.K * (MODE == INPUT && p.glu ? 2 : 1)) + (bf16 ? 63 : 31)) / (bf16 ? 64 : 32);
-    if (MODE != WEIGHT && rows_each <= 32) return {Tiles::ROWS32, k_tiles >= 8 && tiles(32, MODE == FORWARD ? 64 : 128) <= cus};
-    if (bf16 && tiles(256, GLU ? 128 : 256) >= cus / 2) return {Tiles::T256, false};
-    if (tiles(128, GLU ? 64 : 128) >= (bf16 ? cus : 2 * cus)) return {Tiles::T128, false};
-    return {Tiles::T64, k_tiles >= 8 && tiles(64, GLU ? 32 : 64) <= cus};
+    const double rows_each = MODE == WEIGHT ? p.M : static_cast<double>(p.rows) / p.E;           // rows of a group, on average
+    const double groups = MODE == WEIGHT ? p.E * (p.glu ? 2 : 1) : std::min(p.E, p.rows);
+    const int halves = MODE == INPUT && p.glu ? 2 : 1, depth = bf16 ? 64 : 32;
+    const double k_tiles = halves * std::ceil((MODE == WEIGHT ? static_cast<double>(p.rows) / p.E : p.K) / depth);
+    // row tiles of a group: half a tile more than its rows fill, on average, where they are the batch's
+    auto tiles = [&](int BM, int BN) {
+        const double whole = std::ceil(rows_each / BM), mean = MODE == WEIGHT || rows_each < 1 ? whole : std::max(whole, rows_each / BM + (p.E > 1 ? 0.5 : 0.0));
+        return groups * mean * std::ceil(static_cast<double>(p.N) / (GLU ? BN / 2 : BN));
+    };
+    Choice best{Tiles::T64, false};
+    double best_us = 1e30;
+    auto offer = [&](Tiles kind, bool deep, int BM, int BN) {
+        const double n = tiles(BM, BN);
+        if (deep && (k_tiles < 8 || n > 4.0 * cu_count())) return;           // (one tile to a workgroup)
+        const double us = estimate_us({kind, deep}, n, k_tiles, BN == 128, bf16);
+        if (us < best_us) { best = {kind, deep}; best_us = us; }
+    };
+    const int columns32 = GLU || MODE == INPUT ? 128 : 64;
+    if (bf16) offer(Tiles::T256, false, 256, 256);
+    offer(Tiles::T128, false, 128, 128);
+    offer(Tiles::T64, false, 64, 64);
+    offer(Tiles::T64, true, 64, 64);
+    if (MODE != WEIGHT && rows_each <= 256) {
+        offer(Tiles::ROWS32, false, 32, columns32);
+        offer(Tiles::ROWS32, true, 32, columns32);
+    }
+    return best;
 }
 template <bool BF16, int MODE, bool GLU>
 hipError_t launch_typed(const LinearParams& p, hipStream_t st) {
