@@ -123,11 +123,12 @@ __device__ __forceinline__ bool find_tile(const LinearParams& p, const Groups& g
 
 // ---- epilogue --------------------------------------------------------------------------------------------------------
 
-__device__ __forceinline__ float sigmoid(float a) { return 1.0f / (1.0f + __expf(-a)); }
+// (hardware exponential and reciprocal, about 1 ulp each)
+__device__ __forceinline__ float sigmoid(float a) { return __builtin_amdgcn_rcpf(1.0f + __expf(-a)); }
 // The normal distribution function by the Chebyshev fit of erfc in Press et al., Numerical Recipes, 6.2 (fractional error below
 // 1.2e-7): no branch, where erff has two and keeps every value of a tile alive across them (789 spilled registers).
 __device__ __forceinline__ float normal_cdf(float a) {
-    const float x = fabsf(a) * 0.70710678118654752f, u = 1.0f / fmaf(0.5f, x, 1.0f);
+    const float x = fabsf(a) * 0.70710678118654752f, u = __builtin_amdgcn_rcpf(fmaf(0.5f, x, 1.0f));
     float s = 0.17087277f;
     s = fmaf(s, u, -0.82215223f); s = fmaf(s, u, 1.48851587f); s = fmaf(s, u, -1.13520398f); s = fmaf(s, u, 0.27886807f);
     s = fmaf(s, u, -0.18628806f); s = fmaf(s, u, 0.09678418f); s = fmaf(s, u, 0.37409196f); s = fmaf(s, u, 1.00002368f);

@@ -104,8 +104,8 @@ struct NormBackwardParams {
     const piece_t* s; const piece_t* y; const float* gate; const float* w_post; const float* w_pre;
     const piece_t* dx_out; const piece_t* dh;
     piece_t* dx; piece_t* dy; float* dgate;
-    float* part;            // [workgroups][2][d]: partial sums of dw_post and dw_pre (those asked for)
-    int want_post, want_pre;
+    float* part_post; float* part_pre;       // [workgroups][d] `stride` apart, each optional: partial sums of dw_post and dw_pre
+    size_t stride;
     int T, pieces;
     float inv_d, eps, rs, bs;
 };
@@ -207,17 +207,15 @@ __global__ __launch_bounds__(TEAM) void block_norm_backward_kernel(NormBackwardP
             p.dy[row + c] = R::pack(f);
         }
     }
-    const int d = p.pieces * V;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = l + i * TEAM;
         if (c >= p.pieces) continue;
-        float* at = p.part + static_cast<size_t>(blockIdx.x) * (p.want_post + p.want_pre) * d + static_cast<size_t>(c) * V;
+        const size_t at = blockIdx.x * p.stride + static_cast<size_t>(c) * V;
 #pragma unroll
         for (int j = 0; j < V; j += 4) {
-            if (p.want_post) *reinterpret_cast<float4*>(at + j) = make_float4(acc_post[i][j], acc_post[i][j + 1], acc_post[i][j + 2], acc_post[i][j + 3]);
-            if (p.want_pre)
-                *reinterpret_cast<float4*>(at + p.want_post * d + j) = make_float4(acc_pre[i][j], acc_pre[i][j + 1], acc_pre[i][j + 2], acc_pre[i][j + 3]);
+            if (p.part_post) *reinterpret_cast<float4*>(p.part_post + at + j) = make_float4(acc_post[i][j], acc_post[i][j + 1], acc_post[i][j + 2], acc_post[i][j + 3]);
+            if (p.part_pre) *reinterpret_cast<float4*>(p.part_pre + at + j) = make_float4(acc_pre[i][j], acc_pre[i][j + 1], acc_pre[i][j + 2], acc_pre[i][j + 3]);
         }
     }
 }
@@ -312,12 +310,15 @@ hipError_t launch_block_norm_backward(const etr_norm_config& c, const void* x_ou
                                       const float* w_post, const float* w_pre, const void* dx_out, const void* dh, void* dx,
                                       void* dy, float* dgate, float* dw_post, float* dw_pre, void* ws, hipStream_t st) {
     const int groups = backward_groups(c), want = (dw_post != nullptr) + (dw_pre != nullptr);
+    float* part = static_cast<float*>(ws);
+    const bool one = groups == 1;                        // its sums are the results
     const NormBackwardParams p{static_cast<const piece_t*>(x_out), static_cast<const piece_t*>(y), gate, w_post, w_pre,
                                static_cast<const piece_t*>(dx_out), static_cast<const piece_t*>(dh), static_cast<piece_t*>(dx),
-                               static_cast<piece_t*>(dy), dgate, static_cast<float*>(ws), dw_post != nullptr, dw_pre != nullptr,
+                               static_cast<piece_t*>(dy), dgate, one || !dw_post ? dw_post : part, one || !dw_pre ? dw_pre : part + (dw_post ? c.d : 0),
+                               static_cast<size_t>(want) * c.d,
                                c.T, pieces_of(c), 1.0f / c.d, c.eps, c.residual_scale, c.block_scale};
     const hipError_t err = c.dtype == ETR_BF16 ? backward_by_width<true>(p, groups, st) : backward_by_width<false>(p, groups, st);
-    if (err != hipSuccess || want == 0) return err;
+    if (err != hipSuccess || want == 0 || one) return err;
     const int width = want * c.d;
     hipLaunchKernelGGL(norm_weight_sum_kernel, dim3((width / 4 + kSumCols - 1) / kSumCols), dim3(kSumCols * kSumGroups), 0, st,
                        static_cast<const float*>(ws), groups, width, c.d, dw_post, dw_pre);
