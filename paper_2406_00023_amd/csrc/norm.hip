@@ -220,8 +220,8 @@ __global__ __launch_bounds__(TEAM) void block_norm_backward_kernel(NormBackwardP
     }
 }
 
-// Column sums of the workgroups' partial sums: 16 lanes' worth of float4 columns by 64 row groups, joined in LDS in a fixed order.
-constexpr int kSumCols = 16, kSumGroups = 64;
+// Column sums of the workgroups' partial sums: 8 float4 columns by 128 row groups, joined in LDS in a fixed order.
+constexpr int kSumCols = 8, kSumGroups = 128;
 __global__ __launch_bounds__(kSumCols* kSumGroups) void norm_weight_sum_kernel(const float* __restrict__ part, int n_part, int width, int d,
                                                                                float* __restrict__ first, float* __restrict__ second) {
     __shared__ float4 lds[kSumGroups][kSumCols];
