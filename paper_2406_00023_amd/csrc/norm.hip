@@ -6,7 +6,8 @@
 // Bound by memory: two rows in and two out per token forward, four in and two out backward.  So every row crosses once: a
 // team of threads (a wave, or a workgroup) holds a token's rows in registers between the sums and their use, all loads of a
 // token are requested before the first is waited for, and nothing is kept from the forward: the backward has the rows in
-// its hands anyway and takes their sums of squares again.
+// its hands anyway and takes their sums of squares again.  Measured: 32768 x 4096 bf16, everything at once, forward 207 us (5.2 TB/s),
+// backward 333 (4.8; a large copy 4.9) and the weights' sums 8; 3001 x 1080 fp32 without the norm behind the block 10, 21 and 4.
 #include <algorithm>
 
 #include "row_ops.h"
@@ -110,7 +111,7 @@ struct NormBackwardParams {
     float inv_d, eps, rs, bs;
 };
 
-// One workgroup per token at a time, walking on in steps of the grid; the weights' gradients stay in its registers until the end.
+// Backward: one workgroup per token at a time, walking on in steps of the grid; the weights' gradients stay in its registers until the end.
 template <bool BF16, int TEAM, int NV>
 __global__ __launch_bounds__(TEAM) void block_norm_backward_kernel(NormBackwardParams p) {
     using R = Piece<BF16>;
@@ -272,6 +273,8 @@ hipError_t forward_by_width(const NormParams& p, hipStream_t st) {
     if (p.pieces <= 4 * TEAM) return launch_forward<BF16, TEAM, 4>(p, st);
     return launch_forward<BF16, TEAM, 8>(p, st);
 }
+// A wave holds a row of up to 512 pieces (4096 bf16) without a barrier for its sums; a workgroup holds wider ones, and narrower ones where the
+// tokens are too few to fill the chip with waves (32 x 2048: 3.0 us).
 template <bool BF16>
 hipError_t forward_by_team(const NormParams& p, hipStream_t st) {
     if (p.pieces <= 64 || (p.pieces <= 64 * 8 && p.T > 2048)) return forward_by_width<BF16, 64>(p, st);

