@@ -816,7 +816,9 @@ __global__ __launch_bounds__(1024) void linear_bias_kernel(MiddleParams p, float
     Groups g;
     g.load(q, kChunk);
     const int e = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.x * 64 + lane;
-    const int tiles = __builtin_amdgcn_readlane(g.tiles, e), begin = __builtin_amdgcn_readlane(g.tiles_incl, e) - tiles;
+    // (offsets that are no ascending ones may name more chunks than there are)
+    const int begin = min(__builtin_amdgcn_readlane(g.tiles_incl, e) - __builtin_amdgcn_readlane(g.tiles, e), p.chunks);
+    const int tiles = min(__builtin_amdgcn_readlane(g.tiles, e), p.chunks - begin);
     const float* part = p.part + static_cast<size_t>(blockIdx.z) * p.chunks * p.N;
     float s = 0.f;
     if (n < p.N) {
