@@ -875,9 +875,9 @@ hipError_t launch_small_backward(LinearParams input, LinearParams weight, hipStr
     return hipGetLastError();
 }
 
-// The tiles of a product, by estimate.  ROWS32: 32 rows x 64 weight rows (128 for SwiGLU and dx); deep: four groups of waves share a tile's
-// contraction.
-enum class Tiles { ROWS32, T64, T128, T256 };
+// The tiles of a product, by estimate.  THIN (forward): 16 rows x 16 columns, every wave a group of its own, 16 (SwiGLU 8) to share the
+// contraction; ROWS32: 32 rows x 64 weight rows (128 for SwiGLU and dx); deep: four groups of waves share a tile's contraction.
+enum class Tiles { THIN, ROWS32, T64, T128, T256 };
 struct Choice { Tiles tiles; bool deep; };
 // Estimated microseconds: rounds of tiles over the places that they have on the chip, each a time per k-tile (alone ... chip full) and a time
 // besides, and at least the operands at the rate of memory.  In microseconds per 64-deep bf16 k-tile, from 33 products of 1 to 64 groups of 32 to
@@ -885,12 +885,17 @@ struct Choice { Tiles tiles; bool deep; };
 //   T256    one to a CU    0.94 ... 1.69 (the power limit), 5 besides; a last round of half the CUs or fewer goes in parts
 //   T128    two to a CU    0.67 ... 1.2, 5
 //   T64     two to a CU    0.33 ... 0.5, 2.5; deep: one to a CU, 1.05 per four k-tiles, 3
+//   THIN    one to a CU, 0.35 (SwiGLU 0.8) per 16 (8) k-tiles, 3.2, and 1.8 for them all; fp32 0.7 (1.0)
 //   ROWS32  three (of 64 columns) or two to a CU, 0.25 ... 0.45 or 0.38 ... 0.6, 2; deep: one to a CU, 0.65 or 1.2 per four, 3
 // 2048 rows in 16 groups, 2048 x 2048: T256 46, T128 33, T64 40 us; 4096 rows: 48, 57, 68; 512 rows dense, 4096 x 4096: 61, 43, 29.
 // fp32, per 32-deep k-tile, where the CU's matrix pipes set the time as soon as two 64 x 64 tiles share it: T128 2.0 or 1.87 per tile on the
 // CU, T64 0.7 or 0.47, ROWS32 half of it (of 128 columns: all of it); deep: a quarter of the k-tiles, 4.5 times the work in each.
 double estimate_us(Choice c, double tiles, double k_tiles, bool wide, bool bf16) {
     const double cus = cu_count();
+    if (c.tiles == Tiles::THIN) {
+        const double step = bf16 ? (wide ? 0.8 : 0.35) : wide ? 1.0 : 0.7;
+        return 1.8 + std::max(1.0, tiles / cus) * (3.2 + step * std::ceil(k_tiles / (wide ? 8 : 16)));
+    }
     const double steps = c.deep ? std::ceil(k_tiles / 4) : k_tiles;
     if (!bf16) {
         const double alone = c.tiles == Tiles::T128 ? 2.0 : c.tiles == Tiles::T64 || wide ? 0.7 : 0.45, each = c.tiles == Tiles::T128 ? 1.87 : c.tiles == Tiles::T64 || wide ? 0.47 : 0.25;
@@ -898,6 +903,7 @@ double estimate_us(Choice c, double tiles, double k_tiles, bool wide, bool bf16)
     }
     double places = 2, alone = 0, full = 0, besides = 0;
     switch (c.tiles) {
+        case Tiles::THIN: break;
         case Tiles::T256: places = 1; alone = 0.94; full = 1.69; besides = 5.0; break;
         case Tiles::T128: alone = 0.67; full = 1.2; besides = 5.0; break;
         case Tiles::T64: alone = 0.33; full = 0.5; besides = 2.5; break;
@@ -925,7 +931,7 @@ Choice choose_tiles(const LinearParams& p, bool bf16) {
     auto offer = [&](Tiles kind, bool deep, int BM, int BN) {
         const double n = tiles(BM, BN);
         if (deep && (k_tiles < 8 || n > 4.0 * cu_count())) return;           // (one tile to a workgroup)
-        const double us = estimate_us({kind, deep}, n, k_tiles, BN == 128, bf16);
+        const double us = estimate_us({kind, deep}, n, k_tiles, kind == Tiles::THIN ? GLU : BN == 128, bf16);
         if (us < best_us) { best = {kind, deep}; best_us = us; }
     };
     const int columns32 = GLU || MODE == INPUT ? 128 : 64;
@@ -937,11 +943,15 @@ Choice choose_tiles(const LinearParams& p, bool bf16) {
         offer(Tiles::ROWS32, false, 32, columns32);
         offer(Tiles::ROWS32, true, 32, columns32);
     }
+    if (MODE == FORWARD) offer(Tiles::THIN, true, 16, GLU ? 32 : 16);
     return best;
 }
 template <bool BF16, int MODE, bool GLU>
 hipError_t launch_typed(const LinearParams& p, hipStream_t st) {
     const Choice c = choose_tiles<MODE, GLU>(p, BF16);
+    if constexpr (MODE == FORWARD) {
+        if (c.tiles == Tiles::THIN) return launch_tiles<BF16, 16, GLU ? 32 : 16, 1, 1, 2, GLU ? 8 : 16, MODE, GLU>(p, st);
+    }
     if constexpr (MODE != WEIGHT) {
         if (c.tiles == Tiles::ROWS32) {
             if constexpr (GLU || MODE == INPUT)

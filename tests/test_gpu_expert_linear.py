@@ -89,6 +89,19 @@ def test_forward(counts, spare, K, N, act, bias, residual, keep, dtype):
         assert_within(y[rows], want, hs * want.abs() + (1 + hs) * err, "y")
 
 
+# few rows against a long contraction, which many waves share: k-tiles that do not divide by their number, a last row tile of one row,
+# column tiles of a piece
+LONG = [((1,), 0, 1544, 72), ((17,), 3, 4104, 200), ((3, 0, 16, 33), 1, 1096, 152), ((130,), 0, 2048, 40), ((0, 1), 0, 8192, 8)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act,bias,residual,keep", [("none", False, False, False), ("silu", True, True, True), ("gelu", False, True, False),
+                                                    ("swiglu", True, True, True)])
+@pytest.mark.parametrize("counts,spare,K,N", LONG)
+def test_forward_of_few_rows(counts, spare, K, N, act, bias, residual, keep, dtype):
+    test_forward(counts, spare, K, N, act, bias, residual, keep, dtype)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("act", ["none", "silu", "gelu", "swiglu"])
 @pytest.mark.parametrize("counts,spare,K,N", CASES)
