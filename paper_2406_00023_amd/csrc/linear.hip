@@ -705,7 +705,7 @@ __device__ __forceinline__ void linear_tiles(const LinearParams& p, int bid, int
 }
 
 template <bool BF16, int BM, int BN, int WM, int WN, int NBUF, int KS, int MODE, bool GLU>
-__global__ __launch_bounds__(WM* WN * KS * 64, KS > 1 ? 4 : 2) void linear_kernel(LinearParams p) {
+__global__ __launch_bounds__(WM* WN * KS * 64, WM * WN * KS > 8 ? 4 : 2) void linear_kernel(LinearParams p) {
     linear_tiles<BF16, BM, BN, WM, WN, NBUF, KS, MODE, GLU>(p, blockIdx.x, gridDim.x);
 }
 // dx and dw in one launch, where both take the small tiles: the first `n_input` workgroups (a multiple of 8) are dx's
@@ -875,25 +875,27 @@ hipError_t launch_small_backward(LinearParams input, LinearParams weight, hipStr
     return hipGetLastError();
 }
 
-// The tiles of a product, by estimate.  THIN (forward): 16 rows x 16 columns, every wave a group of its own, 16 (SwiGLU 8) to share the
-// contraction; ROWS32: 32 rows x 64 weight rows (128 for SwiGLU and dx); deep: four groups of waves share a tile's contraction.
+// The tiles of a product, by estimate.  THIN: 16 rows x 16 columns (SwiGLU 32 weight rows, dx 64 columns), every wave a group of its own, 16
+// (8) to share the contraction; ROWS32: 32 rows x 64 weight rows (128 for SwiGLU and dx); deep: four groups of waves share a tile's contraction.
 enum class Tiles { THIN, ROWS32, T64, T128, T256 };
-struct Choice { Tiles tiles; bool deep; };
+struct Choice { Tiles tiles; bool deep; double us; };
 // Estimated microseconds: rounds of tiles over the places that they have on the chip, each a time per k-tile (alone ... chip full) and a time
 // besides, and at least the operands at the rate of memory.  In microseconds per 64-deep bf16 k-tile, from 33 products of 1 to 64 groups of 32 to
 // 32768 rows, contractions of 128 to 5632:
 //   T256    one to a CU    0.94 ... 1.69 (the power limit), 5 besides; a last round of half the CUs or fewer goes in parts
 //   T128    two to a CU    0.67 ... 1.2, 5
 //   T64     two to a CU    0.33 ... 0.5, 2.5; deep: one to a CU, 1.05 per four k-tiles, 3
-//   THIN    one to a CU, 0.35 (SwiGLU 0.8) per 16 (8) k-tiles, 3.2, and 1.8 for them all; fp32 0.7 (1.0)
+//   THIN    one to a CU, 0.35 (SwiGLU, dx: 0.8) per 16 (8) k-tiles, 3.2, and 1.8 for them all; fp32 0.7 (1.0, 1.45)
 //   ROWS32  three (of 64 columns) or two to a CU, 0.25 ... 0.45 or 0.38 ... 0.6, 2; deep: one to a CU, 0.65 or 1.2 per four, 3
+// Few rows, THIN and the best of the others: 18 rows, 3840 x 1472 6.0 and 12.0 us, fp32 9.8 and 39.2; 64 rows, 4096 x 4096 24.9 and 12.7, fp32
+// 38.4 and 41.6; dx of 64 rows, 8192 x 256 16.2 and 27.8, fp32 50 and 143.
 // 2048 rows in 16 groups, 2048 x 2048: T256 46, T128 33, T64 40 us; 4096 rows: 48, 57, 68; 512 rows dense, 4096 x 4096: 61, 43, 29.
 // fp32, per 32-deep k-tile, where the CU's matrix pipes set the time as soon as two 64 x 64 tiles share it: T128 2.0 or 1.87 per tile on the
 // CU, T64 0.7 or 0.47, ROWS32 half of it (of 128 columns: all of it); deep: a quarter of the k-tiles, 4.5 times the work in each.
-double estimate_us(Choice c, double tiles, double k_tiles, bool wide, bool bf16) {
+double estimate_us(Choice c, double tiles, double k_tiles, bool wide, bool transposed, bool bf16) {
     const double cus = cu_count();
     if (c.tiles == Tiles::THIN) {
-        const double step = bf16 ? (wide ? 0.8 : 0.35) : wide ? 1.0 : 0.7;
+        const double step = bf16 ? (wide ? 0.8 : 0.35) : transposed ? 1.45 : wide ? 1.0 : 0.7;
         return 1.8 + std::max(1.0, tiles / cus) * (3.2 + step * std::ceil(k_tiles / (wide ? 8 : 16)));
     }
     const double steps = c.deep ? std::ceil(k_tiles / 4) : k_tiles;
@@ -915,8 +917,9 @@ double estimate_us(Choice c, double tiles, double k_tiles, bool wide, bool bf16)
     if (c.tiles == Tiles::T256 && r > 1 && rest > 0) rounds = std::floor(r) + (rest <= 0.25 ? 0.55 : rest <= 0.5 ? 0.7 : 1.0);
     return rounds * (steps * (alone + (full - alone) * std::min(1.0, r)) + besides);
 }
+// small: only T64 is to be had, deep or not
 template <int MODE, bool GLU>
-Choice choose_tiles(const LinearParams& p, bool bf16) {
+Choice choose_tiles(const LinearParams& p, bool bf16, bool small = false, bool small_deep = false) {
     const double rows_each = MODE == WEIGHT ? p.M : static_cast<double>(p.rows) / p.E;           // rows of a group, on average
     const double groups = MODE == WEIGHT ? p.E * (p.glu ? 2 : 1) : std::min(p.E, p.rows);
     const int halves = MODE == INPUT && p.glu ? 2 : 1, depth = bf16 ? 64 : 32;
@@ -926,15 +929,18 @@ Choice choose_tiles(const LinearParams& p, bool bf16) {
         const double whole = std::ceil(rows_each / BM), mean = MODE == WEIGHT || rows_each < 1 ? whole : std::max(whole, rows_each / BM + (p.E > 1 ? 0.5 : 0.0));
         return groups * mean * std::ceil(static_cast<double>(p.N) / (GLU ? BN / 2 : BN));
     };
-    Choice best{Tiles::T64, false};
-    double best_us = 1e30;
+    Choice best{Tiles::T64, false, 1e30};
     auto offer = [&](Tiles kind, bool deep, int BM, int BN) {
         const double n = tiles(BM, BN);
         if (deep && (k_tiles < 8 || n > 4.0 * cu_count())) return;           // (one tile to a workgroup)
-        const double us = estimate_us({kind, deep}, n, k_tiles, kind == Tiles::THIN ? GLU : BN == 128, bf16);
-        if (us < best_us) { best = {kind, deep}; best_us = us; }
+        const double us = estimate_us({kind, deep, 0}, n, k_tiles, kind == Tiles::THIN ? BN > 16 : BN == 128, MODE != FORWARD, bf16);
+        if (us < best.us) best = {kind, deep, us};
     };
     const int columns32 = GLU || MODE == INPUT ? 128 : 64;
+    if (small) {
+        offer(Tiles::T64, small_deep, 64, 64);
+        return best;
+    }
     if (bf16) offer(Tiles::T256, false, 256, 256);
     offer(Tiles::T128, false, 128, 128);
     offer(Tiles::T64, false, 64, 64);
@@ -943,14 +949,15 @@ Choice choose_tiles(const LinearParams& p, bool bf16) {
         offer(Tiles::ROWS32, false, 32, columns32);
         offer(Tiles::ROWS32, true, 32, columns32);
     }
-    if (MODE == FORWARD) offer(Tiles::THIN, true, 16, GLU ? 32 : 16);
+    if (MODE != WEIGHT) offer(Tiles::THIN, true, 16, MODE == INPUT ? 64 : GLU ? 32 : 16);
     return best;
 }
 template <bool BF16, int MODE, bool GLU>
 hipError_t launch_typed(const LinearParams& p, hipStream_t st) {
     const Choice c = choose_tiles<MODE, GLU>(p, BF16);
-    if constexpr (MODE == FORWARD) {
-        if (c.tiles == Tiles::THIN) return launch_tiles<BF16, 16, GLU ? 32 : 16, 1, 1, 2, GLU ? 8 : 16, MODE, GLU>(p, st);
+    if constexpr (MODE != WEIGHT) {
+        constexpr int columns = MODE == INPUT ? 64 : GLU ? 32 : 16;
+        if (c.tiles == Tiles::THIN) return launch_tiles<BF16, 16, columns, 1, 1, 2, (columns > 16 ? 8 : 16), MODE, GLU>(p, st);
     }
     if constexpr (MODE != WEIGHT) {
         if (c.tiles == Tiles::ROWS32) {
@@ -1026,10 +1033,14 @@ hipError_t launch_expert_linear_backward(const etr_linear_config& c, const void*
     q.M = c.N; q.N = c.K; q.K = c.rows; q.lda = c.N; q.ldb = c.K;
     if (dx && dw) {
         const Choice ci = choose_tiles<INPUT, false>(p, bf16), cw = choose_tiles<WEIGHT, false>(q, bf16);
-        if (cw.tiles == Tiles::T64 && (ci.tiles == Tiles::T64 || ci.tiles == Tiles::ROWS32)) {
-            if (ci.deep && tiles_at_most(q, WEIGHT, 64, 64) <= cu_count())
+        // one launch, unless dx in it takes longer than dx by tiles of its own and dw behind it.  fp32, together and apart: 500 rows, 512 x 512
+        // 14.0 and 19.9 us; 2500 in 8 groups, 1048 x 520 92.0 and 97.4; 18 rows, 3840 x 1472 87.9 and 37.6
+        if (cw.tiles == Tiles::T64) {
+            const double apart = ci.us + cw.us;
+            if (tiles_at_most(q, WEIGHT, 64, 64) <= cu_count() && choose_tiles<INPUT, false>(p, bf16, true, true).us <= apart)
                 return bf16 ? launch_small_backward<true, 2, 4>(p, q, st) : launch_small_backward<false, 2, 4>(p, q, st);
-            return bf16 ? launch_small_backward<true, 4, 1>(p, q, st) : launch_small_backward<false, 2, 1>(p, q, st);
+            if (choose_tiles<INPUT, false>(p, bf16, true).us <= apart)
+                return bf16 ? launch_small_backward<true, 4, 1>(p, q, st) : launch_small_backward<false, 2, 1>(p, q, st);
         }
     }
     if (dx && (err = launch_product<INPUT, false>(p, bf16, st)) != hipSuccess) return err;

@@ -148,6 +148,13 @@ def test_backward(counts, spare, K, N, act, dtype):
         assert_within(dx[rows], dx_want, hs * dx_want.abs() + (1 + hs) * dx_err, ("dx", e))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ["none", "gelu", "swiglu"])
+@pytest.mark.parametrize("counts,spare,N,K", LONG)
+def test_backward_of_few_rows(counts, spare, K, N, act, dtype):
+    test_backward(counts, spare, K, N, act, dtype)
+
+
 def test_dense_without_offsets_and_in_place_residual():
     R, K, N = 300, 264, 136
     s = _inputs((R,), 0, K, N, torch.bfloat16, "gelu", True, True)
