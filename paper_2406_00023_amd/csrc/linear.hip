@@ -880,42 +880,47 @@ hipError_t launch_small_backward(LinearParams input, LinearParams weight, hipStr
 enum class Tiles { THIN, ROWS32, T64, T128, T256 };
 struct Choice { Tiles tiles; bool deep; double us; };
 // Estimated microseconds: rounds of tiles over the places that they have on the chip, each a time per k-tile (alone ... chip full) and a time
-// besides, and at least the operands at the rate of memory.  In microseconds per 64-deep bf16 k-tile, from 33 products of 1 to 64 groups of 32 to
-// 32768 rows, contractions of 128 to 5632:
-//   T256    one to a CU    0.94 ... 1.69 (the power limit), 5 besides; a last round of half the CUs or fewer goes in parts
-//   T128    two to a CU    0.67 ... 1.2, 5
-//   T64     two to a CU    0.33 ... 0.5, 2.5; deep: one to a CU, 1.05 per four k-tiles, 3
-//   THIN    one to a CU, 0.35 (SwiGLU, dx: 0.8) per 16 (8) k-tiles, 3.2, and 1.8 for them all; fp32 0.7 (1.0, 1.45)
-//   ROWS32  three (of 64 columns) or two to a CU, 0.25 ... 0.45 or 0.38 ... 0.6, 2; deep: one to a CU, 0.65 or 1.2 per four, 3
+// besides.  In microseconds per 64-deep bf16 k-tile, fitted to 130 products (1 to 16384 rows in 1 to 64 groups, widths of 128 to 8192; each
+// forward, with SwiGLU, dx and dw, by all the tiles); on 130 others the choice takes 1.4 % more than the best of the tiles, on average:
+//   T256    one to a CU    0.94 ... 1.69 (the power limit), 5.5 besides; a last round of half the CUs or fewer goes in parts
+//   T128    two to a CU    0.67 ... 1.2, 4.2
+//   T64     two to a CU    0.33 ... 0.55, 2.8; deep: one to a CU, 1.05 per four k-tiles, 3
+//   ROWS32  three (of 64 columns) or two to a CU, 0.25 ... 0.45 or 0.38 ... 0.6, 2; deep: one to a CU, 0.65 or 1.6 per four, 3
+//   THIN    one to a CU, 0.45 (SwiGLU 0.85, dx 0.8) per 16 (8) k-tiles, 3.2, and 1.8 for them all; fp32 0.7 (0.85, 1.45)
 // Few rows, THIN and the best of the others: 18 rows, 3840 x 1472 6.0 and 12.0 us, fp32 9.8 and 39.2; 64 rows, 4096 x 4096 24.9 and 12.7, fp32
 // 38.4 and 41.6; dx of 64 rows, 8192 x 256 16.2 and 27.8, fp32 50 and 143.
 // 2048 rows in 16 groups, 2048 x 2048: T256 46, T128 33, T64 40 us; 4096 rows: 48, 57, 68; 512 rows dense, 4096 x 4096: 61, 43, 29.
-// fp32, per 32-deep k-tile, where the CU's matrix pipes set the time as soon as two 64 x 64 tiles share it: T128 2.0 or 1.87 per tile on the
-// CU, T64 0.7 or 0.47, ROWS32 half of it (of 128 columns: all of it); deep: a quarter of the k-tiles, 4.5 times the work in each.
+// fp32, per 32-deep k-tile, where the CU's matrix pipes set the time as soon as two 64 x 64 tiles share it: T128 2.0 or 2.1 per tile on the
+// CU and 2.4 for its epilogue, T64 0.7 or 0.47 and 0.5, ROWS32 0.45 or 0.25 and 0.4 (of 128 columns: T64's); deep: a quarter of the k-tiles, 4.5
+// times the work in each.
 double estimate_us(Choice c, double tiles, double k_tiles, bool wide, bool transposed, bool bf16) {
     const double cus = cu_count();
     if (c.tiles == Tiles::THIN) {
-        const double step = bf16 ? (wide ? 0.8 : 0.35) : transposed ? 1.45 : wide ? 1.0 : 0.7;
-        return 1.8 + std::max(1.0, tiles / cus) * (3.2 + step * std::ceil(k_tiles / (wide ? 8 : 16)));
+        const double step = bf16 ? (transposed ? 0.8 : wide ? 0.85 : 0.45) : transposed ? 1.45 : wide ? 0.85 : 0.7;
+        return 1.8 + std::ceil(std::max(1.0, tiles / cus) - 0.1) * (3.2 + step * std::ceil(k_tiles / (wide ? 8 : 16)));
     }
     const double steps = c.deep ? std::ceil(k_tiles / 4) : k_tiles;
     if (!bf16) {
-        const double alone = c.tiles == Tiles::T128 ? 2.0 : c.tiles == Tiles::T64 || wide ? 0.7 : 0.45, each = c.tiles == Tiles::T128 ? 1.87 : c.tiles == Tiles::T64 || wide ? 0.47 : 0.25;
-        return steps * std::max(c.deep ? 1.7 * alone : alone, each * (c.deep ? 4.5 : 1.0) * std::max(1.0, tiles / cus)) + (c.deep ? 5.0 : 4.0);
+        const bool t64 = c.tiles == Tiles::T64 || wide;
+        const double alone = c.tiles == Tiles::T128 ? 2.0 : t64 ? 0.7 : 0.45, each = c.tiles == Tiles::T128 ? 2.1 : t64 ? 0.47 : 0.25;
+        const double epilogue = c.tiles == Tiles::T128 ? 2.4 : t64 ? 0.5 : 0.4;
+        return std::max(steps * (c.deep ? 1.7 * alone : alone), std::max(1.0, tiles / cus) * (steps * each * (c.deep ? 4.5 : 1.0) + epilogue)) + (c.deep ? 5.0 : 4.0);
     }
     double places = 2, alone = 0, full = 0, besides = 0;
     switch (c.tiles) {
         case Tiles::THIN: break;
-        case Tiles::T256: places = 1; alone = 0.94; full = 1.69; besides = 5.0; break;
-        case Tiles::T128: alone = 0.67; full = 1.2; besides = 5.0; break;
-        case Tiles::T64: alone = 0.33; full = 0.5; besides = 2.5; break;
+        case Tiles::T256: places = 1; alone = 0.94; full = 1.69; besides = 5.5; break;
+        case Tiles::T128: alone = 0.67; full = 1.2; besides = 4.2; break;
+        case Tiles::T64: alone = 0.33; full = 0.55; besides = 2.8; break;
         case Tiles::ROWS32: places = wide ? 2 : 3; alone = wide ? 0.38 : 0.25; full = wide ? 0.6 : 0.45; besides = 2.0; break;
     }
-    if (c.deep) { places = 1; alone = full = c.tiles == Tiles::T64 ? 1.05 : wide ? 1.2 : 0.65; besides = 3.0; }
+    if (c.deep) { places = 1; alone = full = c.tiles == Tiles::T64 ? 1.05 : wide ? 1.6 : 0.65; besides = 3.0; }
     const double r = tiles / (places * cus), rest = r - std::floor(r);
-    double rounds = r <= 1 ? 1.0 : c.tiles == Tiles::T256 ? std::ceil(r) : r < 4 ? std::ceil(2 * r) / 2 : r + 0.25;
+    double rounds = r <= 1 ? 1.0 : c.deep ? std::ceil(r - 0.1) : c.tiles == Tiles::T256 ? std::ceil(r) : r < 4 ? std::ceil(2 * r) / 2 : r + 0.25;
     if (c.tiles == Tiles::T256 && r > 1 && rest > 0) rounds = std::floor(r) + (rest <= 0.25 ? 0.55 : rest <= 0.5 ? 0.7 : 1.0);
-    return rounds * (steps * (alone + (full - alone) * std::min(1.0, r)) + besides);
+    double crowd = std::min(1.0, r);                     // half of it the chip's, half from where tiles share a CU
+    if (places > 1) crowd = 0.5 * crowd + 0.5 * std::max(0.0, std::min(1.0, (r * places - 1) / (places - 1)));
+    return rounds * (steps * (alone + (full - alone) * crowd) + besides);
 }
 // small: only T64 is to be had, deep or not
 template <int MODE, bool GLU>
@@ -932,8 +937,11 @@ Choice choose_tiles(const LinearParams& p, bool bf16, bool small = false, bool s
     Choice best{Tiles::T64, false, 1e30};
     auto offer = [&](Tiles kind, bool deep, int BM, int BN) {
         const double n = tiles(BM, BN);
-        if (deep && (k_tiles < 8 || n > 4.0 * cu_count())) return;           // (one tile to a workgroup)
-        const double us = estimate_us({kind, deep, 0}, n, k_tiles, kind == Tiles::THIN ? BN > 16 : BN == 128, MODE != FORWARD, bf16);
+        if (deep && ((k_tiles < 8 && kind != Tiles::THIN) || n > 4.0 * cu_count())) return;           // (one tile to a workgroup)
+        double us = estimate_us({kind, deep, 0}, n, k_tiles, kind == Tiles::THIN ? BN > 16 : BN == 128, MODE != FORWARD, bf16);
+        // dx in bf16 by THIN reads the weights, 128 bytes of a row at a time, at 3.5 TB/s at most; ROWS32 at 5.5 (64 experts of 512 x 6784, 907
+        // rows: 105 and 81 us)
+        if (MODE == INPUT && bf16 && kind == Tiles::THIN) us = std::max(us, groups * p.N * halves * p.K * 2 / 3.5e6);
         if (us < best.us) best = {kind, deep, us};
     };
     const int columns32 = GLU || MODE == INPUT ? 128 : 64;
@@ -1033,15 +1041,18 @@ hipError_t launch_expert_linear_backward(const etr_linear_config& c, const void*
     q.M = c.N; q.N = c.K; q.K = c.rows; q.lda = c.N; q.ldb = c.K;
     if (dx && dw) {
         const Choice ci = choose_tiles<INPUT, false>(p, bf16), cw = choose_tiles<WEIGHT, false>(q, bf16);
-        // one launch, unless dx in it takes longer than dx by tiles of its own and dw behind it.  fp32, together and apart: 500 rows, 512 x 512
-        // 14.0 and 19.9 us; 2500 in 8 groups, 1048 x 520 92.0 and 97.4; 18 rows, 3840 x 1472 87.9 and 37.6
-        if (cw.tiles == Tiles::T64) {
-            const double apart = ci.us + cw.us;
-            if (tiles_at_most(q, WEIGHT, 64, 64) <= cu_count() && choose_tiles<INPUT, false>(p, bf16, true, true).us <= apart)
-                return bf16 ? launch_small_backward<true, 2, 4>(p, q, st) : launch_small_backward<false, 2, 4>(p, q, st);
-            if (choose_tiles<INPUT, false>(p, bf16, true).us <= apart)
-                return bf16 ? launch_small_backward<true, 4, 1>(p, q, st) : launch_small_backward<false, 2, 1>(p, q, st);
-        }
+        // both in one launch of 64 x 64 tiles, unless each by its own takes less: the longer of the two while they fit on the chip together, else
+        // their sum less what a launch costs.  Together and apart: 500 rows, 512 x 512 in fp32 14.0 and 19.9 us; 2500 in 8 groups, 1048 x 520 in fp32
+        // 92.0 and 97.4; 112 in 4, 384 x 1664 21.4 and 25.3 (with the forward); 18 rows, 3840 x 1472 in fp32 87.9 and 37.6
+        const double apart = ci.us + cw.us, weight_us = choose_tiles<WEIGHT, false>(q, bf16, true).us;
+        const long long tiles = tiles_at_most(p, INPUT, 64, 64) + tiles_at_most(q, WEIGHT, 64, 64);
+        auto together = [&](bool deep) {
+            const double input_us = choose_tiles<INPUT, false>(p, bf16, true, deep).us;
+            return tiles <= (deep ? 1 : 2) * cu_count() ? std::max(input_us, weight_us) : input_us + weight_us - 3.0;
+        };
+        if (tiles_at_most(q, WEIGHT, 64, 64) <= cu_count() && together(true) <= apart)
+            return bf16 ? launch_small_backward<true, 2, 4>(p, q, st) : launch_small_backward<false, 2, 4>(p, q, st);
+        if (together(false) <= apart) return bf16 ? launch_small_backward<true, 4, 1>(p, q, st) : launch_small_backward<false, 2, 1>(p, q, st);
     }
     if (dx && (err = launch_product<INPUT, false>(p, bf16, st)) != hipSuccess) return err;
     return dw ? launch_product<WEIGHT, false>(q, bf16, st) : hipSuccess;
