@@ -132,7 +132,8 @@ __device__ __forceinline__ bool find_tile(const LinearParams& p, const Groups& g
 __device__ __forceinline__ float sigmoid(float a) { return __builtin_amdgcn_rcpf(1.0f + __expf(-a)); }
 // The normal distribution function: Phi(-|a|) = u Q(u) exp(-a^2 / 2), u = 1 / (1 + 0.297 |a|) (1 + 0.42 x for x = |a| / sqrt 2), Q of degree 7
 // fitted to the least relative error over |a| <= 13.4 (1.7e-7; with fp32's roundings 7.6e-7 up to 3 and 2.7e-6 up to 5, from the exponent's
-// argument).  12825 rows, 192 x 7744 in bf16 108 us; with a fit of erfc's logarithm of degree 9 (1.2e-7) 120.  No branch, where erff has two and keeps every value of a tile alive across them (789 spilled registers).
+// argument).  12825 rows, 192 x 7744 in bf16: 108 us; with a fit of erfc's logarithm of degree 9 (1.2e-7) 120.  No branch, where erff has two and
+// keeps every value of a tile alive across them (789 spilled registers).
 __device__ __forceinline__ float normal_cdf(float a) {
     const float u = __builtin_amdgcn_rcpf(fmaf(0.29698485f, fabsf(a), 1.0f)), x = a * 0.84932180f;         // x^2 = a^2 / 2 log2 e
     float s = fmaf(0.0351077948f, u, -0.160095614f);
