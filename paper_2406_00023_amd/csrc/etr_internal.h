@@ -177,6 +177,11 @@ hipError_t ensure_dynamic_lds(const void* kernel, size_t bytes);
 // 64 x 64 / 32 x 32 tiles.
 extern "C" int etr_ffn_plan(const etr_config* c, int product, int gathered, long long* workgroups);
 
+// Likewise the tiles of a product on sorted rows (0 forward, 1 dx and 2 dw where each has a launch of its own): 0 of 16 rows, 1 of 32,
+// 2 / 3 / 4 of 64 / 128 / 256, and 8 more where groups of waves share a tile's contraction.  3: whether dx and dw, both asked for, go
+// in one launch of 64-row tiles: 0 no, 1 yes, 2 with shared contractions.
+extern "C" int etr_linear_plan(const etr_linear_config* c, int product);
+
 // ---- device helpers -----------------------------------------------------------
 // Inclusive prefix sum over the 64 lanes of a wave, lane 0 first, by data-parallel-primitive moves: shifts by
 // 1, 2, 4, 8 inside each row of 16 lanes (a lane whose source lies outside its row adds nothing), then lane 15 of

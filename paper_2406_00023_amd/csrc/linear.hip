@@ -891,9 +891,9 @@ struct Choice { Tiles tiles; bool deep; double us; };
 // Few rows, THIN and the best of the others: 18 rows, 3840 x 1472 6.0 and 12.0 us, fp32 9.8 and 39.2; 64 rows, 4096 x 4096 24.9 and 12.7, fp32
 // 38.4 and 41.6; dx of 64 rows, 8192 x 256 16.2 and 27.8, fp32 50 and 143.
 // 2048 rows in 16 groups, 2048 x 2048: T256 46, T128 33, T64 40 us; 4096 rows: 48, 57, 68; 512 rows dense, 4096 x 4096: 61, 43, 29.
-// fp32, per 32-deep k-tile, where the CU's matrix pipes set the time as soon as two 64 x 64 tiles share it: T128 2.0 or 2.1 per tile on the
-// CU and 2.4 for its epilogue, T64 0.7 or 0.47 and 0.5, ROWS32 0.45 or 0.25 and 0.4 (of 128 columns: T64's); deep: a quarter of the k-tiles, 4.5
-// times the work in each.
+// fp32, per 32-deep k-tile, where the CU's matrix pipes set the time as soon as two 64 x 64 tiles share it: T64 0.7 alone or 0.47 per tile on the
+// CU, and 0.5 for its epilogue, ROWS32 0.45 or 0.25 and 0.4 (of 128 columns: T64's); deep: a quarter of the k-tiles, 4.5 times the work in
+// each.  (A tile of 128 x 128: 2.1 and 2.4, more than the four 64 x 64 tiles in its place, and 2.0 alone: not built.)
 double estimate_us(Choice c, double tiles, double k_tiles, bool wide, bool transposed, bool bf16) {
     const double cus = cu_count();
     if (c.tiles == Tiles::THIN) {
@@ -903,8 +903,7 @@ double estimate_us(Choice c, double tiles, double k_tiles, bool wide, bool trans
     const double steps = c.deep ? std::ceil(k_tiles / 4) : k_tiles;
     if (!bf16) {
         const bool t64 = c.tiles == Tiles::T64 || wide;
-        const double alone = c.tiles == Tiles::T128 ? 2.0 : t64 ? 0.7 : 0.45, each = c.tiles == Tiles::T128 ? 2.1 : t64 ? 0.47 : 0.25;
-        const double epilogue = c.tiles == Tiles::T128 ? 2.4 : t64 ? 0.5 : 0.4;
+        const double alone = t64 ? 0.7 : 0.45, each = t64 ? 0.47 : 0.25, epilogue = t64 ? 0.5 : 0.4;
         return std::max(steps * (c.deep ? 1.7 * alone : alone), std::max(1.0, tiles / cus) * (steps * each * (c.deep ? 4.5 : 1.0) + epilogue)) + (c.deep ? 5.0 : 4.0);
     }
     double places = 2, alone = 0, full = 0, besides = 0;
@@ -950,8 +949,10 @@ Choice choose_tiles(const LinearParams& p, bool bf16, bool small = false, bool s
         offer(Tiles::T64, small_deep, 64, 64);
         return best;
     }
-    if (bf16) offer(Tiles::T256, false, 256, 256);
-    offer(Tiles::T128, false, 128, 128);
+    if (bf16) {
+        offer(Tiles::T256, false, 256, 256);
+        offer(Tiles::T128, false, 128, 128);
+    }
     offer(Tiles::T64, false, 64, 64);
     offer(Tiles::T64, true, 64, 64);
     if (MODE != WEIGHT && rows_each <= 256) {
@@ -978,13 +979,46 @@ hipError_t launch_typed(const LinearParams& p, hipStream_t st) {
     }
     if constexpr (BF16) {
         if (c.tiles == Tiles::T256) return launch_tiles<true, 256, 256, 2, 4, 2, 1, MODE, GLU>(p, st);
+        if (c.tiles == Tiles::T128) return launch_tiles<true, 128, 128, 2, 2, 2, 1, MODE, GLU>(p, st);
     }
-    if (c.tiles == Tiles::T128) return launch_tiles<BF16, 128, 128, 2, 2, 2, 1, MODE, GLU>(p, st);
     return c.deep ? launch_tiles<BF16, 64, 64, 2, 2, 2, 4, MODE, GLU>(p, st) : launch_tiles<BF16, 64, 64, 2, 2, BF16 ? 4 : 2, 1, MODE, GLU>(p, st);
 }
 template <int MODE, bool GLU>
 hipError_t launch_product(const LinearParams& p, bool bf16, hipStream_t st) {
     return bf16 ? launch_typed<true, MODE, GLU>(p, st) : launch_typed<false, MODE, GLU>(p, st);
+}
+
+// dx and dw in one launch of 64 x 64 tiles, unless each by its own takes less: the longer of the two while they fit on the chip together, else
+// their sum less what a launch costs.  Together and apart: 500 rows, 512 x 512 in fp32 14.0 and 19.9 us; 2500 in 8 groups, 1048 x 520 in fp32
+// 92.0 and 97.4; 112 in 4, 384 x 1664 21.4 and 25.3 (with the forward); 18 rows, 3840 x 1472 in fp32 87.9 and 37.6
+enum class Joint { NONE, PLAIN, DEEP };
+Joint choose_joint(const LinearParams& p, const LinearParams& q, bool bf16) {
+    const Choice ci = choose_tiles<INPUT, false>(p, bf16), cw = choose_tiles<WEIGHT, false>(q, bf16);
+    const double apart = ci.us + cw.us, weight_us = choose_tiles<WEIGHT, false>(q, bf16, true).us;
+    const long long tiles = tiles_at_most(p, INPUT, 64, 64) + tiles_at_most(q, WEIGHT, 64, 64);
+    auto together = [&](bool deep) {
+        const double input_us = choose_tiles<INPUT, false>(p, bf16, true, deep).us;
+        return tiles <= (deep ? 1 : 2) * cu_count() ? std::max(input_us, weight_us) : input_us + weight_us - 3.0;
+    };
+    if (tiles_at_most(q, WEIGHT, 64, 64) <= cu_count() && together(true) <= apart) return Joint::DEEP;
+    return together(false) <= apart ? Joint::PLAIN : Joint::NONE;
+}
+
+// sizes of the three products
+LinearParams forward_sizes(const etr_linear_config& c) {
+    LinearParams p{};
+    p.rows = c.rows; p.E = c.E; p.N = c.N; p.K = c.K; p.lda = p.ldb = c.K; p.act = c.act; p.glu = c.act == ETR_ACT_SWIGLU;
+    return p;
+}
+LinearParams input_sizes(const etr_linear_config& c) {
+    LinearParams p{};
+    p.rows = c.rows; p.E = c.E; p.N = c.K; p.K = c.N; p.lda = c.N; p.ldb = c.K; p.glu = c.act == ETR_ACT_SWIGLU;
+    return p;
+}
+LinearParams weight_sizes(const etr_linear_config& c) {
+    LinearParams p{};
+    p.rows = c.rows; p.E = c.E; p.M = c.N; p.N = c.K; p.K = c.rows; p.lda = c.N; p.ldb = c.K; p.glu = c.act == ETR_ACT_SWIGLU;
+    return p;
 }
 
 int chunks_at_most(const etr_linear_config& c) { return c.rows / kChunk + std::min(c.E, c.rows); }
@@ -1001,10 +1035,9 @@ size_t linear_ws_bytes(const etr_linear_config& c) {
 
 hipError_t launch_expert_linear(const etr_linear_config& c, const void* x, const int32_t* offsets, const void* w, const void* w_up, const float* bias,
                                 const float* bias_up, const void* residual, void* y, void* pre, void* pre_up, hipStream_t st) {
-    LinearParams p{};
+    LinearParams p = forward_sizes(c);
     p.A[0] = x; p.B[0] = w; p.B[1] = w_up; p.C[0] = y;
     p.offsets = offsets; p.bias[0] = bias; p.bias[1] = bias_up; p.residual = residual; p.pre[0] = pre; p.pre[1] = pre_up;
-    p.rows = c.rows; p.E = c.E; p.N = c.N; p.K = c.K; p.lda = p.ldb = c.K; p.act = c.act; p.glu = c.act == ETR_ACT_SWIGLU;
     return p.glu ? launch_product<FORWARD, true>(p, c.dtype == ETR_BF16, st) : launch_product<FORWARD, false>(p, c.dtype == ETR_BF16, st);
 }
 
@@ -1032,31 +1065,29 @@ hipError_t launch_expert_linear_backward(const etr_linear_config& c, const void*
         hipLaunchKernelGGL(linear_bias_kernel, dim3((c.N + 63) / 64, c.E, glu ? 2 : 1), dim3(1024), 0, st, m, dbias, dbias_up);
         if ((err = hipGetLastError()) != hipSuccess) return err;
     }
-    LinearParams p{};
-    p.offsets = offsets; p.rows = c.rows; p.E = c.E; p.glu = glu;
-    p.A[0] = da ? da : dy; p.A[1] = db;
-    LinearParams q = p;
+    LinearParams p = input_sizes(c), q = weight_sizes(c);
+    p.offsets = q.offsets = offsets;
+    p.A[0] = q.A[0] = da ? da : dy; p.A[1] = q.A[1] = db;
     p.B[0] = w; p.B[1] = w_up; p.C[0] = dx;
-    p.N = c.K; p.K = c.N; p.lda = c.N; p.ldb = c.K;
     q.B[0] = x; q.C[0] = dw; q.C[1] = dw_up;
-    q.M = c.N; q.N = c.K; q.K = c.rows; q.lda = c.N; q.ldb = c.K;
     if (dx && dw) {
-        const Choice ci = choose_tiles<INPUT, false>(p, bf16), cw = choose_tiles<WEIGHT, false>(q, bf16);
-        // both in one launch of 64 x 64 tiles, unless each by its own takes less: the longer of the two while they fit on the chip together, else
-        // their sum less what a launch costs.  Together and apart: 500 rows, 512 x 512 in fp32 14.0 and 19.9 us; 2500 in 8 groups, 1048 x 520 in fp32
-        // 92.0 and 97.4; 112 in 4, 384 x 1664 21.4 and 25.3 (with the forward); 18 rows, 3840 x 1472 in fp32 87.9 and 37.6
-        const double apart = ci.us + cw.us, weight_us = choose_tiles<WEIGHT, false>(q, bf16, true).us;
-        const long long tiles = tiles_at_most(p, INPUT, 64, 64) + tiles_at_most(q, WEIGHT, 64, 64);
-        auto together = [&](bool deep) {
-            const double input_us = choose_tiles<INPUT, false>(p, bf16, true, deep).us;
-            return tiles <= (deep ? 1 : 2) * cu_count() ? std::max(input_us, weight_us) : input_us + weight_us - 3.0;
-        };
-        if (tiles_at_most(q, WEIGHT, 64, 64) <= cu_count() && together(true) <= apart)
-            return bf16 ? launch_small_backward<true, 2, 4>(p, q, st) : launch_small_backward<false, 2, 4>(p, q, st);
-        if (together(false) <= apart) return bf16 ? launch_small_backward<true, 4, 1>(p, q, st) : launch_small_backward<false, 2, 1>(p, q, st);
+        const Joint joint = choose_joint(p, q, bf16);
+        if (joint == Joint::DEEP) return bf16 ? launch_small_backward<true, 2, 4>(p, q, st) : launch_small_backward<false, 2, 4>(p, q, st);
+        if (joint == Joint::PLAIN) return bf16 ? launch_small_backward<true, 4, 1>(p, q, st) : launch_small_backward<false, 2, 1>(p, q, st);
     }
     if (dx && (err = launch_product<INPUT, false>(p, bf16, st)) != hipSuccess) return err;
     return dw ? launch_product<WEIGHT, false>(q, bf16, st) : hipSuccess;
 }
 
 }  // namespace etr
+
+extern "C" int etr_linear_plan(const etr_linear_config* c, int product) {
+    using namespace etr;
+    const bool bf16 = c->dtype == ETR_BF16;
+    auto form = [](Choice t) { return static_cast<int>(t.tiles) + (t.deep ? 8 : 0); };
+    const LinearParams p = forward_sizes(*c), i = input_sizes(*c), w = weight_sizes(*c);
+    if (product == 0) return form(p.glu ? choose_tiles<FORWARD, true>(p, bf16) : choose_tiles<FORWARD, false>(p, bf16));
+    if (product == 1) return form(choose_tiles<INPUT, false>(i, bf16));
+    if (product == 2) return form(choose_tiles<WEIGHT, false>(w, bf16));
+    return static_cast<int>(choose_joint(i, w, bf16));
+}
