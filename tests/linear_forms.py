@@ -38,9 +38,15 @@ CASES = {
     (JOINT, "f32", "swiglu"): {"apart": (268, 2, 232, 344), "64": (577, 4, 392, 136), "64+": (264, 2, 224, 136)},
 }
 
+# more tiles of 256 rows than a chip of 256 CUs has places: workgroups go from tile to tile, and a last round goes whole, in halves or in quarters
+WALKS = [(FORWARD, "bf16", "none", "256", 3303, 3, 200, 6152), (FORWARD, "bf16", "swiglu", "256", 3303, 3, 200, 2568),
+         (INPUT, "bf16", "none", "256", 2603, 3, 5896, 200), (INPUT, "bf16", "swiglu", "256", 2603, 3, 6664, 136),
+         (WEIGHT, "bf16", "none", "256", 700, 4, 2056, 2056), (WEIGHT, "bf16", "swiglu", "256", 700, 4, 2056, 2056)]
+
 
 def listed(*products):
-    return [(p, dtype, act, form, *shape) for (p, dtype, act), forms in CASES.items() if p in products for form, shape in forms.items()]
+    cases = [(p, dtype, act, form, *shape) for (p, dtype, act), forms in CASES.items() for form, shape in forms.items()]
+    return [c for c in cases + WALKS if c[0] in products]
 
 
 def plan(product, dtype, act, rows, E, K, N):
