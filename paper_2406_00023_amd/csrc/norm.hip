@@ -254,7 +254,7 @@ int pieces_of(const etr_norm_config& c) { return static_cast<int>(static_cast<si
 // that the partial sums stay small beside the rows.
 int backward_groups(const etr_norm_config& c) {
     const int most = 256 * 4;
-    const int groups = (c.T + 3) / 4;
+    const int groups = c.T / 4 + (c.T % 4 != 0);         // (T + 3 may not fit 32 bits)
     return groups < most ? groups : most;
 }
 
