@@ -372,7 +372,9 @@ typedef enum { ETR_ACT_NONE = 0, ETR_ACT_SILU = 1, ETR_ACT_GELU = 2, ETR_ACT_SWI
  * fp32 accumulation, one rounding to dtype.  E = 1 with offsets = NULL is a dense product of all rows. */
 typedef struct {
     int32_t rows;           /* rows of x and y (T * k of the sort); offsets[E] <= rows of them belong to an expert */
-    int32_t K, N, E;        /* K % 8 == 0, N % 8 == 0, both <= 2^20; E <= 64; rows <= 2^28 */
+    int32_t K, N, E;        /* K % 8 == 0, N % 8 == 0, both <= 2^20; E <= 64; rows <= 2^28; tiles are counted in 32 bits: with
+                               w = ceil(max(K, N) / 32), w (rows / 32 + E) <= 2^30 and w^2 E <= 2^30 (for every call, forward ones
+                               too); ETR_ERR_UNSUPPORTED past any of them */
     int32_t dtype;          /* etr_dtype of x, w, residual, y, pre and their gradients */
     int32_t act;            /* etr_act */
 } etr_linear_config;
