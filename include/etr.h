@@ -407,6 +407,8 @@ etr_status etr_expert_linear_backward(const etr_linear_config* cfg, const void* 
  *   dscore = gate .* (dgate - <dgate, gate>);   dx[t] = dx_add[t] + sum_e dscore[t][e] d score[t][e] / d x[t]
  *   x [T][d], w_emb [E][d/D], score, gate [T][E]: of the forward call; dx_add [T][d] dtype in, optional (zero): the gradient
  *   that reaches x by the other ways; dx [T][d] dtype out; may be dx_add.  A zero-norm token gets dx_add.
+ * The embeddings w_emb are held fixed, as in etr_moe_backward: they get no gradient.  (dscore, of which a caller that trains them makes
+ * it, is the first line, of what the caller has.)
  * E * (d/D) * 4 bytes must fit in 120 KiB (ETR_ERR_UNSUPPORTED). */
 etr_status etr_route_backward(const etr_config* cfg, const void* x, const float* w_emb, const float* score,
                               const float* gate, const float* dgate, const void* dx_add, void* dx, void* stream);

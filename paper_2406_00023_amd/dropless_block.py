@@ -83,7 +83,8 @@ class DroplessBlock:
         return self.x_out, self.h_next
 
     def backward(self, x, w_emb, w, dx_out, dh_next):
-        """Gradients of the last forward call: returns dx; the weights' are in `grads`."""
+        """Gradients of the last forward call: returns dx; those of the tensors of WEIGHTS are in `grads`.  The experts' embeddings w_emb are constants
+        of the method and get none."""
         g = self.grads
         B.etr_block_norm_backward(self.norm, self.x_out, self.y, None, w["w_post"], w["w_next"], dx_out, dh_next, self.dx, self.dy, None,
                                   g["w_post"], g["w_next"], self.ws)
