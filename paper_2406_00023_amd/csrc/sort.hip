@@ -187,21 +187,27 @@ __device__ __forceinline__ int lane_row(const int32_t* row_of, size_t t, int k, 
     const int r = lane < k ? row_of[t * k + lane] : -1;
     return r < rows ? r : -1;
 }
-// v over a token's sum of weights, 0 without one.  (A division: the inverse of a sum below 2^-128 would be infinite.)
-__device__ __forceinline__ float over_sum(float v, float sum) { return sum > 0.f ? v / sum : v * 0.f; }
-// Lane j < k: weight of the token's j-th pair (0 if not in use); with `norm` divided by the token's sum, which is handed back
+// The inverse of a token's sum of weights, 0 without one, in two factors: that of a sum below 2^-128 is no fp32 number.
+struct Inverse {
+    float lift = 1.0f, value = 1.0f;
+    __device__ __forceinline__ void set(float sum) {
+        lift = sum < 0x1p-100f ? 0x1p100f : 1.0f;
+        value = sum > 0.f ? 1.0f / (sum * lift) : 0.f;
+    }
+    __device__ __forceinline__ float of(float v) const { return v * lift * value; }
+};
+// Lane j < k: weight of the token's j-th pair (0 if not in use); with `norm` divided by the token's sum, whose inverse is handed back
 __device__ __forceinline__ float lane_weight(const float* gate, const int32_t* topk, size_t t, int k, int E, int row, int norm, int lane,
-                                             int& expert, float& sum) {
+                                             int& expert, Inverse& inverse) {
     expert = -1;
     float w = 0.f;
     if (row >= 0) {                                          // (only in lanes below k)
         expert = topk[t * k + lane];
         if (expert >= 0 && expert < E) w = gate[t * E + expert];
     }
-    sum = 1.0f;
     if (norm) {
-        sum = wave_sum(w);
-        w = over_sum(w, sum);
+        inverse.set(wave_sum(w));
+        w = inverse.of(w);
     }
     return w;
 }
@@ -243,9 +249,10 @@ __global__ __launch_bounds__(kRowsThreads) void gather_sum_kernel(RowsParams p) 
         const long long t = unit / p.segments;
         const int c0 = static_cast<int>(unit - t * p.segments) * kSegment * kWave + lane;
         const int mine = lane_row(p.row_of, t, p.k, p.rows, lane);
-        float weight = 1.0f, sum;
+        float weight = 1.0f;
         int expert;
-        if constexpr (WEIGHTED) weight = lane_weight(p.gate, p.topk, t, p.k, p.E, mine, p.gate_norm, lane, expert, sum);
+        Inverse inverse;
+        if constexpr (WEIGHTED) weight = lane_weight(p.gate, p.topk, t, p.k, p.E, mine, p.gate_norm, lane, expert, inverse);
         float acc[kSegment][V];
 #pragma unroll
         for (int u = 0; u < kSegment; ++u)
@@ -314,8 +321,8 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void unsort_backward_kerne
         int j = left ? __builtin_ctzll(left) : -1;
         if (j >= 0) request(j);
         int expert;
-        float sum;
-        const float weight = lane_weight(p.gate, p.topk, t, p.k, p.E, mine, p.gate_norm, lane, expert, sum);
+        Inverse inverse;
+        const float weight = lane_weight(p.gate, p.topk, t, p.k, p.E, mine, p.gate_norm, lane, expert, inverse);
         float dweight = 0.f;                                     // lane j: <dout[t], ys[row_tj]>
         while (j >= 0) {
             left &= left - 1;
@@ -348,7 +355,7 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void unsort_backward_kerne
         if (TEAM > 64 && threadIdx.x >= 64) continue;            // the first wave has all that is left to do
         if (p.gate_norm) {                                       // w = g / S: d / d g_j = (dw_j - sum_i dw_i w_i) / S
             const float mix = wave_sum(dweight * weight);
-            dweight = over_sum(dweight - mix, sum);
+            dweight = inverse.of(dweight - mix);
         }
         float dg = 0.f;                                          // lane e
         for (uint64_t m = __ballot(mine >= 0 && expert >= 0); m; m &= m - 1) {
