@@ -5,8 +5,9 @@
 // and dx_add joined to it.  Bound by memory (two rows in, one out), so a wave holds its token's row in registers between
 // its norm and its use; the embeddings, divided by their norms, lie in LDS for all waves of a workgroup, and u passes through
 // LDS from the lanes that have the groups to those that have their 16-byte pieces.  Measured: 65536 x 4096 bf16, 64 experts of 64 pooled
-// features 319 us (5.2 TB/s); 213 x 5120 fp32, 64 experts of 80, whose rows come twice, 21 us (element by element 58); 512 x 256 fp32, 8
-// experts, 3.2 us.
+// features 319 us (5.2 TB/s), pooled 329; 32768 x 2048 fp32, 32 experts of 64, 155 and pooled 162 (5.2); 213 x 5120 fp32, 64 experts of 80, whose
+// rows come twice, 21 us (element by element 58); 512 x 256 fp32, 8 experts, 3.2 us.  Element by element: 32768 x 1536 bf16 in groups of 12, 208
+// us for 63 of bytes, pooled in groups of 24 434.
 #include <algorithm>
 #include <cmath>
 
