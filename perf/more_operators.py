@@ -1,0 +1,537 @@
+"""The experts in 8 bits, as cases that can be timed and compared: packing, products of packed operands, and the backward
+from packed activations.
+
+A packed matrix holds e4m3 values (sign, 4 bits of exponent, 3 of mantissa, largest 448) and a power of two for each block of
+128 values along the contraction.  A case is one pass through the public entry points of the binding, of one of these kinds (`op`):
+
+  pack     rows into a packed matrix and back to the values that it stands for: tokens through the tables of the rows sorted by
+           expert (etr_pack_sorted_rows), or stacked weights, along both of their directions (etr_pack_rows, etr_pack_columns);
+           etr_unpack_rows
+  linear   etr_expert_linear8: the experts' products of packed rows and packed weights, with bias, activation and residual; with
+           `keep` the result and the pre-activations are kept packed, as a training forward does
+  backward etr_act_backward8: the pre-activations' gradient from the packed pre-activations, packed along rows and along columns;
+           etr_expert_linear8 for dx; etr_repack_columns of the packed rows and etr_weight_gradient8 for dw
+
+The sizes are those of the workloads of `paper_2406_00023_amd.inputs`, decode batches on the same layers, and generic
+ragged ones.  The plain forms are elementary torch operations in 32 bits, rounded to the output's type once.
+"""
+from __future__ import annotations
+
+import math
+import random
+
+import torch
+
+own = False
+
+DEV = "cuda:0"
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+SIZES = {"f32": 4, "bf16": 2}
+ACTS = {"none": 0, "silu": 1, "gelu": 2, "swiglu": 3}
+BLOCK = 128                                                    # values that share a scale
+
+
+def _pack_case(name, dtype, *, T=0, d=0, E=1, k=0, N=0, used=1.0):
+    """k > 0: T tokens of d values, k rows each; else E weight matrices [N][d], packed along both directions.  used: the share of
+    the pairs that a selection has kept."""
+    return {"name": name, "op": "pack", "dtype": dtype, "T": T, "d": d, "E": E, "k": k, "N": N, "used": used}
+
+
+def _linear(name, rows, E, K, N, dtype, act, *, keep=False, bias=False, residual=False, used=1.0, skew=0.3):
+    """used: the share of the rows that belong to an expert at all; skew: spread of the experts' popularity."""
+    return {"name": name, "op": "linear", "rows": rows, "E": E, "K": K, "N": N, "dtype": dtype, "act": act, "keep": keep, "bias": bias,
+            "residual": residual, "used": used, "skew": skew}
+
+
+def _backward(name, rows, E, K, N, dtype, act, *, bias=False, used=1.0, skew=0.3):
+    return {"name": name, "op": "backward", "rows": rows, "E": E, "K": K, "N": N, "dtype": dtype, "act": act, "bias": bias, "used": used,
+            "skew": skew}
+
+
+def listed():
+    return [
+        # a decode step of 32 sequences, top-2 of 16: bound by the launches
+        _pack_case("pack_decode", "bf16", T=32, d=2048, E=16, k=2),
+        # the rows of a training step of the 32-expert workload, packed once per token and kept as checkpoints
+        _pack_case("pack_train", "bf16", T=32768, d=4096, E=32, k=2),
+        # the gate weights of the 16-expert workload after an optimizer's step: for the forward products and for the input's gradient
+        _pack_case("pack_weights", "bf16", E=16, N=5632, d=2048),
+        # what a capacity has left of a ragged batch, in the type that gradients are checked in
+        _pack_case("pack_f32_ragged", "f32", T=3001, d=1080, E=12, k=3, used=0.85),
+        # the gate and up products of a decode step: every expert's weights for a few rows
+        _linear("linear_decode", 64, 16, 2048, 5632, "bf16", "swiglu"),
+        # the same products for 8192 tokens, top-2: a prompt or an evaluation pass
+        _linear("linear_prompt", 16384, 16, 2048, 5632, "bf16", "swiglu"),
+        # a training forward of the 8 experts with H = 1408: what the next product and the backward need is kept in 8 bits
+        _linear("linear_keep", 32768, 8, 4096, 1408, "bf16", "swiglu", keep=True),
+        # a small layer with everything in the epilogue and rows that belong to nobody
+        _linear("linear_f32_ragged", 2501, 8, 520, 1048, "f32", "gelu", bias=True, residual=True, used=0.9),
+        # a fine-tuning step of a few tokens on 4 experts
+        _backward("backward_small", 96, 4, 1024, 1408, "bf16", "swiglu"),
+        # the gate and up products of a training step of 8192 tokens, top-2
+        _backward("backward_train", 16384, 16, 2048, 5632, "bf16", "swiglu"),
+        # the products of a small layer without an activation, with the biases' gradient
+        _backward("backward_f32_ragged", 2501, 8, 520, 1048, "f32", "none", bias=True, used=0.9),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def _width(rng):
+    w = _log_int(rng, 128, 8192) // 8 * 8
+    return max(128, w // 64 * 64) if rng.random() < 0.6 else w
+
+
+def draw(rng: random.Random):
+    """A case of the same ranges: from one row to 65536, widths up to 8192, up to 64 experts, both types, both directions."""
+    while True:
+        op = rng.choice(["pack", "pack", "linear", "linear", "linear", "backward", "backward"])
+        dtype = "f32" if rng.random() < 0.3 else "bf16"
+        E = rng.choice([1, 4, 8, 12, 16, 32, 64])
+        used = rng.choice([1.0, 1.0, 0.8])
+        if op == "pack":
+            if rng.random() < 0.4:
+                c = _pack_case("", dtype, E=E, N=_width(rng), d=_width(rng))
+                if E * c["N"] * c["d"] > 16 * 5632 * 2048:
+                    continue
+            else:
+                k = rng.randint(1, min(E, 8))
+                c = _pack_case("", dtype, T=_log_int(rng, 1, 65536), d=_width(rng), E=E, k=k, used=used)
+                if c["T"] * (k + 1) * c["d"] * SIZES[dtype] > 32768 * 3 * 4096 * 2:
+                    continue
+        else:
+            rows, K, N = _log_int(rng, 1, 32768), _width(rng), _width(rng)
+            act, bias = rng.choice(list(ACTS)), rng.random() < 0.6
+            if op == "linear":
+                # (packed results of 32-bit values say what bf16 ones do: they are kept in training, which is in bf16)
+                c = _linear("", rows, E, K, N, dtype, act, keep=dtype == "bf16" and rng.random() < 0.4, bias=bias, residual=rng.random() < 0.3,
+                            used=used, skew=rng.uniform(0.0, 0.6))
+            else:
+                c = _backward("", rows, E, K, N, dtype, "none" if dtype == "f32" else act, bias=bias, used=used, skew=rng.uniform(0.0, 0.6))
+            if E * K * N > 2e8 or work(c)["flops"] > 1.5e12:
+                continue
+        del c["name"]
+        return c
+
+
+# ---- packed matrices in plain torch ---------------------------------------------------------------------------------
+
+def _blocks(n):
+    return -(-n // BLOCK)
+
+
+def _round8(v):
+    """v [..., whole blocks]: the nearest e4m3 values (bytes) after division by a power of two for each block, and that power's
+    exponent + 127.  The power is the smallest that leaves no finite value over 448."""
+    v = v.reshape(*v.shape[:-1], -1, BLOCK)
+    top = torch.where(torch.isfinite(v), v.abs(), 0.0).amax(-1)
+    bits = top.view(torch.int32)
+    power = ((bits >> 23) - 8 + ((bits & 0x7FFFFF) > 0x600000).int()).clamp(min=0)
+    inverse = ((254 - power) << 23).view(torch.float32)                                    # a power of two: the division is exact
+    q = (v * inverse[..., None]).to(torch.float8_e4m3fn).view(torch.uint8)
+    return q.flatten(-2), power.to(torch.uint8)
+
+
+def _pack(x):
+    """x [..., rows, K] float32: values [..., rows, whole blocks] and scales [..., blocks / 4, rows, 4], both bytes."""
+    K = x.shape[-1]
+    q, power = _round8(torch.nn.functional.pad(x, (0, _blocks(K) * BLOCK - K)))
+    power = torch.nn.functional.pad(power, (0, -power.shape[-1] % 4), value=127)
+    return q.contiguous(), power.reshape(*power.shape[:-1], -1, 4).transpose(-3, -2).contiguous()
+
+
+def _values(q, power):
+    """What bytes [..., blocks * 128] and exponents [..., blocks] stand for."""
+    scale = torch.where(power == 0, 2.0 ** -127, (power.int() << 23).view(torch.float32))
+    v = q.view(torch.float8_e4m3fn).float().reshape(*power.shape, BLOCK) * scale[..., None]
+    return v.flatten(-2)
+
+
+def _unpack(packed, K):
+    q, s = packed
+    power = s.transpose(-3, -2).flatten(-2)[..., : q.shape[-1] // BLOCK]
+    return _values(q, power)[..., :K]
+
+
+# ---- inputs -----------------------------------------------------------------------------------------------------
+
+def _generator(case, seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed((int(seed) * 1000003 + 29) % (1 << 62))
+    return g
+
+
+def _normal(g, shape, dtype=torch.float32, std=1.0):
+    return torch.randn(shape, generator=g, device=DEV, dtype=torch.float32).mul_(std).to(dtype)
+
+
+def _packed_buffers(rows, K):
+    """Values and scales of a packed matrix that a call fills."""
+    return (torch.zeros(rows, _blocks(K) * BLOCK, dtype=torch.uint8, device=DEV),
+            torch.zeros(-(-K // (4 * BLOCK)), rows, 4, dtype=torch.uint8, device=DEV))
+
+
+def _prepare_pack(case, seed):
+    g, dt, T, d, E, k, N = _generator(case, seed), DTYPES[case["dtype"]], case["T"], case["d"], case["E"], case["k"], case["N"]
+    if not k:
+        w = _normal(g, (E, N, d), dt, d ** -0.5)
+        rows, columns = _packed_buffers(E * N, d), _packed_buffers(E * d, N)
+        return {"x": w, "rows8": rows, "columns8": columns, "along_rows": torch.zeros(E, N, d, dtype=dt, device=DEV),
+                "along_columns": torch.zeros(E, d, N, dtype=dt, device=DEV)}
+    # activations whose features differ in size, as behind a norm with learned weights
+    x = (_normal(g, (T, d)) * torch.exp(0.5 * _normal(g, (d,)))).to(dt)
+    choice = torch.topk(_normal(g, (T, E)), k, dim=1)[1]
+    kept = torch.rand((T, k), generator=g, device=DEV) < case["used"]
+    kept[0, 0] = True
+    key = torch.where(kept, choice, E).reshape(-1)
+    order = torch.sort(key, stable=True)[1]
+    place = torch.empty_like(order)
+    place[order] = torch.arange(T * k, device=DEV)
+    row_of = torch.where(kept.reshape(-1), place, -1).to(torch.int32).reshape(T, k).contiguous()
+    return {"x": x, "row_of": row_of, "rows8": _packed_buffers(T * k, d), "along_rows": torch.zeros(T * k, d, dtype=dt, device=DEV)}
+
+
+def _group_ends(case, seed):
+    """Rows of each expert: shares of unlike popularity, whole numbers that add up to the rows in use."""
+    rng, R, E = random.Random(int(seed) * 7919 + 5), case["rows"], case["E"]
+    used = max(1, int(R * case["used"])) if case["used"] < 1.0 else R
+    shares = [math.exp(rng.gauss(0.0, case["skew"])) for _ in range(E)]
+    ends = [int(used * sum(shares[: e + 1]) / sum(shares)) for e in range(E)]
+    ends[-1] = used
+    return ends
+
+
+def _prepare_rows(case, seed):
+    g, R, E, K, N, dt = _generator(case, seed), case["rows"], case["E"], case["K"], case["N"], DTYPES[case["dtype"]]
+    ends = _group_ends(case, seed)
+    glu = case["act"] == "swiglu"
+    s = {"offsets": torch.tensor([0] + ends, dtype=torch.int32, device=DEV), "most": max(b - a for a, b in zip([0] + ends, ends)),
+         "x8": _pack(_normal(g, (R, K)))}
+    if case["op"] == "linear":
+        for name in ("w8", "w_up8")[: 1 + glu]:
+            s[name] = _pack(_normal(g, (E, N, K), std=K ** -0.5))
+        s.update(bias=_normal(g, (E, N), std=0.2) if case["bias"] else None, bias_up=_normal(g, (E, N), std=0.2) if case["bias"] and glu else None,
+                 residual=_normal(g, (R, N), dt) if case["residual"] else None)
+        if case["keep"]:
+            for name in ("y", "pre", "pre_up")[: 1 + (case["act"] != "none") + glu]:
+                s[name + "8"], s[name] = _packed_buffers(R, N), torch.zeros(R, N, dtype=dt, device=DEV)
+        else:
+            s["y"] = torch.zeros(R, N, dtype=dt, device=DEV)
+        return s
+    # the weights along their columns, gate and up beside each other; what the forward has kept; the gradient from above
+    halves = [torch.nn.functional.pad(_normal(g, (E, N, K), std=K ** -0.5).transpose(1, 2), (0, -N % BLOCK)) for _ in range(1 + glu)]
+    s["wt8"] = _pack(torch.cat(halves, 2))
+    for name in ("pre8", "pre_up8")[: (case["act"] != "none") + glu]:
+        s[name] = _pack(_normal(g, (R, N)))
+    n = 1 + glu
+    s.update(dy=_normal(g, (R, N), dt, 0.01), d8=_packed_buffers(R, n * _blocks(N) * BLOCK), dx=torch.zeros(R, K, dtype=dt, device=DEV),
+             dw=torch.zeros(E, N, K, dtype=dt, device=DEV), dw_up=torch.zeros(E, N, K, dtype=dt, device=DEV) if glu else None,
+             dbias=torch.zeros(E, N, device=DEV) if case["bias"] else None,
+             dbias_up=torch.zeros(E, N, device=DEV) if case["bias"] and glu else None)
+    # room for both operands of the weights' gradient, whose blocks of 128 rows begin anew with each expert
+    blocks, groups = R // BLOCK + min(E, R), R // (4 * BLOCK) + min(E, R)
+    for name, width in (("dt8", n * N), ("xt8", K)):
+        s[name] = (torch.zeros(blocks * BLOCK * width, dtype=torch.uint8, device=DEV), torch.zeros(groups * 4 * width, dtype=torch.uint8, device=DEV))
+    return s
+
+
+def prepare(case, seed):
+    """Inputs, weights and output buffers, as a program that calls the operator again and again keeps them."""
+    s = _prepare_pack(case, seed) if case["op"] == "pack" else _prepare_rows(case, seed)
+    s["case"] = case
+    return s
+
+
+# ---- one pass ---------------------------------------------------------------------------------------------------
+
+def run(s):
+    return {"pack": (_plain_pack, _own_pack), "linear": (_plain_linear, _own_linear),
+            "backward": (_plain_backward, _own_backward)}[s["case"]["op"]][1 if own else 0](s)
+
+
+def _present(s, names):
+    return {n: s[n] for n in names if s.get(n) is not None}
+
+
+def _plain_pack(s):
+    c, dt = s["case"], s["x"].dtype
+    x = s["x"].float()
+    if not c["k"]:
+        return {"along_rows": _unpack(_pack(x), c["d"]).to(dt), "along_columns": _unpack(_pack(x.transpose(1, 2).contiguous()), c["N"]).to(dt)}
+    T, k, d = c["T"], c["k"], c["d"]
+    row = s["row_of"].long().reshape(-1)
+    v = _unpack(_pack(x), d).to(dt)
+    out = torch.zeros(T * k + 1, d, dtype=dt, device=DEV)                                 # one row more takes the pairs not in use
+    out[torch.where(row >= 0, row, T * k)] = v.repeat_interleave(k, dim=0)
+    return {"along_rows": out[: T * k]}
+
+
+def _own_pack(s):
+    from paper_2406_00023_amd import binding as B
+    c = s["case"]
+    if not c["k"]:
+        if "cfg" not in s:
+            s["cfg"] = B.make_pack_config(c["N"], c["d"], s["x"].dtype, E=c["E"])
+            s["cfg_t"] = B.make_pack_config(c["d"], c["N"], s["x"].dtype, E=c["E"])
+        B.etr_pack_rows(s["cfg"], s["x"], s["rows8"])
+        B.etr_pack_columns(s["cfg"], s["x"], None, s["columns8"])
+        B.etr_unpack_rows(s["cfg"], s["rows8"], s["along_rows"])
+        B.etr_unpack_rows(s["cfg_t"], s["columns8"], s["along_columns"])
+        return _present(s, ("along_rows", "along_columns"))
+    if "cfg" not in s:
+        s["cfg"] = B.make_sort_config(c["T"], c["k"], c["E"], c["d"], s["x"].dtype)
+        s["cfg_rows"] = B.make_pack_config(c["T"] * c["k"], c["d"], s["x"].dtype)
+    B.etr_pack_sorted_rows(s["cfg"], s["x"], s["row_of"], s["rows8"])
+    B.etr_unpack_rows(s["cfg_rows"], s["rows8"], s["along_rows"])
+    return _present(s, ("along_rows",))
+
+
+def _activation(act, a, b):
+    if act == "none":
+        return a
+    if act == "gelu":
+        return 0.5 * a * (1.0 + torch.erf(a * math.sqrt(0.5)))
+    h = a * torch.sigmoid(a)
+    return h * b if act == "swiglu" else h
+
+
+def _spreading(s):
+    """Rows laid out by expert, as many whole blocks of 128 for each as the fullest has, so that the products are one batch; and back."""
+    c = s["case"]
+    R, E, most = c["rows"], c["E"], _blocks(s["most"]) * BLOCK
+    offsets = s["offsets"].long()
+    at = offsets[:-1, None] + torch.arange(most, device=DEV)[None, :]
+    live = at < offsets[1:, None]
+    source = torch.where(live, at, 0).reshape(-1)
+    target = torch.where(live, at, R).reshape(-1)              # one row more takes what is no row
+
+    def spread(v):
+        return torch.where(live.reshape(-1, 1), v[source].float(), 0.0).reshape(E, most, v.shape[1])
+
+    def rows(v, dtype):
+        out = torch.zeros(R + 1, v.shape[2], device=DEV)
+        out[target] = v.reshape(-1, v.shape[2])
+        return out[:R].to(dtype)
+
+    return spread, rows
+
+
+def _plain_linear(s):
+    c, dt = s["case"], s["y"].dtype
+    K, N, act = c["K"], c["N"], c["act"]
+    glu = act == "swiglu"
+    spread, rows = _spreading(s)
+    x = spread(_unpack(s["x8"], K))
+    a = torch.bmm(x, _unpack(s["w8"], K).transpose(1, 2).contiguous())
+    b = torch.bmm(x, _unpack(s["w_up8"], K).transpose(1, 2).contiguous()) if glu else None
+    if c["bias"]:
+        a = a + s["bias"][:, None, :]
+        b = b + s["bias_up"][:, None, :] if glu else None
+    y = _activation(act, a, b)
+    if c["residual"]:
+        y = y + spread(s["residual"])
+    if not c["keep"]:
+        return {"y": rows(y, dt)}
+    r = {"y": y, "pre": a if act != "none" else None, "pre_up": b}
+    return {n: _unpack(_pack(rows(v, torch.float32)), N).to(dt) for n, v in r.items() if v is not None}
+
+
+def _own_linear(s):
+    from paper_2406_00023_amd import binding as B
+    c = s["case"]
+    if "cfg" not in s:
+        s["cfg"] = B.make_linear_config(c["rows"], c["K"], c["N"], c["E"], DTYPES[c["dtype"]], act=ACTS[c["act"]])
+        s["cfg_out"] = B.make_pack_config(c["rows"], c["N"], DTYPES[c["dtype"]])
+    B.etr_expert_linear8(s["cfg"], s["x8"], s["offsets"], s["w8"], y=None if c["keep"] else s["y"], w_up8=s.get("w_up8"), bias=s["bias"],
+                         bias_up=s["bias_up"], residual=s["residual"], y8=s.get("y8"), pre8=s.get("pre8"), pre_up8=s.get("pre_up8"))
+    if c["keep"]:
+        for n in ("y", "pre", "pre_up"):
+            if n in s:
+                B.etr_unpack_rows(s["cfg_out"], s[n + "8"], s[n])
+    return _present(s, ("y", "pre", "pre_up"))
+
+
+def _plain_backward(s):
+    c, dt = s["case"], s["dy"].dtype
+    K, N, act = c["K"], c["N"], c["act"]
+    glu = act == "swiglu"
+    spread, rows = _spreading(s)
+    d = [spread(s["dy"])]
+    if act != "none":
+        a = spread(_unpack(s["pre8"], N))
+        sig = torch.sigmoid(a)
+        if act == "gelu":
+            d = [d[0] * (0.5 * (1.0 + torch.erf(a * math.sqrt(0.5))) + a * torch.exp(-0.5 * a * a) / math.sqrt(2.0 * math.pi))]
+        else:
+            slope = sig * (1.0 + a * (1.0 - sig))
+            d = [d[0] * spread(_unpack(s["pre_up8"], N)) * slope, d[0] * a * sig] if glu else [d[0] * slope]
+    r = {}
+    if c["bias"]:
+        for name, v in zip(("dbias", "dbias_up"), d):
+            r[name] = v.sum(1)
+    # along the rows, as dx takes it
+    along_rows = torch.cat([torch.nn.functional.pad(v, (0, -N % BLOCK)) for v in d], 2)
+    along_rows = _values(*_round8(along_rows))
+    wt = _unpack(s["wt8"], along_rows.shape[2])
+    r["dx"] = rows(torch.bmm(along_rows, wt.transpose(1, 2).contiguous()), dt)
+    del along_rows, wt
+    # along an expert's rows, as dw takes both operands
+    xt = _values(*_round8(spread(_unpack(s["x8"], K)).transpose(1, 2).contiguous())).transpose(1, 2).contiguous()
+    for name, v in zip(("dw", "dw_up"), d):
+        r[name] = torch.bmm(_values(*_round8(v.transpose(1, 2).contiguous())), xt).to(dt)
+    return r
+
+
+def _own_backward(s):
+    from paper_2406_00023_amd import binding as B
+    c, dt = s["case"], s["dy"].dtype
+    if "cfg" not in s:
+        s["cfg"] = B.make_linear_config(c["rows"], c["K"], c["N"], c["E"], dt, act=ACTS[c["act"]])
+        s["cfg_dx"] = B.make_linear_config(c["rows"], s["d8"][0].shape[1], c["K"], c["E"], dt)
+        s["cfg_x"] = B.make_pack_config(c["rows"], c["K"], dt, E=c["E"], sorted=1)
+        s["ws"] = B.alloc_workspace(B.etr_act_backward8_workspace_bytes(s["cfg"]), DEV)
+    B.etr_act_backward8(s["cfg"], s["dy"], s["offsets"], s["ws"], pre8=s.get("pre8"), pre_up8=s.get("pre_up8"), d8=s["d8"], dt8=s["dt8"],
+                        dbias=s["dbias"], dbias_up=s["dbias_up"])
+    B.etr_expert_linear8(s["cfg_dx"], s["d8"], s["offsets"], s["wt8"], y=s["dx"])
+    B.etr_repack_columns(s["cfg_x"], s["x8"], s["offsets"], s["xt8"])
+    B.etr_weight_gradient8(s["cfg"], s["dt8"], s["xt8"], s["offsets"], s["dw"], dw_up=s["dw_up"])
+    return _present(s, ("dx", "dw", "dw_up", "dbias", "dbias_up"))
+
+
+# ---- what a pass cannot do without ------------------------------------------------------------------------------
+
+def work(case):
+    c, el = case, SIZES[case["dtype"]]
+    packed = 1.0 + 1.0 / BLOCK
+    if c["op"] == "pack":
+        if not c["k"]:
+            n = float(c["E"] * c["N"] * c["d"])
+            return {"bytes": n * el + 2 * n * (2 * packed + el), "flops": 4 * n}
+        n, m = float(c["T"] * c["d"]), float(c["T"] * c["k"] * c["d"]) * c["used"]
+        return {"bytes": n * el + m * (2 * packed + el) + 4 * c["T"] * c["k"], "flops": 2 * n + m}
+    R, E, K, N = int(c["rows"] * c["used"]), c["E"], c["K"], c["N"]
+    n = 2 if c["act"] == "swiglu" else 1
+    live = min(E, max(1, R))
+    weights = n * live * K * N
+    if c["op"] == "linear":
+        kept = (1 + (c["act"] != "none") + (n == 2)) * (2 * packed + el) if c["keep"] else el
+        return {"bytes": packed * (weights + R * K) + R * N * (kept + el * c["residual"]) + 4 * n * E * N * c["bias"], "flops": 2.0 * n * R * K * N}
+    kept = n * packed if c["act"] != "none" else 0
+    return {"bytes": packed * (weights + R * K) + R * N * (el + kept) + R * K * el + n * E * K * N * el + 4 * n * E * N * c["bias"],
+            "flops": 4.0 * n * R * K * N}
+
+
+# ---- the definitions in 64 bits ---------------------------------------------------------------------------------
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return {"pack": _exact_pack, "linear": _exact_linear, "backward": _exact_backward}[case["op"]](s)
+
+
+def _table():
+    """The value of each byte, by its bits."""
+    v = []
+    for b in range(256):
+        sign, e, m = -1.0 if b & 128 else 1.0, (b >> 3) & 15, b & 7
+        v.append(math.nan if e == 15 and m == 7 else sign * (m / 8 * 2.0 ** -6 if e == 0 else (1 + m / 8) * 2.0 ** (e - 7)))
+    return torch.tensor(v, dtype=torch.float64, device=DEV)
+
+
+def _decode(q, s, K):
+    """One packed matrix [rows][K] in 64 bits."""
+    block = torch.arange(q.shape[1], device=DEV) // BLOCK
+    exponent = s[block // 4, :, block % 4].t().double() - 127.0
+    return (_table()[q.long()] * torch.exp2(exponent))[:, :K]
+
+
+def _nearest(x):
+    """What the blocks of 128 along the last axis of x (64 bits) are worth once they are packed."""
+    n = x.shape[-1]
+    out = torch.empty_like(x)
+    for at in range(0, n, BLOCK):
+        v = x[..., at: at + BLOCK]
+        top = v.abs().amax(-1, keepdim=True)
+        power = torch.ceil(torch.log2(torch.where(top > 0, top, 1.0) / 448.0)) - 2          # (two below: the logarithm is rounded)
+        for _ in range(3):
+            power = torch.where(top > 448.0 * torch.exp2(power), power + 1, power)
+        scale = torch.exp2(torch.where(top > 0, power, 0.0).clamp(min=-127.0))
+        u = v / scale
+        step = torch.exp2((torch.frexp(u)[1] - 4).clamp(min=-9).double())                    # three bits behind the first
+        out[..., at: at + BLOCK] = torch.round(u / step) * step * scale
+    return out
+
+
+def _slices(n, width):
+    step = max(1, (1 << 26) // max(1, width))
+    return [slice(i, min(n, i + step)) for i in range(0, n, step)]
+
+
+def _exact_pack(s):
+    c = s["case"]
+    if not c["k"]:
+        return {"along_rows": torch.stack([_nearest(w.double()).float() for w in s["x"]]),
+                "along_columns": torch.stack([_nearest(w.double().t().contiguous()).float() for w in s["x"]])}
+    out = torch.zeros(c["T"] * c["k"], c["d"], dtype=torch.float32, device=DEV)             # (the values have four bits)
+    for sl in _slices(c["T"], c["d"]):
+        v = _nearest(s["x"][sl].double()).float()
+        for j in range(c["k"]):
+            row = s["row_of"][sl, j].long()
+            out[row[row >= 0]] = v[row >= 0]
+    return {"along_rows": out.double()}
+
+
+def _exact_linear(s):
+    c = s["case"]
+    R, K, N, act = c["rows"], c["K"], c["N"], c["act"]
+    glu, ends = act == "swiglu", s["offsets"].tolist()
+    names = [n for n in ("y", "pre", "pre_up") if s.get(n) is not None]
+    r = {n: torch.zeros(R, N, dtype=torch.float64, device=DEV) for n in names}
+    x = _decode(*s["x8"], K)
+    for e in range(c["E"]):
+        rows = slice(ends[e], ends[e + 1])
+        if ends[e] == ends[e + 1]:
+            continue
+        a = x[rows] @ _decode(s["w8"][0][e], s["w8"][1][e], K).t() + (s["bias"][e].double() if c["bias"] else 0.0)
+        b = x[rows] @ _decode(s["w_up8"][0][e], s["w_up8"][1][e], K).t() + (s["bias_up"][e].double() if c["bias"] else 0.0) if glu else None
+        got = {"y": _activation(act, a, b) + (s["residual"][rows].double() if c["residual"] else 0.0), "pre": a, "pre_up": b}
+        for n in names:
+            r[n][rows] = _nearest(got[n]) if c["keep"] else got[n]
+    return r
+
+
+def _exact_backward(s):
+    c = s["case"]
+    R, E, K, N, act = c["rows"], c["E"], c["K"], c["N"], c["act"]
+    glu, ends = act == "swiglu", s["offsets"].tolist()
+
+    def zeros(*n):
+        return torch.zeros(*n, dtype=torch.float64, device=DEV)
+
+    r = {"dx": zeros(R, K)}
+    for n in ("dw", "dw_up", "dbias", "dbias_up"):
+        if s.get(n) is not None:
+            r[n] = zeros(*s[n].shape)
+    x = _decode(*s["x8"], K)
+    pre = [_decode(*s[n], N) for n in ("pre8", "pre_up8") if n in s]
+    padded = _blocks(N) * BLOCK
+    for e in range(E):
+        rows = slice(ends[e], ends[e + 1])
+        if ends[e] == ends[e + 1]:
+            continue
+        dy = s["dy"][rows].double()
+        if act == "none":
+            d = [dy]
+        else:
+            leaf = [p[rows].clone().requires_grad_(True) for p in pre]
+            d = torch.autograd.grad(_activation(act, leaf[0], leaf[1] if glu else None), leaf, dy)
+        wt = _decode(s["wt8"][0][e], s["wt8"][1][e], s["wt8"][0].shape[2])
+        xt = _nearest(x[rows].t().contiguous()).t().contiguous()
+        for i, v in enumerate(d):
+            up = "_up" if i else ""
+            r["dx"][rows] += _nearest(v) @ wt[:, i * padded: i * padded + N].t()
+            r["dw" + up][e] = _nearest(v.t().contiguous()) @ xt
+            if c["bias"]:
+                r["dbias" + up][e] = v.sum(0)
+    return r
