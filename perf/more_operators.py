@@ -7,10 +7,10 @@ A packed matrix holds e4m3 values (sign, 4 bits of exponent, 3 of mantissa, larg
   pack     rows into a packed matrix and back to the values that it stands for: tokens through the tables of the rows sorted by
            expert (etr_pack_sorted_rows), or stacked weights, along both of their directions (etr_pack_rows, etr_pack_columns);
            etr_unpack_rows
-  linear   etr_expert_linear8: the experts' products of packed rows and packed weights, with bias, activation and residual; with
+  linear   etr_packed_linear: the experts' products of packed rows and packed weights, with bias, activation and residual; with
            `keep` the result and the pre-activations are kept packed, as a training forward does
-  backward etr_act_backward8: the pre-activations' gradient from the packed pre-activations, packed along rows and along columns;
-           etr_expert_linear8 for dx; etr_repack_columns of the packed rows and etr_weight_gradient8 for dw
+  backward etr_packed_act_backward: the pre-activations' gradient from the packed pre-activations, packed along rows and along columns;
+           etr_packed_linear for dx; etr_repack_columns of the packed rows and etr_packed_weight_gradient for dw
 
 The sizes are those of the workloads of `paper_2406_00023_amd.inputs`, decode batches on the same layers, and generic
 ragged ones.  The plain forms are elementary torch operations in 32 bits, rounded to the output's type once.
@@ -344,7 +344,7 @@ def _own_linear(s):
     if "cfg" not in s:
         s["cfg"] = B.make_linear_config(c["rows"], c["K"], c["N"], c["E"], DTYPES[c["dtype"]], act=ACTS[c["act"]])
         s["cfg_out"] = B.make_pack_config(c["rows"], c["N"], DTYPES[c["dtype"]])
-    B.etr_expert_linear8(s["cfg"], s["x8"], s["offsets"], s["w8"], y=None if c["keep"] else s["y"], w_up8=s.get("w_up8"), bias=s["bias"],
+    B.etr_packed_linear(s["cfg"], s["x8"], s["offsets"], s["w8"], y=None if c["keep"] else s["y"], w_up8=s.get("w_up8"), bias=s["bias"],
                          bias_up=s["bias_up"], residual=s["residual"], y8=s.get("y8"), pre8=s.get("pre8"), pre_up8=s.get("pre_up8"))
     if c["keep"]:
         for n in ("y", "pre", "pre_up"):
@@ -391,12 +391,12 @@ def _own_backward(s):
         s["cfg"] = B.make_linear_config(c["rows"], c["K"], c["N"], c["E"], dt, act=ACTS[c["act"]])
         s["cfg_dx"] = B.make_linear_config(c["rows"], s["d8"][0].shape[1], c["K"], c["E"], dt)
         s["cfg_x"] = B.make_pack_config(c["rows"], c["K"], dt, E=c["E"], sorted=1)
-        s["ws"] = B.alloc_workspace(B.etr_act_backward8_workspace_bytes(s["cfg"]), DEV)
-    B.etr_act_backward8(s["cfg"], s["dy"], s["offsets"], s["ws"], pre8=s.get("pre8"), pre_up8=s.get("pre_up8"), d8=s["d8"], dt8=s["dt8"],
+        s["ws"] = B.alloc_workspace(B.etr_packed_act_workspace_bytes(s["cfg"]), DEV)
+    B.etr_packed_act_backward(s["cfg"], s["dy"], s["offsets"], s["ws"], pre8=s.get("pre8"), pre_up8=s.get("pre_up8"), d8=s["d8"], dt8=s["dt8"],
                         dbias=s["dbias"], dbias_up=s["dbias_up"])
-    B.etr_expert_linear8(s["cfg_dx"], s["d8"], s["offsets"], s["wt8"], y=s["dx"])
+    B.etr_packed_linear(s["cfg_dx"], s["d8"], s["offsets"], s["wt8"], y=s["dx"])
     B.etr_repack_columns(s["cfg_x"], s["x8"], s["offsets"], s["xt8"])
-    B.etr_weight_gradient8(s["cfg"], s["dt8"], s["xt8"], s["offsets"], s["dw"], dw_up=s["dw_up"])
+    B.etr_packed_weight_gradient(s["cfg"], s["dt8"], s["xt8"], s["offsets"], s["dw"], dw_up=s["dw_up"])
     return _present(s, ("dx", "dw", "dw_up", "dbias", "dbias_up"))
 
 
