@@ -413,6 +413,97 @@ etr_status etr_expert_linear_backward(const etr_linear_config* cfg, const void* 
 etr_status etr_route_backward(const etr_config* cfg, const void* x, const float* w_emb, const float* score,
                               const float* gate, const float* dgate, const void* dx_add, void* dx, void* stream);
 
+/* ---- the experts in 8 bits ------------------------------------------------------------------------------ */
+
+/* Packed matrices.  A matrix [rows][K] is held as e4m3 values (sign, 4 bits of exponent, 3 of mantissa, largest 448, no infinity) and one power
+ * of two for each block of 128 values of a row:
+ *   values [rows][Kp] bytes, Kp = 128 ceil(K / 128), zeros past K
+ *   scales [ceil(Kp / 512)][rows][4] bytes: byte (b / 4, r, b % 4) is the exponent of row r's block b, plus 127; 127 past the last block
+ * and stands for value * 2^(scale - 127).  Packing takes the smallest power, 2^-127 at least, by which the block's largest finite magnitude
+ * comes to 448 or less, and rounds to the nearest e4m3 value, ties to even.  NaN and infinities become NaN, and have no part in the power.
+ * (Powers of two, because the matrix pipe applies them, and because a value that is packed again, in other blocks, stays what it is unless it lies
+ * 2^13 below its new block's largest.)  A stack of E matrices is one after the other, values and scales each.
+ * ALONG COLUMNS the transposed matrix is packed: [K][rows], blocks of 128 rows of a column; this is what a product contracts over the rows takes.
+ * For rows sorted by expert every expert's rows are such a matrix of its own, [K][rows of e], without a gap behind that of expert e - 1 (an
+ * expert without rows has none); its blocks begin with its first row.  All pointers 16-byte aligned. */
+typedef struct {
+    int32_t rows, K, E;     /* K % 8 == 0, K <= 2^20, E <= 64, rows (of the whole stack) <= 2^28 */
+    int32_t dtype;          /* etr_dtype of the matrix that is packed or unpacked */
+    int32_t sorted;         /* 0: E matrices of `rows` rows each; 1: one of `rows` rows, sorted by expert (E experts) */
+} etr_pack_config;
+
+/* Bytes of the values and scales of what is packed along rows or columns (sorted: the most that any offsets need). 0 for an
+ * invalid config. */
+size_t etr_packed_rows_bytes(const etr_pack_config* cfg);
+size_t etr_packed_rows_scale_bytes(const etr_pack_config* cfg);
+size_t etr_packed_columns_bytes(const etr_pack_config* cfg);
+size_t etr_packed_columns_scale_bytes(const etr_pack_config* cfg);
+
+/* x [E][rows][K] (sorted: [rows][K]) dtype in; values, scales out, along rows. */
+etr_status etr_pack_rows(const etr_pack_config* cfg, const void* x, void* values, void* scales, void* stream);
+
+/* etr_sort_rows that writes packed rows: xs[row_of[t][j]] = packed x[t]; rows from offsets[E] on are left untouched.
+ *   x [T][d] dtype in, row_of [T][k] in; values, scales out: a matrix of T * k rows and K = d */
+etr_status etr_pack_sorted_rows(const etr_sort_config* cfg, const void* x, const int32_t* row_of, void* values, void* scales,
+                                void* stream);
+
+/* What a matrix (or stack) packed along rows stands for: y [E][rows][K] dtype out, each value rounded to it once (exact but for bf16 below
+ * 2^-133 and fp32 below 2^-149). */
+etr_status etr_unpack_rows(const etr_pack_config* cfg, const void* values, const void* scales, void* y, void* stream);
+
+/* Along columns: x [E][rows][K] dtype in (sorted: [rows][K], and offsets [E+1] int32 in, ascending from 0, clamped to rows; else
+ * offsets NULL); values, scales out. */
+etr_status etr_pack_columns(const etr_pack_config* cfg, const void* x, const int32_t* offsets, void* values, void* scales, void* stream);
+
+/* The same from a matrix that is packed along rows (dtype is not looked at). */
+etr_status etr_repack_columns(const etr_pack_config* cfg, const void* row_values, const void* row_scales, const int32_t* offsets,
+                              void* values, void* scales, void* stream);
+
+/* One packed matrix or stack, as an argument. */
+typedef struct { void* values; void* scales; } etr_packed;
+
+/* etr_expert_linear of packed operands:  y[r] = act(x[r] W[e]^T + bias[e]) + residual[r], x and W being what the packed ones stand for.
+ *   x [rows][K], w, w_up E x [N][K], packed along rows (w_up values and scales NULL without SwiGLU); offsets, bias, bias_up, residual as in
+ *   etr_expert_linear
+ *   y [rows][N] dtype out, optional; may be residual
+ *   y8, pre8, pre_up8 [rows][N] out, packed along rows, each optional (NULL values; then NULL scales); at least one of y and y8.  pre8 is a,
+ *   pre_up8 the up product (SwiGLU: both or neither; else pre_up8 NULL), for the backward; they are packed from fp32 results
+ * Rows of the outputs that belong to no expert are left untouched.
+ * dtype is that of y and residual, and says how exact the sums are.  ETR_BF16: the matrix pipe multiplies 8-bit values, and what is
+ * 2^-13 below the largest of some 16 neighbouring products is cut off there (1.5e-5 of a result's size on normal data, 1/250 of a rounding to
+ * bf16).  ETR_F32: the values, exact in bf16, go through bf16 products, whose sums are in fp32; half the rate. */
+etr_status etr_packed_linear(const etr_linear_config* cfg, const etr_packed* x, const int32_t* offsets, const etr_packed* w,
+                              const etr_packed* w_up, const float* bias, const float* bias_up, const void* residual, void* y,
+                              const etr_packed* y8, const etr_packed* pre8, const etr_packed* pre_up8, void* stream);
+
+/* Scratch of etr_packed_act_backward (partial sums of the biases' gradients). 0 for an invalid config. */
+size_t etr_packed_act_workspace_bytes(const etr_linear_config* cfg);
+
+/* The element-wise part of the backward, from packed pre-activations:  da = dy act'(a);  SwiGLU: da = dy up SiLU'(a), db = dy SiLU(a)
+ *   dy [rows][N] dtype in; pre8 (not with ETR_ACT_NONE), pre_up8 (SwiGLU) [rows][N] in, packed along rows: what the forward kept
+ *   d8 out, optional: da packed along rows, with SwiGLU da and db beside each other, [rows][2 Np], Np = 128 ceil(N / 128), zeros past N.
+ *   This is the x of the etr_packed_linear that gives dx, with K = Np (SwiGLU 2 Np), N = this K, no activation, and the weights packed
+ *   along columns ([K][N] of each expert; SwiGLU: both beside each other, etr_pack_columns_pair)
+ *   dt8 out, optional: the same along columns, for each expert [N][its rows], SwiGLU [2 N][its rows], da above db: for etr_packed_weight_gradient
+ *   dbias, dbias_up [E][N] fp32 out, optional (both or neither with SwiGLU): sums over the expert's rows before packing, in a fixed
+ *   order; 0 for an expert without rows
+ * At least one output.  ws is needed with dbias only. */
+etr_status etr_packed_act_backward(const etr_linear_config* cfg, const void* dy, const int32_t* offsets, const etr_packed* pre8,
+                             const etr_packed* pre_up8, const etr_packed* d8, const etr_packed* dt8, float* dbias, float* dbias_up,
+                             void* ws, size_t ws_bytes, void* stream);
+
+/* Two stacks along columns, beside each other: E x [K][2 Np], Np = 128 ceil(rows / 128), x in the first half of a row, x_up in the second.
+ * cfg->sorted must be 0.  (Its bytes are those of a matrix along rows, rows = K and K = 2 Np.) */
+etr_status etr_pack_columns_pair(const etr_pack_config* cfg, const void* x, const void* x_up, void* values, void* scales, void* stream);
+
+/* Gradient of the experts' weights:  dw[e] = da^T x over the expert's rows (dw_up with db)
+ *   dt8 as etr_packed_act_backward writes it; xt8 for each expert [K][its rows]: x by etr_repack_columns (or etr_pack_columns), same offsets
+ *   dw, dw_up [E][N][K] dtype out (dw_up with SwiGLU, else NULL), overwritten; zeros for an expert without rows
+ * dtype says how exact the sums are, as in etr_packed_linear.  The activation of cfg matters only as SwiGLU or not.  rows <= 2^24
+ * (ETR_ERR_UNSUPPORTED). */
+etr_status etr_packed_weight_gradient(const etr_linear_config* cfg, const etr_packed* dt8, const etr_packed* xt8, const int32_t* offsets,
+                                void* dw, void* dw_up, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

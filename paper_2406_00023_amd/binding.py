@@ -25,7 +25,10 @@ EXPORTS = ("etr_workspace_bytes", "etr_select_workspace_bytes", "etr_ffn_workspa
            "etr_moe_forward_train", "etr_select_noalloc", "etr_select_noalloc_max_bytes",
            "etr_block_norm", "etr_norm_workspace_bytes", "etr_block_norm_backward", "etr_sort_workspace_bytes",
            "etr_sort_tokens", "etr_sort_rows", "etr_sort_rows_backward", "etr_unsort_rows", "etr_unsort_rows_backward",
-           "etr_expert_linear", "etr_linear_workspace_bytes", "etr_expert_linear_backward", "etr_route_backward")
+           "etr_expert_linear", "etr_linear_workspace_bytes", "etr_expert_linear_backward", "etr_route_backward",
+           "etr_packed_rows_bytes", "etr_packed_rows_scale_bytes", "etr_packed_columns_bytes", "etr_packed_columns_scale_bytes",
+           "etr_pack_rows", "etr_pack_sorted_rows", "etr_unpack_rows", "etr_pack_columns", "etr_repack_columns", "etr_pack_columns_pair",
+           "etr_packed_linear", "etr_packed_act_workspace_bytes", "etr_packed_act_backward", "etr_packed_weight_gradient")
 N_STAGE_EVENTS = 7
 STAGE_NAMES = ("route", "select", "dispatch", "ffn_gate_up", "ffn_down", "combine")
 
@@ -46,6 +49,14 @@ class EtrSortConfig(ctypes.Structure):
 
 class EtrLinearConfig(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("rows", "K", "N", "E", "dtype", "act")]
+
+
+class EtrPackConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "K", "E", "dtype", "sorted")]
+
+
+class EtrPacked(ctypes.Structure):
+    _fields_ = [("values", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
 
 
 ACT_NONE, ACT_SILU, ACT_GELU, ACT_SWIGLU = 0, 1, 2, 3
@@ -74,9 +85,10 @@ def load_library():
                  "etr_stats_workspace_bytes", "etr_backward_workspace_bytes"):
         getattr(lib, name).restype = sz
         getattr(lib, name).argtypes = [cp]
-    np_, sp, lp = (ctypes.POINTER(c) for c in (EtrNormConfig, EtrSortConfig, EtrLinearConfig))
+    np_, sp, lp, pp, pk = (ctypes.POINTER(c) for c in (EtrNormConfig, EtrSortConfig, EtrLinearConfig, EtrPackConfig, EtrPacked))
     for name, arg in (("etr_norm_workspace_bytes", np_), ("etr_sort_workspace_bytes", sp),
-                      ("etr_linear_workspace_bytes", lp)):
+                      ("etr_linear_workspace_bytes", lp), ("etr_packed_act_workspace_bytes", lp), ("etr_packed_rows_bytes", pp),
+                      ("etr_packed_rows_scale_bytes", pp), ("etr_packed_columns_bytes", pp), ("etr_packed_columns_scale_bytes", pp)):
         getattr(lib, name).restype = sz
         getattr(lib, name).argtypes = [arg]
     lib.etr_select_noalloc_max_bytes.restype = sz
@@ -108,6 +120,15 @@ def load_library():
         "etr_expert_linear": [lp] + [vp] * 11,
         "etr_expert_linear_backward": [lp] + [vp] * 13 + [sz, vp],
         "etr_route_backward": [cp] + [vp] * 8,
+        "etr_pack_rows": [pp] + [vp] * 4,
+        "etr_pack_sorted_rows": [sp] + [vp] * 5,
+        "etr_unpack_rows": [pp] + [vp] * 4,
+        "etr_pack_columns": [pp] + [vp] * 5,
+        "etr_repack_columns": [pp] + [vp] * 6,
+        "etr_pack_columns_pair": [pp] + [vp] * 5,
+        "etr_packed_linear": [lp, pk, vp, pk, pk, vp, vp, vp, vp, pk, pk, pk, vp],
+        "etr_packed_act_backward": [lp, vp, vp, pk, pk, pk, pk, vp, vp, vp, sz, vp],
+        "etr_packed_weight_gradient": [lp, pk, pk, vp, vp, vp, vp],
     }
     for name, args in sigs.items():
         getattr(lib, name).restype = ctypes.c_int
@@ -145,6 +166,10 @@ def make_sort_config(T, k, E, d, dtype, gate_norm: int = 0) -> EtrSortConfig:
 
 def make_linear_config(rows, K, N, E, dtype, act: int = ACT_NONE) -> EtrLinearConfig:
     return EtrLinearConfig(rows, K, N, E, _dtype(dtype), act)
+
+
+def make_pack_config(rows, K, dtype, E: int = 1, sorted: int = 0) -> EtrPackConfig:
+    return EtrPackConfig(rows, K, E, _dtype(dtype), sorted)
 
 
 # Small calls are bound by the host: addresses go to ctypes as plain integers (None = NULL; the declared argument types
@@ -336,6 +361,89 @@ def etr_expert_linear_backward(cfg, x, offsets, w, dy, ws, w_up=None, pre=None, 
 def etr_route_backward(cfg, x, w_emb, score, gate, dgate, dx_add, dx):
     _check("etr_route_backward", load_library().etr_route_backward(
         ctypes.byref(cfg), _ptr(x), _ptr(w_emb), _ptr(score), _ptr(gate), _ptr(dgate), _ptr(dx_add), _ptr(dx), _stream()))
+
+
+# A packed matrix or stack is a pair of uint8 tensors, (values, scales).
+def _packed(p) -> Optional[EtrPacked]:
+    return None if p is None else EtrPacked(_ptr(p[0]), _ptr(p[1]))
+
+
+def etr_packed_rows_bytes(cfg: EtrPackConfig) -> int:
+    return int(load_library().etr_packed_rows_bytes(ctypes.byref(cfg)))
+
+
+def etr_packed_rows_scale_bytes(cfg: EtrPackConfig) -> int:
+    return int(load_library().etr_packed_rows_scale_bytes(ctypes.byref(cfg)))
+
+
+def etr_packed_columns_bytes(cfg: EtrPackConfig) -> int:
+    return int(load_library().etr_packed_columns_bytes(ctypes.byref(cfg)))
+
+
+def etr_packed_columns_scale_bytes(cfg: EtrPackConfig) -> int:
+    return int(load_library().etr_packed_columns_scale_bytes(ctypes.byref(cfg)))
+
+
+def alloc_packed_rows(cfg: EtrPackConfig, device="cuda"):
+    """(values, scales) for what is packed along rows; zeros."""
+    return (torch.zeros(etr_packed_rows_bytes(cfg), dtype=torch.uint8, device=device),
+            torch.zeros(etr_packed_rows_scale_bytes(cfg), dtype=torch.uint8, device=device))
+
+
+def alloc_packed_columns(cfg: EtrPackConfig, device="cuda"):
+    """(values, scales) for what is packed along columns; zeros."""
+    return (torch.zeros(etr_packed_columns_bytes(cfg), dtype=torch.uint8, device=device),
+            torch.zeros(etr_packed_columns_scale_bytes(cfg), dtype=torch.uint8, device=device))
+
+
+def etr_pack_rows(cfg, x, out):
+    _check("etr_pack_rows", load_library().etr_pack_rows(ctypes.byref(cfg), _ptr(x), _ptr(out[0]), _ptr(out[1]), _stream()))
+
+
+def etr_pack_sorted_rows(cfg, x, row_of, out):
+    _check("etr_pack_sorted_rows", load_library().etr_pack_sorted_rows(ctypes.byref(cfg), _ptr(x), _ptr(row_of), _ptr(out[0]),
+                                                                       _ptr(out[1]), _stream()))
+
+
+def etr_unpack_rows(cfg, packed, y):
+    _check("etr_unpack_rows", load_library().etr_unpack_rows(ctypes.byref(cfg), _ptr(packed[0]), _ptr(packed[1]), _ptr(y), _stream()))
+
+
+def etr_pack_columns(cfg, x, offsets, out):
+    _check("etr_pack_columns", load_library().etr_pack_columns(ctypes.byref(cfg), _ptr(x), _ptr(offsets), _ptr(out[0]), _ptr(out[1]),
+                                                               _stream()))
+
+
+def etr_repack_columns(cfg, packed, offsets, out):
+    _check("etr_repack_columns", load_library().etr_repack_columns(ctypes.byref(cfg), _ptr(packed[0]), _ptr(packed[1]), _ptr(offsets),
+                                                                   _ptr(out[0]), _ptr(out[1]), _stream()))
+
+
+def etr_pack_columns_pair(cfg, x, x_up, out):
+    _check("etr_pack_columns_pair", load_library().etr_pack_columns_pair(ctypes.byref(cfg), _ptr(x), _ptr(x_up), _ptr(out[0]),
+                                                                         _ptr(out[1]), _stream()))
+
+
+def etr_packed_linear(cfg, x8, offsets, w8, y=None, w_up8=None, bias=None, bias_up=None, residual=None, y8=None, pre8=None,
+                       pre_up8=None):
+    _check("etr_packed_linear", load_library().etr_packed_linear(
+        ctypes.byref(cfg), _packed(x8), _ptr(offsets), _packed(w8), _packed(w_up8), _ptr(bias), _ptr(bias_up), _ptr(residual), _ptr(y),
+        _packed(y8), _packed(pre8), _packed(pre_up8), _stream()))
+
+
+def etr_packed_act_workspace_bytes(cfg: EtrLinearConfig) -> int:
+    return int(load_library().etr_packed_act_workspace_bytes(ctypes.byref(cfg)))
+
+
+def etr_packed_act_backward(cfg, dy, offsets, ws=None, pre8=None, pre_up8=None, d8=None, dt8=None, dbias=None, dbias_up=None):
+    _check("etr_packed_act_backward", load_library().etr_packed_act_backward(
+        ctypes.byref(cfg), _ptr(dy), _ptr(offsets), _packed(pre8), _packed(pre_up8), _packed(d8), _packed(dt8), _ptr(dbias),
+        _ptr(dbias_up), _ptr(ws), _nbytes(ws), _stream()))
+
+
+def etr_packed_weight_gradient(cfg, dt8, xt8, offsets, dw, dw_up=None):
+    _check("etr_packed_weight_gradient", load_library().etr_packed_weight_gradient(
+        ctypes.byref(cfg), _packed(dt8), _packed(xt8), _ptr(offsets), _ptr(dw), _ptr(dw_up), _stream()))
 
 
 class StageEvents:

@@ -7,6 +7,7 @@
 #include <vector>
 
 #include "etr_internal.h"
+#include "packed.h"
 
 namespace etr {
 
@@ -109,6 +110,24 @@ etr_status check_linear(const etr_linear_config* c) {
     const long long columns = (std::max(c->K, c->N) + 31) / 32;
     if (columns * (c->rows / 32 + c->E) > (1ll << 30) || columns * columns * c->E > (1ll << 30)) return ETR_ERR_UNSUPPORTED;
     return ETR_OK;
+}
+
+etr_status check_pack(const etr_pack_config* c) {
+    if (!c) return ETR_ERR_NULL;
+    if (c->rows <= 0 || c->K <= 0 || c->E <= 0) return ETR_ERR_SHAPE;
+    if (!known_dtype(c->dtype) || (c->sorted != 0 && c->sorted != 1)) return ETR_ERR_UNSUPPORTED;
+    if (c->E > 64 || c->K % 8 != 0 || c->K > (1 << 20)) return ETR_ERR_UNSUPPORTED;
+    const long long rows = static_cast<long long>(c->rows) * (c->sorted ? 1 : c->E);
+    if (rows > (1 << 28)) return ETR_ERR_UNSUPPORTED;
+    if (((c->K + 127) / 128) * (rows / 128 + c->E) > (1ll << 30)) return ETR_ERR_UNSUPPORTED;        // 32-bit numbers of tiles
+    return ETR_OK;
+}
+
+// A packed operand: optional (`p` null) unless `required`; both of its parts.
+etr_status check_packed(const etr_packed* p, bool required) {
+    if (!p) return required ? ETR_ERR_NULL : ETR_OK;
+    if (!p->values || !p->scales) return ETR_ERR_NULL;
+    return aligned16(p->values) && aligned16(p->scales) ? ETR_OK : ETR_ERR_ALIGN;
 }
 
 // Workspace of etr_moe_forward: optional outputs that the caller did not ask for, the
@@ -549,6 +568,135 @@ etr_status etr_route_backward(const etr_config* cfg, const void* x, const float*
     ETR_REQUIRE_PTR(dx); ETR_OPTIONAL_PTR(dx_add);
     if (static_cast<size_t>(cfg->E) * (cfg->d / cfg->D) * 4 > 120 * 1024) return ETR_ERR_UNSUPPORTED;
     ETR_HIP(launch_route_backward(*cfg, x, w_emb, score, gate, dgate, dx_add, dx, static_cast<hipStream_t>(stream)));
+    return ETR_OK;
+}
+
+size_t etr_packed_rows_bytes(const etr_pack_config* cfg) {
+    if (check_pack(cfg) != ETR_OK) return 0;
+    return packed_bytes(static_cast<size_t>(cfg->rows) * (cfg->sorted ? 1 : cfg->E), cfg->K);
+}
+size_t etr_packed_rows_scale_bytes(const etr_pack_config* cfg) {
+    if (check_pack(cfg) != ETR_OK) return 0;
+    return scale_bytes(static_cast<size_t>(cfg->rows) * (cfg->sorted ? 1 : cfg->E), cfg->K);
+}
+size_t etr_packed_columns_bytes(const etr_pack_config* cfg) {
+    if (check_pack(cfg) != ETR_OK) return 0;
+    return packed_columns_bytes(*cfg);
+}
+size_t etr_packed_columns_scale_bytes(const etr_pack_config* cfg) {
+    if (check_pack(cfg) != ETR_OK) return 0;
+    return packed_columns_scale_bytes(*cfg);
+}
+
+etr_status etr_pack_rows(const etr_pack_config* cfg, const void* x, void* values, void* scales, void* stream) {
+    etr_status s = check_pack(cfg);
+    if (s != ETR_OK) return s;
+    ETR_REQUIRE_PTR(x); ETR_REQUIRE_PTR(values); ETR_REQUIRE_PTR(scales);
+    ETR_HIP(launch_pack_rows(*cfg, x, values, scales, static_cast<hipStream_t>(stream)));
+    return ETR_OK;
+}
+
+etr_status etr_pack_sorted_rows(const etr_sort_config* cfg, const void* x, const int32_t* row_of, void* values, void* scales, void* stream) {
+    etr_status s = check_sort(cfg);
+    if (s != ETR_OK) return s;
+    ETR_REQUIRE_PTR(x); ETR_REQUIRE_PTR(row_of); ETR_REQUIRE_PTR(values); ETR_REQUIRE_PTR(scales);
+    ETR_HIP(launch_pack_sorted_rows(*cfg, x, row_of, values, scales, static_cast<hipStream_t>(stream)));
+    return ETR_OK;
+}
+
+etr_status etr_unpack_rows(const etr_pack_config* cfg, const void* values, const void* scales, void* y, void* stream) {
+    etr_status s = check_pack(cfg);
+    if (s != ETR_OK) return s;
+    ETR_REQUIRE_PTR(values); ETR_REQUIRE_PTR(scales); ETR_REQUIRE_PTR(y);
+    ETR_HIP(launch_unpack_rows(*cfg, values, scales, y, static_cast<hipStream_t>(stream)));
+    return ETR_OK;
+}
+
+etr_status etr_pack_columns(const etr_pack_config* cfg, const void* x, const int32_t* offsets, void* values, void* scales, void* stream) {
+    etr_status s = check_pack(cfg);
+    if (s != ETR_OK) return s;
+    ETR_REQUIRE_PTR(x); ETR_REQUIRE_PTR(values); ETR_REQUIRE_PTR(scales); ETR_OPTIONAL_PTR(offsets);
+    if (cfg->sorted ? !offsets && cfg->E != 1 : offsets != nullptr) return ETR_ERR_NULL;
+    ETR_HIP(launch_pack_columns(*cfg, x, nullptr, offsets, -1, values, scales, static_cast<hipStream_t>(stream)));
+    return ETR_OK;
+}
+
+etr_status etr_repack_columns(const etr_pack_config* cfg, const void* row_values, const void* row_scales, const int32_t* offsets, void* values,
+                              void* scales, void* stream) {
+    etr_status s = check_pack(cfg);
+    if (s != ETR_OK) return s;
+    ETR_REQUIRE_PTR(row_values); ETR_REQUIRE_PTR(row_scales); ETR_REQUIRE_PTR(values); ETR_REQUIRE_PTR(scales); ETR_OPTIONAL_PTR(offsets);
+    if (cfg->sorted ? !offsets && cfg->E != 1 : offsets != nullptr) return ETR_ERR_NULL;
+    const etr_packed rows{const_cast<void*>(row_values), const_cast<void*>(row_scales)};
+    ETR_HIP(launch_pack_columns(*cfg, nullptr, &rows, offsets, -1, values, scales, static_cast<hipStream_t>(stream)));
+    return ETR_OK;
+}
+
+etr_status etr_pack_columns_pair(const etr_pack_config* cfg, const void* x, const void* x_up, void* values, void* scales, void* stream) {
+    etr_status s = check_pack(cfg);
+    if (s != ETR_OK) return s;
+    if (cfg->sorted) return ETR_ERR_UNSUPPORTED;
+    ETR_REQUIRE_PTR(x); ETR_REQUIRE_PTR(x_up); ETR_REQUIRE_PTR(values); ETR_REQUIRE_PTR(scales);
+    ETR_HIP(launch_pack_columns(*cfg, x, nullptr, nullptr, 0, values, scales, static_cast<hipStream_t>(stream)));
+    ETR_HIP(launch_pack_columns(*cfg, x_up, nullptr, nullptr, 1, values, scales, static_cast<hipStream_t>(stream)));
+    return ETR_OK;
+}
+
+etr_status etr_packed_linear(const etr_linear_config* cfg, const etr_packed* x, const int32_t* offsets, const etr_packed* w, const etr_packed* w_up,
+                              const float* bias, const float* bias_up, const void* residual, void* y, const etr_packed* y8, const etr_packed* pre8,
+                              const etr_packed* pre_up8, void* stream) {
+    etr_status s = check_linear(cfg);
+    if (s != ETR_OK) return s;
+    const bool glu = cfg->act == ETR_ACT_SWIGLU;
+    if ((s = check_packed(x, true)) != ETR_OK || (s = check_packed(w, true)) != ETR_OK || (s = check_packed(w_up, glu)) != ETR_OK) return s;
+    if ((s = check_packed(y8, false)) != ETR_OK || (s = check_packed(pre8, false)) != ETR_OK || (s = check_packed(pre_up8, false)) != ETR_OK) return s;
+    ETR_OPTIONAL_PTR(offsets); ETR_OPTIONAL_PTR(bias); ETR_OPTIONAL_PTR(bias_up); ETR_OPTIONAL_PTR(residual); ETR_OPTIONAL_PTR(y);
+    if (!y && !y8) return ETR_ERR_NULL;
+    if (!offsets && cfg->E != 1) return ETR_ERR_NULL;
+    if (!glu && w_up) return ETR_ERR_NULL;
+    if (glu ? (bias == nullptr) != (bias_up == nullptr) || (pre8 == nullptr) != (pre_up8 == nullptr) : bias_up || pre_up8) return ETR_ERR_NULL;
+    const etr_packed* weights[2] = {w, w_up};
+    const etr_packed* kept[3] = {y8, pre8, pre_up8};
+    ETR_HIP(launch_packed_linear(*cfg, *x, offsets, weights, bias, bias_up, residual, y, kept, static_cast<hipStream_t>(stream)));
+    return ETR_OK;
+}
+
+size_t etr_packed_act_workspace_bytes(const etr_linear_config* cfg) {
+    if (check_linear(cfg) != ETR_OK) return 0;
+    return packed_act_ws_bytes(*cfg);
+}
+
+etr_status etr_packed_act_backward(const etr_linear_config* cfg, const void* dy, const int32_t* offsets, const etr_packed* pre8, const etr_packed* pre_up8,
+                             const etr_packed* d8, const etr_packed* dt8, float* dbias, float* dbias_up, void* ws, size_t ws_bytes, void* stream) {
+    etr_status s = check_linear(cfg);
+    if (s != ETR_OK) return s;
+    const bool glu = cfg->act == ETR_ACT_SWIGLU, act = cfg->act != ETR_ACT_NONE;
+    ETR_REQUIRE_PTR(dy); ETR_OPTIONAL_PTR(offsets); ETR_OPTIONAL_PTR(dbias); ETR_OPTIONAL_PTR(dbias_up);
+    if ((s = check_packed(pre8, act)) != ETR_OK || (s = check_packed(pre_up8, glu)) != ETR_OK) return s;
+    if ((s = check_packed(d8, false)) != ETR_OK || (s = check_packed(dt8, false)) != ETR_OK) return s;
+    if (!offsets && cfg->E != 1) return ETR_ERR_NULL;
+    if (!d8 && !dt8 && !dbias) return ETR_ERR_NULL;                  // nothing asked for
+    if ((!act && pre8) || (!glu && pre_up8)) return ETR_ERR_NULL;
+    if (glu ? (dbias == nullptr) != (dbias_up == nullptr) : dbias_up != nullptr) return ETR_ERR_NULL;
+    if (dbias) {
+        ETR_REQUIRE_PTR(ws);
+        if (ws_bytes < packed_act_ws_bytes(*cfg)) return ETR_ERR_WORKSPACE;
+    }
+    ETR_HIP(launch_packed_act_backward(*cfg, dy, offsets, pre8, pre_up8, d8, dt8, dbias, dbias_up, ws, static_cast<hipStream_t>(stream)));
+    return ETR_OK;
+}
+
+etr_status etr_packed_weight_gradient(const etr_linear_config* cfg, const etr_packed* dt8, const etr_packed* xt8, const int32_t* offsets, void* dw,
+                                void* dw_up, void* stream) {
+    etr_status s = check_linear(cfg);
+    if (s != ETR_OK) return s;
+    const bool glu = cfg->act == ETR_ACT_SWIGLU;
+    if (cfg->rows > (1 << 24)) return ETR_ERR_UNSUPPORTED;           // 32-bit offsets inside a tile's rows, which are as long as an expert has rows
+    if ((s = check_packed(dt8, true)) != ETR_OK || (s = check_packed(xt8, true)) != ETR_OK) return s;
+    ETR_REQUIRE_PTR(dw); ETR_OPTIONAL_PTR(dw_up); ETR_OPTIONAL_PTR(offsets);
+    if (!offsets && cfg->E != 1) return ETR_ERR_NULL;
+    if (glu != (dw_up != nullptr)) return ETR_ERR_NULL;
+    ETR_HIP(launch_packed_weight_gradient(*cfg, *dt8, *xt8, offsets, dw, dw_up, static_cast<hipStream_t>(stream)));
     return ETR_OK;
 }
 

@@ -162,6 +162,27 @@ hipError_t launch_expert_linear_backward(const etr_linear_config& c, const void*
 hipError_t launch_route_backward(const etr_config& c, const void* x, const float* w_emb, const float* score, const float* gate,
                                  const float* dgate, const void* dx_add, void* dx, hipStream_t st);
 
+// pack.hip
+size_t packed_columns_bytes(const etr_pack_config& c);
+size_t packed_columns_scale_bytes(const etr_pack_config& c);
+hipError_t launch_pack_rows(const etr_pack_config& c, const void* x, void* values, void* scales, hipStream_t st);
+hipError_t launch_pack_sorted_rows(const etr_sort_config& c, const void* x, const int32_t* row_of, void* values, void* scales, hipStream_t st);
+hipError_t launch_unpack_rows(const etr_pack_config& c, const void* values, const void* scales, void* y, hipStream_t st);
+// from x, or from `packed`; half: -1, or 0 / 1: which half of a pair of stacks beside each other
+hipError_t launch_pack_columns(const etr_pack_config& c, const void* x, const etr_packed* packed, const int32_t* offsets, int half, void* values,
+                               void* scales, hipStream_t st);
+size_t packed_act_ws_bytes(const etr_linear_config& c);
+hipError_t launch_packed_act_backward(const etr_linear_config& c, const void* dy, const int32_t* offsets, const etr_packed* pre8,
+                                const etr_packed* pre_up8, const etr_packed* d8, const etr_packed* dt8, float* dbias, float* dbias_up,
+                                void* ws, hipStream_t st);
+
+// packed_linear.hip; w: the weights and the up weights; kept: y, a and the up product, packed (each may be null)
+hipError_t launch_packed_linear(const etr_linear_config& c, const etr_packed& x, const int32_t* offsets, const etr_packed* const w[2],
+                                 const float* bias, const float* bias_up, const void* residual, void* y,
+                                 const etr_packed* const kept[3], hipStream_t st);
+hipError_t launch_packed_weight_gradient(const etr_linear_config& c, const etr_packed& dt, const etr_packed& xt, const int32_t* offsets, void* dw,
+                                   void* dw_up, hipStream_t st);
+
 // Host-side launch helpers (api.hip).  Both remember their answer per device, so a steady-state call issues no
 // runtime call besides its launches.
 //   cu_count            compute units of the current device (256 if the query fails)

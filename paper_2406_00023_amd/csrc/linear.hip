@@ -14,7 +14,9 @@
 #include <algorithm>
 #include <cmath>
 
+#include "activation.h"
 #include "row_ops.h"
+#include "tiles.h"
 
 namespace etr {
 namespace {
@@ -22,8 +24,6 @@ namespace {
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((address_space(3))) void* lds_ptr;
-
-enum Product { FORWARD = 0, INPUT = 1, WEIGHT = 2 };     // y, dx, dw
 
 struct LinearParams {
     const void* A[2]; const void* B[2];                  // second: SwiGLU (FORWARD: B; INPUT: both; WEIGHT: A)
@@ -55,108 +55,8 @@ constexpr int kPatch = 4096;                             // LDS of a wave's epil
 // s_waitcnt: at most n vector memory operations outstanding, the others as they are
 template <int N> __device__ __forceinline__ void wait_copies() { __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0F70); }
 
-// Rows of the groups, one group per lane (E <= 64): first row, number, and the row tiles before it.
-struct Groups {
-    int first, count, tiles_incl, tiles;
-    __device__ __forceinline__ void load(const LinearParams& p, int BM) {
-        const int lane = threadIdx.x & 63;
-        first = 0; count = 0;
-        if (lane < p.E) {
-            first = p.offsets ? min(max(p.offsets[lane], 0), p.rows) : 0;
-            const int end = p.offsets ? min(max(p.offsets[lane + 1], first), p.rows) : p.rows;
-            count = end - first;
-        }
-        tiles = (count + BM - 1) / BM;
-        tiles_incl = wave_scan_incl(tiles);
-    }
-};
-
-// count: rows of the group; limit: the tile stores rows below it; half: WEIGHT with SwiGLU, which of the two outputs
-struct Tile { int e, first, m0, n0, count, limit, half; };
-
-// The tile list: groups one after the other; inside a group bands of 8 row tiles, in a band the row tiles of a column tile next to
-// each other.  Each XCD (workgroups go round them) has an equal contiguous part of the list, so its 32 CUs work on some 8 x 4 tiles at
-// once and share 8 + 4 operand slabs in its L2.
-// SPLIT (large tiles, one workgroup to a CU): where the last round over an XCD's CUs would keep half of them or fewer busy, its tiles go in
-// halves or quarters of their rows to as many workgroups.
-template <int MODE, bool SPLIT>
-__device__ __forceinline__ bool find_tile(const LinearParams& p, const Groups& g, int BM, int BN, int bid, int grid, int j, Tile& t) {
-    int total, MTw = 0;
-    if (MODE == WEIGHT) {
-        MTw = (p.M + BM - 1) / BM;
-        total = p.E * MTw * (p.glu ? 2 : 1) * p.NT;
-    } else {
-        total = __builtin_amdgcn_readlane(g.tiles_incl, 63) * p.NT;
-    }
-    const int share = (total + 7) >> 3;
-    int part = 0, parts_log = 0;
-    if constexpr (SPLIT) {
-        const int W = grid >> 3, full = share / W * W, rest = share - full;
-        if (j >= full) {
-            parts_log = rest * 4 <= W ? 2 : rest * 2 <= W ? 1 : 0;
-            part = (j - full) & ((1 << parts_log) - 1);
-            j = full + ((j - full) >> parts_log);
-        }
-    }
-    const int q = (bid & 7) * share + j;
-    if (j >= share || q >= total) return false;
-    int in, rows;
-    if (MODE == WEIGHT) {
-        rows = MTw * (p.glu ? 2 : 1);
-        t.e = q / (rows * p.NT);
-        in = q - t.e * (rows * p.NT);
-    } else {
-        t.e = __builtin_ctzll(__ballot(g.tiles_incl * p.NT > q));
-        rows = __builtin_amdgcn_readlane(g.tiles, t.e);
-        in = q - (__builtin_amdgcn_readlane(g.tiles_incl, t.e) - rows) * p.NT;
-    }
-    const int band = in / (8 * p.NT), in_band = in - band * 8 * p.NT, height = min(8, rows - band * 8);
-    const int nt = in_band / height, mt = band * 8 + in_band - nt * height;
-    t.first = __builtin_amdgcn_readlane(g.first, t.e);
-    t.count = __builtin_amdgcn_readlane(g.count, t.e);
-    t.half = MODE == WEIGHT && mt >= MTw ? 1 : 0;
-    t.m0 = (mt - t.half * MTw) * BM;
-    t.n0 = nt * BN;
-    t.limit = MODE == WEIGHT ? p.M : t.count;
-    if (SPLIT && parts_log) {                            // (a part past the last row stores nothing: it stays at the tile's start)
-        const int height = BM >> parts_log, m0 = t.m0 + part * height;
-        t.limit = m0 < t.limit ? min(t.limit, m0 + height) : t.m0;
-        t.m0 = t.limit > t.m0 ? m0 : t.m0;
-    }
-    return true;
-}
-
 // ---- epilogue --------------------------------------------------------------------------------------------------------
 
-// Activations by the hardware's exponential of 2 and reciprocal, an ulp each.  What costs more is the exponent, whose rounding the exponential
-// magnifies (at |a| = 80 to 63 half steps of fp32, 208 in the distribution function at 12).  Results that are rounded to bf16 do not
-// show it; for fp32 the exponent keeps its lower part l, as 2^(t + l) = 2^t (1 + l ln 2): 4 and 9 half steps.  (The bounds keep an infinite
-// exponent's lower part from being no number; exponentials are 0 or infinite there already.)
-__device__ __forceinline__ float exp_f32(float v) {                   // e^v
-    v = fminf(fmaxf(v, -150.f), 150.f);
-    const float t = v * 1.44269504f, l = fmaf(v, 1.44269504f, -t) + v * 1.92596303e-8f;
-    return __builtin_amdgcn_exp2f(t) * fmaf(l, 0.693147181f, 1.0f);
-}
-__device__ __forceinline__ float gaussian_f32(float a) {              // e^(-a^2 / 2)
-    a = fminf(fabsf(a), 20.f);
-    const float q = a * a, t = q * 0.721347520f, l = fmaf(q, 0.721347520f, -t) + fmaf(fmaf(a, a, -q), 0.721347520f, q * 9.62981517e-9f);
-    return __builtin_amdgcn_exp2f(-t) * fmaf(l, -0.693147181f, 1.0f);
-}
-template <bool BF16>
-__device__ __forceinline__ float sigmoid(float a) { return __builtin_amdgcn_rcpf(1.0f + (BF16 ? __expf(-a) : exp_f32(-a))); }
-// The normal distribution function: Phi(-|a|) = u Q(u) exp(-a^2 / 2), u = 1 / (1 + 0.297 |a|) (1 + 0.42 x for x = |a| / sqrt 2), Q of degree 7
-// fitted to the least relative error over |a| <= 13.4 (1.7e-7; with fp32's roundings 5.4e-7).  12825 rows, 192 x 7744 in bf16: 108 us; with a
-// fit of erfc's logarithm of degree 9 (1.2e-7) 120.  No branch, where erff has two and keeps every value of a tile alive across them (789
-// spilled registers).
-template <bool BF16>
-__device__ __forceinline__ float normal_cdf(float a) {
-    const float u = __builtin_amdgcn_rcpf(fmaf(0.29698485f, fabsf(a), 1.0f)), x = a * 0.84932180f;         // x^2 = a^2 / 2 log2 e
-    float s = fmaf(0.0351077948f, u, -0.160095614f);
-    s = fmaf(s, u, 0.220279561f); s = fmaf(s, u, -0.0652102044f); s = fmaf(s, u, 0.134342835f);
-    s = fmaf(s, u, 0.0973718593f); s = fmaf(s, u, 0.119791471f); s = fmaf(s, u, 0.118412214f);
-    const float tail = s * (u * (BF16 ? __builtin_amdgcn_exp2f(-x * x) : gaussian_f32(a)));
-    return a < 0.f ? tail : 1.0f - tail;
-}
 template <bool BF16>
 __device__ __forceinline__ void load4(const void* p, uint32_t at, float (&f)[4]) {
     if constexpr (BF16) {

@@ -1,0 +1,471 @@
+// Packing into 8 bits and back: rows, tokens through the tables of the sorted rows, columns (from either form), and the element-wise
+// part of the products' backward, which packs its results both ways.
+//   scale = the smallest power of two by which the largest finite magnitude of a block of 128 comes to 448 or less; q = e4m3(x / scale)
+// All of it is bound by memory.  The division is by a power of two, so that it is exact, and the result the same in any arithmetic.
+#include <algorithm>
+
+#include "activation.h"
+#include "packed.h"
+
+namespace etr {
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / kWave;
+
+// ---- along rows ------------------------------------------------------------------------------------------------------
+//
+// A wave takes 512 columns at a time, 8 to a lane: sixteen lanes hold a block, and the four blocks' scales are one dword.
+struct RowsParams {
+    const void* x; uint8_t* q; uint32_t* s;             // unpack: q, s in, y out
+    void* y;
+    const int32_t* row_of;
+    int rows, k;            // rows in; pack of tokens: rows of x, and k rows of the result for each
+    int out_rows;           // rows of the packed matrix (the stride of its scales)
+    int K, blocks, groups;
+    int parts;              // of a row, each a wave's
+};
+constexpr int kSteps = 4;                                // of 512 columns that a wave has on their way at once
+
+template <bool BF16>
+__device__ __forceinline__ void load8(const void* x, size_t at, float (&f)[8]) {
+    if constexpr (BF16) {
+        Piece<true>::unpack(*reinterpret_cast<const piece_t*>(static_cast<const uint16_t*>(x) + at), f);
+    } else {
+        Piece<false>::unpack(*reinterpret_cast<const piece_t*>(static_cast<const float*>(x) + at), f);
+        Piece<false>::unpack(*reinterpret_cast<const piece_t*>(static_cast<const float*>(x) + at + 4), f + 4);
+    }
+}
+template <bool BF16>
+__device__ __forceinline__ void store8(void* y, size_t at, const float (&f)[8]) {
+    if constexpr (BF16) {
+        *reinterpret_cast<piece_t*>(static_cast<uint16_t*>(y) + at) = Piece<true>::pack(f);
+    } else {
+        *reinterpret_cast<piece_t*>(static_cast<float*>(y) + at) = Piece<false>::pack(f);
+        *reinterpret_cast<piece_t*>(static_cast<float*>(y) + at + 4) = Piece<false>::pack(f + 4);
+    }
+}
+
+template <bool BF16, bool TOKENS>
+__global__ __launch_bounds__(kThreads) void pack_rows_kernel(RowsParams p, int matrices) {
+    const int lane = threadIdx.x & 63;
+    const long long units = static_cast<long long>(p.rows) * matrices * p.parts;
+    for (long long unit = static_cast<long long>(blockIdx.x) * kWaves + (threadIdx.x >> 6); unit < units; unit += static_cast<long long>(gridDim.x) * kWaves) {
+        const long long row = unit / p.parts;
+        const int g0 = static_cast<int>(unit - row * p.parts) * kSteps;
+        float f[kSteps][8];
+#pragma unroll
+        for (int u = 0; u < kSteps; ++u) {
+            const int c = (g0 + u) * 512 + lane * 8;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[u][i] = 0.f;
+            if (c < p.K) load8<BF16>(p.x, static_cast<size_t>(row) * p.K + c, f[u]);
+        }
+        int mine = -1;
+        if constexpr (TOKENS) {
+            mine = lane < p.k ? p.row_of[row * p.k + lane] : -1;
+            if (mine >= p.out_rows) mine = -1;
+        }
+        uint2 q[kSteps];
+        uint32_t s[kSteps];
+#pragma unroll
+        for (int u = 0; u < kSteps; ++u) {
+            float top = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, finite_abs(f[u][i]));
+            const uint32_t byte = scale_byte(row16_max(top));
+            const float inverse = scale_inverse(byte);
+            q[u].x = to_e4m3(f[u][0] * inverse, f[u][1] * inverse, f[u][2] * inverse, f[u][3] * inverse);
+            q[u].y = to_e4m3(f[u][4] * inverse, f[u][5] * inverse, f[u][6] * inverse, f[u][7] * inverse);
+            s[u] = 0;
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+                s[u] |= ((g0 + u) * 4 + b < p.blocks ? static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(byte), 16 * b)) : 127u) << (8 * b);
+        }
+        auto put = [&](size_t values, size_t scales, size_t stride) {
+#pragma unroll
+            for (int u = 0; u < kSteps; ++u) {
+                const int c = (g0 + u) * 512 + lane * 8;
+                if (c < p.blocks * kBlock) *reinterpret_cast<uint2*>(p.q + values + c) = q[u];
+                if (g0 + u < p.groups && lane == 0) p.s[scales + static_cast<size_t>(g0 + u) * stride] = s[u];
+            }
+        };
+        if constexpr (TOKENS) {
+            for (int j = 0; j < p.k; ++j) {
+                const int r = __builtin_amdgcn_readlane(mine, j);
+                if (r >= 0) put(static_cast<size_t>(r) * p.blocks * kBlock, r, p.out_rows);
+            }
+        } else {
+            const long long matrix = row / p.rows, r = row - matrix * p.rows;
+            put(static_cast<size_t>(row) * p.blocks * kBlock, static_cast<size_t>(matrix) * p.groups * p.rows + r, p.rows);
+        }
+    }
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void unpack_rows_kernel(RowsParams p, int matrices) {
+    const int lane = threadIdx.x & 63;
+    const long long units = static_cast<long long>(p.rows) * matrices * p.parts;
+    for (long long unit = static_cast<long long>(blockIdx.x) * kWaves + (threadIdx.x >> 6); unit < units; unit += static_cast<long long>(gridDim.x) * kWaves) {
+        const long long row = unit / p.parts, matrix = row / p.rows, r = row - matrix * p.rows;
+        const int g0 = static_cast<int>(unit - row * p.parts) * kSteps;
+        uint2 q[kSteps];
+        uint32_t s[kSteps];
+#pragma unroll
+        for (int u = 0; u < kSteps; ++u) {
+            const int c = (g0 + u) * 512 + lane * 8;
+            q[u] = make_uint2(0u, 0u);
+            s[u] = 0;
+            if (c < p.K) {
+                q[u] = *reinterpret_cast<const uint2*>(p.q + static_cast<size_t>(row) * p.blocks * kBlock + c);
+                s[u] = p.s[(static_cast<size_t>(matrix) * p.groups + g0 + u) * p.rows + r];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kSteps; ++u) {
+            const int c = (g0 + u) * 512 + lane * 8;
+            const float scale = scale_value((s[u] >> (8 * (lane >> 4))) & 255u);
+            float f[8];
+            from_e4m3(q[u].x, f);
+            from_e4m3(q[u].y, f + 4);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] *= scale;
+            if (c < p.K) store8<BF16>(p.y, static_cast<size_t>(row) * p.K + c, f);
+        }
+    }
+}
+
+// ---- tiles of 128 rows and 128 columns: along columns, and both ways ----------------------------------------------------
+//
+// A thread has eight neighbouring columns of eight neighbouring rows.  A row's largest is found in the sixteen lanes that have it, a
+// column's over a wave's 32 rows and then, through LDS, over the four waves.  Values along columns go through LDS too, 8 rows of a
+// column at a time, so that they leave as 128 bytes of a column.
+enum Source { FROM_F32 = 0, FROM_BF16 = 1, FROM_PACKED = 2 };
+
+struct TileParams {
+    const void* x;                                       // the matrix, or dy
+    const uint8_t* q[2]; const uint32_t* s[2];           // a matrix packed along rows; or the packed pre-activations
+    const int32_t* offsets;
+    int rows, E, K, stacked;                             // rows: of each matrix of a stack, or of all
+    int act;                                             // ETR_ACT_NONE: the values as they are
+    uint8_t* row_q; uint8_t* row_s; int row_pitch;       // along rows: out, optional
+    uint8_t* column_q; uint8_t* column_s; int column_rows;   // along columns: out, optional; rows of a segment's matrix
+    int half_blocks;                                     // > 0: a pair of stacks beside each other: blocks of 128 rows to a half
+    int half;                                            // which of the two
+    float* part; int chunks;                             // column sums of every chunk, optional
+    float* sums[2];                                      // where no expert has more than a chunk: the sums of an expert
+};
+
+struct TileLds {
+    float top[kWaves][kBlock];
+    uint2 column[kBlock][16];                            // [column][8 rows each], the eights of a column in the order o ^ (column / 8)
+};
+
+// Packs a tile v[row][column] (rows 8 rg + i, columns 8 cg + j of it) along columns.
+// block: the block of rows, `last` if its matrix has no more; values: the matrix's first byte; pitch: bytes of its rows;
+// scales: its first byte of scales; c0: the tile's first column, limit: its columns; matrix_rows: rows of the packed matrix;
+// base: row of the packed matrix that column 0 is
+__device__ __forceinline__ void pack_tile_columns(const float (&v)[8][8], TileLds& lds, uint8_t* values, size_t pitch, uint8_t* scales, int block, bool last,
+                                                  int c0, int limit, int matrix_rows, int base) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, cg = lane & 15, rg = tid >> 4;
+    float top[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        top[j] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top[j] = fmaxf(top[j], finite_abs(v[i][j]));
+        top[j] = fmaxf(top[j], __shfl_xor(top[j], 16));
+        top[j] = fmaxf(top[j], __shfl_xor(top[j], 32));
+    }
+    __syncthreads();                                     // (an earlier tile's reads are done)
+    if (lane < 16) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) lds.top[wave][cg * 8 + j] = top[j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int c = cg * 8 + j;
+        float t = lds.top[0][c];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) t = fmaxf(t, lds.top[w][c]);
+        const uint32_t byte = scale_byte(t);
+        const float inverse = scale_inverse(byte);
+        uint2 q;
+        q.x = to_e4m3(v[0][j] * inverse, v[1][j] * inverse, v[2][j] * inverse, v[3][j] * inverse);
+        q.y = to_e4m3(v[4][j] * inverse, v[5][j] * inverse, v[6][j] * inverse, v[7][j] * inverse);
+        lds.column[c][rg ^ cg] = q;
+        if (rg == 0 && c0 + c < limit) {
+            uint8_t* at = scales + (static_cast<size_t>(block >> 2) * matrix_rows + base + c0 + c) * 4;
+            at[block & 3] = static_cast<uint8_t>(byte);
+            if (last)
+                for (int b = (block & 3) + 1; b < 4; ++b) at[b] = 127;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const int c = u * 32 + (tid >> 3), piece = tid & 7;
+        const uint2 lo = lds.column[c][(2 * piece) ^ (c >> 3)], hi = lds.column[c][(2 * piece + 1) ^ (c >> 3)];
+        if (c0 + c < limit)
+            *reinterpret_cast<piece_t*>(values + static_cast<size_t>(base + c0 + c) * pitch + static_cast<size_t>(block) * kBlock + piece * 16) = piece_t{lo.x, lo.y, hi.x, hi.y};
+    }
+}
+
+// Packs the same tile along rows.  first: the tile's first row of the packed matrix; n_rows: its rows; block: its block of columns
+__device__ __forceinline__ void pack_tile_rows(const float (&v)[8][8], uint8_t* values, size_t pitch, uint8_t* scales, int block, bool last, size_t first, int n_rows,
+                                               int matrix_rows) {
+    const int cg = threadIdx.x & 15, rg = threadIdx.x >> 4;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float top = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, finite_abs(v[i][j]));
+        const uint32_t byte = scale_byte(row16_max(top));
+        const float inverse = scale_inverse(byte);
+        if (rg * 8 + i < n_rows) {
+            const size_t row = first + rg * 8 + i;
+            *reinterpret_cast<uint2*>(values + row * pitch + static_cast<size_t>(block) * kBlock + cg * 8) =
+                make_uint2(to_e4m3(v[i][0] * inverse, v[i][1] * inverse, v[i][2] * inverse, v[i][3] * inverse),
+                           to_e4m3(v[i][4] * inverse, v[i][5] * inverse, v[i][6] * inverse, v[i][7] * inverse));
+            if (cg == 0) {
+                uint8_t* at = scales + (static_cast<size_t>(block >> 2) * matrix_rows + row) * 4;
+                at[block & 3] = static_cast<uint8_t>(byte);
+                if (last)
+                    for (int b = (block & 3) + 1; b < 4; ++b) at[b] = 127;
+            }
+        }
+    }
+}
+
+// Column sums of a tile, in a fixed order: a thread's rows, the wave's, the waves'.
+__device__ __forceinline__ void tile_sums(const float (&v)[8][8], TileLds& lds, float* out, int c0, int limit) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, cg = lane & 15;
+    float sum[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        sum[j] = ((v[0][j] + v[1][j]) + (v[2][j] + v[3][j])) + ((v[4][j] + v[5][j]) + (v[6][j] + v[7][j]));
+        sum[j] += __shfl_xor(sum[j], 16);
+        sum[j] += __shfl_xor(sum[j], 32);
+    }
+    __syncthreads();
+    if (lane < 16) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) lds.top[wave][cg * 8 + j] = sum[j];
+    }
+    __syncthreads();
+    if (tid < kBlock && c0 + tid < limit) out[c0 + tid] = (lds.top[0][tid] + lds.top[1][tid]) + (lds.top[2][tid] + lds.top[3][tid]);
+}
+
+template <int SOURCE>
+__device__ __forceinline__ void load_source(const TileParams& p, int which, size_t matrix_scales, size_t row, size_t scale_row, int matrix_rows, int c, float (&f)[8]) {
+    if constexpr (SOURCE == FROM_PACKED) {
+        const int pitch = blocks_of(p.K) * kBlock;
+        const uint2 q = *reinterpret_cast<const uint2*>(p.q[which] + row * pitch + c);
+        const uint32_t s = p.s[which][matrix_scales + static_cast<size_t>(c >> 9) * matrix_rows + scale_row];
+        const float scale = scale_value((s >> (8 * ((c >> 7) & 3))) & 255u);
+        from_e4m3(q.x, f);
+        from_e4m3(q.y, f + 4);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] *= scale;
+    } else {
+        load8<SOURCE == FROM_BF16>(p.x, row * p.K + c, f);
+    }
+}
+
+// ACT: dy in `x`, the packed pre-activations in q and s
+template <int SOURCE, bool ACT>
+__global__ __launch_bounds__(kThreads, 2) void pack_tiles_kernel(TileParams p) {
+    __shared__ TileLds lds;
+    const int tid = threadIdx.x, cg = tid & 15, rg = tid >> 4;
+    Segments g;
+    g.load(p.offsets, p.rows, p.E, p.stacked);
+    const bool direct = p.sums[0] != nullptr;            // a workgroup to an expert, which has 128 rows at most
+    const int per_half = blocks_of(p.K), nb = blockIdx.x % per_half, chunk = blockIdx.x / per_half, c0 = nb * kBlock, c = c0 + cg * 8;
+    if (!direct && chunk >= __builtin_amdgcn_readlane(g.blocks_incl, 63)) return;
+    const int e = direct ? chunk : __builtin_ctzll(__ballot(g.blocks_incl > chunk));
+    const int blocks = __builtin_amdgcn_readlane(g.blocks, e), blocks_before = __builtin_amdgcn_readlane(g.blocks_incl, e) - blocks;
+    const int groups_before = __builtin_amdgcn_readlane(g.groups_incl, e) - __builtin_amdgcn_readlane(g.groups, e);
+    const int block = direct ? 0 : chunk - blocks_before;
+    const int n_rows = min(kBlock, __builtin_amdgcn_readlane(g.count, e) - block * kBlock);
+    const size_t first = static_cast<size_t>(__builtin_amdgcn_readlane(g.first, e)) + static_cast<size_t>(block) * kBlock;
+    const bool nothing = direct && n_rows <= 0;          // an expert without rows: zeros for its sums, and no block
+    const int n_halves = ACT && p.act == ETR_ACT_SWIGLU ? 2 : 1;
+
+    float v[8][8];
+    // (both halves load anew: the second time from the caches)
+    for (int h = 0; h < n_halves; ++h) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const bool in = rg * 8 + i < n_rows && c < p.K;
+            const size_t row = first + rg * 8 + i;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+            if (!in) continue;
+            if constexpr (SOURCE == FROM_PACKED) {
+                // a stack's matrices have scales of their own
+                const size_t matrix_scales = p.stacked ? static_cast<size_t>(e) * scale_groups_of(p.K) * p.rows : 0;
+                load_source<FROM_PACKED>(p, 0, matrix_scales, row, p.stacked ? row - static_cast<size_t>(e) * p.rows : row, p.rows, c, v[i]);
+            } else {
+                load_source<SOURCE>(p, 0, 0, row, row, p.rows, c, v[i]);
+            }
+            if constexpr (ACT) {
+                float a[8], b[8];
+                load_source<FROM_PACKED>(p, 0, 0, row, row, p.rows, c, a);
+                if (p.act == ETR_ACT_SWIGLU && h == 0) load_source<FROM_PACKED>(p, 1, 0, row, row, p.rows, c, b);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if (p.act == ETR_ACT_GELU) {
+                        v[i][j] *= normal_cdf<false>(a[j]) + a[j] * 0.39894228040143268f * gaussian_f32(a[j]);
+                    } else {
+                        const float sg = sigmoid<false>(a[j]);
+                        if (h) v[i][j] *= a[j] * sg;
+                        else v[i][j] *= (p.act == ETR_ACT_SWIGLU ? b[j] : 1.0f) * (sg * (1.0f + a[j] * (1.0f - sg)));
+                    }
+                }
+            }
+        }
+        if (p.row_q && !nothing) {
+            pack_tile_rows(v, p.row_q, p.row_pitch, p.row_s, h * per_half + nb, h == n_halves - 1 && nb == per_half - 1, first, n_rows, p.rows);
+        }
+        if (p.part || direct) {
+            float* out = direct ? p.sums[h] + static_cast<size_t>(e) * p.K : p.part + (static_cast<size_t>(h) * p.chunks + chunk) * p.K;
+            tile_sums(v, lds, out, c0, p.K);
+        }
+        if (p.column_q && !nothing) {
+            if (p.half_blocks) {                         // a pair of stacks: the matrix has 2 half_blocks blocks
+                const int all = 2 * p.half_blocks, at = p.half * p.half_blocks + block;
+                pack_tile_columns(v, lds, p.column_q + static_cast<size_t>(e) * p.K * all * kBlock, static_cast<size_t>(all) * kBlock,
+                                  p.column_s + static_cast<size_t>(e) * ((all + 3) / 4) * p.K * 4, at, at == all - 1, c0, p.K, p.K, 0);
+            } else {
+                pack_tile_columns(v, lds, p.column_q + static_cast<size_t>(blocks_before) * kBlock * p.column_rows, static_cast<size_t>(blocks) * kBlock,
+                                  p.column_s + static_cast<size_t>(groups_before) * 4 * p.column_rows, block, block == blocks - 1, c0, p.K, p.column_rows,
+                                  h * p.K);
+            }
+        }
+    }
+}
+
+// dbias[e][n]: the chunks of expert e, sixteen groups of them side by side, in a fixed order
+__global__ __launch_bounds__(1024) void join_sums_kernel(TileParams p, float* dbias, float* dbias_up) {
+    __shared__ float sums[16][64];
+    Segments g;
+    g.load(p.offsets, p.rows, p.E, false);
+    const int e = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.x * 64 + lane;
+    const int blocks = __builtin_amdgcn_readlane(g.blocks, e), begin = __builtin_amdgcn_readlane(g.blocks_incl, e) - blocks;
+    const float* part = p.part + static_cast<size_t>(blockIdx.z) * p.chunks * p.K;
+    float s = 0.f;
+    if (n < p.K) {
+#pragma unroll 4
+        for (int i = wave; i < blocks; i += 16) s += part[static_cast<size_t>(begin + i) * p.K + n];
+    }
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave > 0 || n >= p.K) return;
+    s = 0.f;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) s += sums[w][lane];
+    (blockIdx.z ? dbias_up : dbias)[static_cast<size_t>(e) * p.K + n] = s;
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+
+RowsParams rows_params(int rows, int K) {
+    RowsParams p{};
+    p.rows = p.out_rows = rows;
+    p.K = K; p.blocks = blocks_of(K); p.groups = scale_groups_of(K);
+    p.parts = (p.groups + kSteps - 1) / kSteps;
+    return p;
+}
+dim3 rows_grid(const RowsParams& p, int matrices) {
+    const long long units = static_cast<long long>(p.rows) * matrices * p.parts;
+    return dim3(static_cast<unsigned>(std::min<long long>((units + kWaves - 1) / kWaves, 1 << 20)));
+}
+int chunks_at_most(int rows, int E, bool stacked) { return stacked ? E * blocks_of(rows) : rows / kBlock + std::min(E, rows); }
+
+template <int SOURCE, bool ACT>
+hipError_t launch_tiles(const TileParams& p, int chunks, hipStream_t st) {
+    hipLaunchKernelGGL((pack_tiles_kernel<SOURCE, ACT>), dim3(static_cast<unsigned>(blocks_of(p.K)) * chunks), dim3(kThreads), 0, st, p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t packed_columns_bytes(const etr_pack_config& c) {
+    if (!c.sorted) return packed_bytes(static_cast<size_t>(c.E) * c.K, c.rows);
+    return static_cast<size_t>(c.K) * kBlock * (c.rows / kBlock + std::min(c.E, c.rows));
+}
+size_t packed_columns_scale_bytes(const etr_pack_config& c) {
+    if (!c.sorted) return scale_bytes(static_cast<size_t>(c.E) * c.K, c.rows);
+    return static_cast<size_t>(c.K) * 4 * (c.rows / (4 * kBlock) + std::min(c.E, c.rows));
+}
+
+hipError_t launch_pack_rows(const etr_pack_config& c, const void* x, void* values, void* scales, hipStream_t st) {
+    RowsParams p = rows_params(c.rows, c.K);
+    const int matrices = c.sorted ? 1 : c.E;
+    p.x = x; p.q = static_cast<uint8_t*>(values); p.s = static_cast<uint32_t*>(scales);
+    if (c.dtype == ETR_BF16) hipLaunchKernelGGL((pack_rows_kernel<true, false>), rows_grid(p, matrices), dim3(kThreads), 0, st, p, matrices);
+    else hipLaunchKernelGGL((pack_rows_kernel<false, false>), rows_grid(p, matrices), dim3(kThreads), 0, st, p, matrices);
+    return hipGetLastError();
+}
+
+hipError_t launch_pack_sorted_rows(const etr_sort_config& c, const void* x, const int32_t* row_of, void* values, void* scales, hipStream_t st) {
+    RowsParams p = rows_params(c.T, c.d);
+    p.k = c.k; p.out_rows = c.T * c.k; p.row_of = row_of;
+    p.x = x; p.q = static_cast<uint8_t*>(values); p.s = static_cast<uint32_t*>(scales);
+    if (c.dtype == ETR_BF16) hipLaunchKernelGGL((pack_rows_kernel<true, true>), rows_grid(p, 1), dim3(kThreads), 0, st, p, 1);
+    else hipLaunchKernelGGL((pack_rows_kernel<false, true>), rows_grid(p, 1), dim3(kThreads), 0, st, p, 1);
+    return hipGetLastError();
+}
+
+hipError_t launch_unpack_rows(const etr_pack_config& c, const void* values, const void* scales, void* y, hipStream_t st) {
+    RowsParams p = rows_params(c.rows, c.K);
+    const int matrices = c.sorted ? 1 : c.E;
+    p.q = static_cast<uint8_t*>(const_cast<void*>(values)); p.s = static_cast<uint32_t*>(const_cast<void*>(scales)); p.y = y;
+    if (c.dtype == ETR_BF16) hipLaunchKernelGGL(unpack_rows_kernel<true>, rows_grid(p, matrices), dim3(kThreads), 0, st, p, matrices);
+    else hipLaunchKernelGGL(unpack_rows_kernel<false>, rows_grid(p, matrices), dim3(kThreads), 0, st, p, matrices);
+    return hipGetLastError();
+}
+
+hipError_t launch_pack_columns(const etr_pack_config& c, const void* x, const etr_packed* packed, const int32_t* offsets, int half, void* values, void* scales,
+                               hipStream_t st) {
+    TileParams p{};
+    p.x = x;
+    if (packed) { p.q[0] = static_cast<const uint8_t*>(packed->values); p.s[0] = static_cast<const uint32_t*>(packed->scales); }
+    p.offsets = offsets; p.rows = c.rows; p.E = c.E; p.K = c.K; p.stacked = !c.sorted;
+    p.column_q = static_cast<uint8_t*>(values); p.column_s = static_cast<uint8_t*>(scales); p.column_rows = c.K;
+    if (half >= 0) { p.half_blocks = blocks_of(c.rows); p.half = half; }
+    const int chunks = chunks_at_most(c.rows, c.E, p.stacked);
+    if (packed) return launch_tiles<FROM_PACKED, false>(p, chunks, st);
+    return c.dtype == ETR_BF16 ? launch_tiles<FROM_BF16, false>(p, chunks, st) : launch_tiles<FROM_F32, false>(p, chunks, st);
+}
+
+size_t packed_act_ws_bytes(const etr_linear_config& c) {
+    return align_up(static_cast<size_t>(c.act == ETR_ACT_SWIGLU ? 2 : 1) * chunks_at_most(c.rows, c.E, false) * c.N * 4);
+}
+
+hipError_t launch_packed_act_backward(const etr_linear_config& c, const void* dy, const int32_t* offsets, const etr_packed* pre8, const etr_packed* pre_up8,
+                                const etr_packed* d8, const etr_packed* dt8, float* dbias, float* dbias_up, void* ws, hipStream_t st) {
+    const bool glu = c.act == ETR_ACT_SWIGLU, direct = dbias && c.rows <= kBlock;
+    TileParams p{};
+    p.x = dy; p.offsets = offsets; p.rows = c.rows; p.E = c.E; p.K = c.N; p.act = c.act;
+    const etr_packed* pre[2] = {pre8, pre_up8};
+    for (int i = 0; i < 2; ++i)
+        if (pre[i]) { p.q[i] = static_cast<const uint8_t*>(pre[i]->values); p.s[i] = static_cast<const uint32_t*>(pre[i]->scales); }
+    if (d8) {
+        p.row_q = static_cast<uint8_t*>(d8->values); p.row_s = static_cast<uint8_t*>(d8->scales);
+        p.row_pitch = (glu ? 2 : 1) * blocks_of(c.N) * kBlock;
+    }
+    if (dt8) { p.column_q = static_cast<uint8_t*>(dt8->values); p.column_s = static_cast<uint8_t*>(dt8->scales); p.column_rows = (glu ? 2 : 1) * c.N; }
+    p.chunks = chunks_at_most(c.rows, c.E, false);
+    if (direct) { p.sums[0] = dbias; p.sums[1] = dbias_up; }
+    else if (dbias) p.part = static_cast<float*>(ws);
+    const int chunks = direct ? c.E : p.chunks;
+    const bool bf16 = c.dtype == ETR_BF16;
+    hipError_t err = c.act == ETR_ACT_NONE ? (bf16 ? launch_tiles<FROM_BF16, false>(p, chunks, st) : launch_tiles<FROM_F32, false>(p, chunks, st))
+                                           : (bf16 ? launch_tiles<FROM_BF16, true>(p, chunks, st) : launch_tiles<FROM_F32, true>(p, chunks, st));
+    if (err != hipSuccess || !p.part) return err;
+    hipLaunchKernelGGL(join_sums_kernel, dim3((c.N + 63) / 64, c.E, glu ? 2 : 1), dim3(1024), 0, st, p, dbias, dbias_up);
+    return hipGetLastError();
+}
+
+}  // namespace etr

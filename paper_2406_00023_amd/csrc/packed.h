@@ -1,0 +1,82 @@
+// Packed matrices: e4m3 values with a power of two for each block of 128 along the contraction.  Sizes, and the device side of
+// packing one block.
+#pragma once
+
+#include "row_ops.h"
+#include "tiles.h"
+
+namespace etr {
+
+constexpr int kBlock = 128;                              // values that share a scale
+inline __host__ __device__ int blocks_of(int n) { return (n + kBlock - 1) / kBlock; }
+inline __host__ __device__ int scale_groups_of(int n) { return (n + 4 * kBlock - 1) / (4 * kBlock); }   // dwords of scales to a row
+
+// Bytes of matrices of `count` x [rows][K], along rows
+inline size_t packed_bytes(size_t count, int K) { return count * static_cast<size_t>(blocks_of(K)) * kBlock; }
+inline size_t scale_bytes(size_t count, int K) { return count * 4 * static_cast<size_t>(scale_groups_of(K)); }
+
+namespace {
+
+// The byte of the smallest power of two, 2^-127 at least, by which a magnitude comes to 448 = 1.75 x 2^8 or less, and the power's inverse.
+__device__ __forceinline__ uint32_t scale_byte(float top) {
+    const uint32_t bits = __float_as_uint(top);
+    return static_cast<uint32_t>(max(static_cast<int>(bits >> 23) - 8 + ((bits & 0x7FFFFFu) > 0x600000u ? 1 : 0), 0));
+}
+__device__ __forceinline__ float scale_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+// 2^(byte - 127); byte 0 is below the normal numbers
+__device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(byte ? byte << 23 : 0x400000u); }
+// magnitude that takes part in a block's largest: NaN and infinities have none
+__device__ __forceinline__ float finite_abs(float v) { return fabsf(v) < __builtin_inff() ? fabsf(v) : 0.f; }
+// four values, lowest byte first.  (An infinity stays one under any power, and is converted to NaN, as NaN is; what is finite is 448 at most.)
+__device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d) {
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true));
+}
+__device__ __forceinline__ void from_e4m3(uint32_t v, float* f) {
+    f[0] = __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(v), 0); f[1] = __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(v), 1);
+    f[2] = __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(v), 2); f[3] = __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(v), 3);
+}
+
+// Largest over the 16 lanes of a row of lanes, in all of them.  All lanes active.
+__device__ __forceinline__ float row16_max(float v) {
+    auto dpp = [](float x, auto ctrl) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xF, 0xF, true));
+    };
+    v = fmaxf(v, dpp(v, std::integral_constant<int, 0xB1>{}));       // quad swap 1
+    v = fmaxf(v, dpp(v, std::integral_constant<int, 0x4E>{}));       // quad swap 2
+    v = fmaxf(v, dpp(v, std::integral_constant<int, 0x141>{}));      // half-row mirror
+    return fmaxf(v, dpp(v, std::integral_constant<int, 0x140>{}));   // row mirror
+}
+
+// Rows of the groups, one group per lane, for operands whose groups lie one behind the other: the offsets' running maximum, so that
+// the groups' rows are `rows` in all whatever the offsets say.  blocks: of 128 rows, a last one in part; groups: of four blocks, whose scales
+// are a dword; _incl: those of the groups before and of this one.
+struct Segments {
+    int first, count, blocks, blocks_incl, groups, groups_incl;
+    __device__ __forceinline__ void load(const int32_t* offsets, int rows, int E, bool stacked) {
+        const int lane = threadIdx.x & 63;
+        int end = 0;
+        if (stacked) {
+            first = lane < E ? lane * rows : 0;
+            count = lane < E ? rows : 0;
+        } else {
+            int begin = lane < E && offsets ? min(max(offsets[lane], 0), rows) : 0;
+            end = lane < E ? (offsets ? min(max(offsets[lane + 1], 0), rows) : rows) : 0;
+#pragma unroll
+            for (int s = 1; s < 64; s <<= 1) {
+                const int a = __shfl_up(begin, s), b = __shfl_up(end, s);
+                if (lane >= s) { begin = max(begin, a); end = max(end, b); }
+            }
+            end = max(begin, end);
+            first = begin;
+            count = lane < E ? end - begin : 0;
+        }
+        blocks = (count + kBlock - 1) / kBlock;
+        groups = (blocks + 3) / 4;
+        blocks_incl = wave_scan_incl(blocks);
+        groups_incl = wave_scan_incl(groups);
+    }
+};
+
+}  // namespace
+}  // namespace etr

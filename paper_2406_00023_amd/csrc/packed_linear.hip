@@ -1,0 +1,636 @@
+// The experts' products of packed operands (e4m3 values, a power of two per block of 128 along the contraction), with bias, activation,
+// residual and packing of the results in the epilogue, and the gradient of their weights.
+//   forward  y[r][n] = act(sum_k x[r][k] w[e][n][k] + bias[e][n]) + residual[r][n]       (dx is this product too, of weights along columns)
+//   weights  dw[e][n][k] = sum_r da[r][n] x[r][k]                                        both operands along columns
+// Every operand is rows of whole 128-byte blocks, padded with zeros, so that every product is C[m][n] = sum_k A(m, k) B(n, k) with both
+// contractions contiguous, and a k-tile is one block: 128 bytes and one scale for each row of a tile.
+// Results in bf16: the scaled MFMA, 32 x 32 x 64 8-bit values, takes the bytes and the scales as they are.  It cuts products off 2^-13 below the
+// largest of some 16 neighbours (measured: 1.5e-5 of a result's size on normal data).  Results in fp32 go without it: the values are
+// converted to bf16, which holds them and their scale exactly, and multiplied there, with sums in fp32 (6e-8).
+#include <algorithm>
+
+#include "activation.h"
+#include "packed.h"
+
+namespace etr {
+namespace {
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) void* lds_ptr;
+
+struct PackedParams {
+    const uint8_t* A; const uint8_t* As;                 // x, or da (and db) along columns
+    const uint8_t* B[2]; const uint8_t* Bs[2];           // the weights (second: up), or x along columns
+    void* C[2];                                          // y (optional), or dw and dw_up
+    uint8_t* P[3]; uint8_t* Ps[3];                       // packed results, optional: y, a, the up product
+    const int32_t* offsets;
+    const float* bias[2];
+    const void* residual;
+    int rows, E;
+    int M, N;                                            // WEIGHT: output rows of each half; output columns
+    int blocks;                                          // FORWARD: k-tiles
+    int act, glu;
+    int NT;                                              // column tiles
+};
+
+// What the copies of one operand need: 64-bit base of a tile's first row in this k-tile, and the buffer bound.
+constexpr uint32_t kRange = 0xFFFFFF00u, kPast = 0xFFFFFF80u;         // an offset past any buffer: such a lane copies zeros
+
+__device__ __forceinline__ v4i descriptor(uint64_t base) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(base));
+    const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(base >> 32));
+    return v4i{static_cast<int>(lo), static_cast<int>(hi & 0xFFFFu), static_cast<int>(kRange), 0x00027000};
+}
+// Copies into LDS, 16 or 4 bytes a lane, lane after lane from `at`.  In assembly, without an output: the compiler would otherwise take every
+// later read of LDS to wait for them; they are waited for by count (wait_copies).
+__device__ __forceinline__ void copy16(v4i from, uint32_t off, uint32_t at) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(from) : "memory");
+}
+__device__ __forceinline__ void copy4(v4i from, uint32_t off, uint32_t at) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(from) : "memory");
+}
+// at most n vector memory operations outstanding, and every read of LDS done
+template <int N> __device__ __forceinline__ void wait_copies() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0070);
+    asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// eight values of a block as bf16, exactly
+__device__ __forceinline__ bf16x8 widen(int lo, int hi, float scale) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// ---- epilogue --------------------------------------------------------------------------------------------------------
+
+template <bool WIDE>
+__device__ __forceinline__ float activate(int act, float a, float up, bool glu) {
+    if (glu) return a * sigmoid<!WIDE>(a) * up;
+    if (act == ETR_ACT_SILU) return a * sigmoid<!WIDE>(a);
+    if (act == ETR_ACT_GELU) return a * normal_cdf<!WIDE>(a);
+    return a;
+}
+template <bool WIDE>
+__device__ __forceinline__ void store4(void* p, size_t at, const float (&f)[4]) {
+    if constexpr (WIDE) {
+        *reinterpret_cast<float4*>(static_cast<float*>(p) + at) = make_float4(f[0], f[1], f[2], f[3]);
+    } else {
+        typedef __attribute__((ext_vector_type(2))) float f32x2;
+        const uint32_t lo = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{f[0], f[1]}, bf16x2));
+        const uint32_t hi = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{f[2], f[3]}, bf16x2));
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + at) = make_uint2(lo, hi);
+    }
+}
+template <bool WIDE>
+__device__ __forceinline__ void load4(const void* p, size_t at, float (&f)[4]) {
+    if constexpr (WIDE) {
+        const float4 v = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
+        f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
+    } else {
+        const uint2 v = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + at);
+        f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xFFFF0000u);
+        f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xFFFF0000u);
+    }
+}
+
+// A lane's results come in runs of four neighbouring columns of one row.  `Runs` says which: MB row places, NR runs each.
+//   acc(i, r): the run as a reference to its four values; row(i): row in the tile; column(r): first output column, in the tile
+// Packing needs the largest of a row's 128 columns: over a lane's runs, over the lanes that share the row (`fold`), and over the
+// waves that share the block, through LDS: tops[wave of the block's waves][row].
+struct PackPlace { uint8_t* values; uint8_t* scales; };
+
+// ---- tiles of 32 x 32 blocks -------------------------------------------------------------------------------------------
+//
+// LDS, an operand of a k-tile: [row][8 pieces of 16 bytes]; the piece at place s of a row is s ^ (row / 2 % 8), so that the rows of a fragment
+// spread over the banks.  Behind both operands their scales, a dword (four k-tiles) for each row.  A fragment's lane has row lane % 32 of its
+// block and 32 of the 64 bytes of half a k-tile; which ones does not matter as long as it is the same for both operands.
+// A workgroup of WM x WN waves has a BM x BN tile at a time; NBUF buffers, of which all but one are on their way.
+// The MFMAs take the columns' fragment first, so that a lane ends up with runs of four neighbouring columns of one row.
+// WIDE: results in fp32.
+template <bool WIDE, int BM, int BN, int WM, int WN, int NBUF, int MODE, bool GLU, bool WALK>
+__global__ __launch_bounds__(WM* WN * 64, 2) void packed_tiles_kernel(PackedParams p) {
+    constexpr int NW = WM * WN, MB = BM / WM / 32, NB = BN / WN / 32, NO = GLU ? NB / 2 : NB;
+    constexpr int OUT_N = GLU ? BN / 2 : BN;
+    constexpr int CA = BM / 8, CB = BN / 8;              // copies of 64 pieces per operand and k-tile
+    constexpr int SA = (BM + 63) / 64, SB = BN / 64;     // copies of 64 scales
+    constexpr int CW = (CA + CB) / NW, SW = (SA + SB + NW - 1) / NW;                        // of a wave
+    constexpr int A_BYTES = BM * 128, TILE_BYTES = (BM + BN) * 128, STAGE = TILE_BYTES + (SA + SB) * 256;
+    constexpr int kColumnWaves = kBlock / (NO * 32);     // waves that share a block of 128 output columns
+    static_assert((CA + CB) % NW == 0 && BN % 64 == 0 && OUT_N % kBlock == 0 && kBlock % (NO * 32) == 0 && (!GLU || NB % 2 == 0), "");
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    float (*tops)[BM] = reinterpret_cast<float (*)[BM]>(lds + NBUF * STAGE);                 // [WN][BM]
+    const int lane = threadIdx.x & 63, l32 = lane & 31, kh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
+    const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr)lds));
+
+    // groups in rows (FORWARD) or in blocks of the contraction (WEIGHT)
+    Segments seg;
+    seg.load(p.offsets, p.rows, p.E, false);
+    Groups groups;
+    groups.first = seg.first; groups.count = seg.count;
+    groups.tiles = (seg.count + BM - 1) / BM;
+    groups.tiles_incl = wave_scan_incl(groups.tiles);
+    Tile t;
+    const int bid = blockIdx.x, grid = gridDim.x;
+    int j = bid >> 3;
+    if (!find_tile<MODE, WALK>(p, groups, BM, OUT_N, bid, grid, j, t)) return;
+
+    // ---- the copy side: a tile and a k-tile of its own, ahead of the products
+    struct Source { uint64_t base[2], up, scales[2], scales_up; size_t stride[2]; uint32_t at[CW], at_s[SW]; int KT, kt; bool empty; };
+    Source s;
+    bool more = true;                                    // s is a tile that is still to be copied
+    auto row_piece = [&](int c) { return (lane & 7) ^ (((8 * c + (lane >> 3)) >> 1) & 7); };
+    auto aim = [&](const Tile& x) {
+        s.kt = 0;
+        uint32_t pitch;
+        int last_a, last_b, halves = p.glu ? 2 : 1;
+        if constexpr (MODE == WEIGHT) {
+            const int blocks = __builtin_amdgcn_readlane(seg.blocks, x.e), before = __builtin_amdgcn_readlane(seg.blocks_incl, x.e) - blocks;
+            const int groups_before = __builtin_amdgcn_readlane(seg.groups_incl, x.e) - __builtin_amdgcn_readlane(seg.groups, x.e);
+            const size_t rows_a = static_cast<size_t>(p.M) * halves;
+            s.empty = blocks == 0;
+            s.KT = max(blocks, 1);
+            pitch = static_cast<uint32_t>(blocks) * kBlock;
+            const size_t row_a = static_cast<size_t>(x.half) * p.M + x.m0;
+            s.base[0] = reinterpret_cast<uint64_t>(p.A) + static_cast<uint64_t>(before) * kBlock * rows_a + row_a * pitch;
+            s.base[1] = reinterpret_cast<uint64_t>(p.B[0]) + static_cast<uint64_t>(before) * kBlock * p.N + static_cast<uint64_t>(x.n0) * pitch;
+            s.scales[0] = reinterpret_cast<uint64_t>(p.As) + (static_cast<uint64_t>(groups_before) * rows_a + row_a) * 4;
+            s.scales[1] = reinterpret_cast<uint64_t>(p.Bs[0]) + (static_cast<uint64_t>(groups_before) * p.N + x.n0) * 4;
+            s.stride[0] = rows_a * 4;
+            s.stride[1] = static_cast<size_t>(p.N) * 4;
+            last_a = p.M - 1 - x.m0;
+        } else {
+            s.empty = false;
+            s.KT = p.blocks;
+            pitch = static_cast<uint32_t>(p.blocks) * kBlock;
+            const uint64_t row_a = static_cast<uint64_t>(x.first) + x.m0, row_b = static_cast<uint64_t>(x.e) * p.N + x.n0;
+            const uint64_t groups_b = static_cast<uint64_t>(x.e) * ((p.blocks + 3) / 4) * p.N + x.n0;
+            s.base[0] = reinterpret_cast<uint64_t>(p.A) + row_a * pitch;
+            s.base[1] = reinterpret_cast<uint64_t>(p.B[0]) + row_b * pitch;
+            s.scales[0] = reinterpret_cast<uint64_t>(p.As) + row_a * 4;
+            s.scales[1] = reinterpret_cast<uint64_t>(p.Bs[0]) + groups_b * 4;
+            s.stride[0] = static_cast<size_t>(p.rows) * 4;
+            s.stride[1] = static_cast<size_t>(p.N) * 4;
+            s.up = GLU ? reinterpret_cast<uint64_t>(p.B[1]) + row_b * pitch : 0;
+            s.scales_up = GLU ? reinterpret_cast<uint64_t>(p.Bs[1]) + groups_b * 4 : 0;
+            last_a = x.count - 1 - x.m0;
+        }
+        last_b = p.N - 1 - x.n0;
+        // (rows past the last one: the last again, whose results are not stored)
+#pragma unroll
+        for (int i = 0; i < CW; ++i) {
+            const int c = wave * CW + i;
+            if (c < CA) {
+                s.at[i] = static_cast<uint32_t>(min(8 * c + (lane >> 3), last_a)) * pitch + row_piece(c) * 16u;
+            } else {
+                const int r = 8 * (c - CA) + (lane >> 3);
+                s.at[i] = static_cast<uint32_t>(min(GLU && r >= BN / 2 ? r - BN / 2 : r, last_b)) * pitch + row_piece(c - CA) * 16u;
+            }
+            if (s.empty) s.at[i] = kPast;
+        }
+#pragma unroll
+        for (int i = 0; i < SW; ++i) {
+            const int c = min(wave + i * NW, SA + SB - 1);
+            if (c < SA) {
+                s.at_s[i] = static_cast<uint32_t>(min(64 * c + lane, last_a)) * 4;
+            } else {
+                const int r = 64 * (c - SA) + lane;
+                s.at_s[i] = static_cast<uint32_t>(min(GLU && r >= BN / 2 ? r - BN / 2 : r, last_b)) * 4;
+            }
+            if (s.empty) s.at_s[i] = kPast;
+        }
+    };
+    auto issue = [&](int buf) {
+        const uint32_t dst = lds0 + buf * STAGE;
+#pragma unroll
+        for (int i = 0; i < CW; ++i) {
+            const int c = wave * CW + i;
+            const uint64_t base = c < CA ? s.base[0] : GLU && c >= CA + CB / 2 ? s.up : s.base[1];
+            copy16(descriptor(base + static_cast<uint64_t>(s.kt) * kBlock), s.at[i], dst + c * 1024);
+        }
+#pragma unroll
+        for (int i = 0; i < SW; ++i) {                   // (waves without one of their own copy the last again)
+            const int c = min(wave + i * NW, SA + SB - 1);
+            const uint64_t base = c < SA ? s.scales[0] : GLU && c >= SA + SB / 2 ? s.scales_up : s.scales[1];
+            copy4(descriptor(base + static_cast<uint64_t>(s.kt >> 2) * s.stride[c < SA ? 0 : 1]), s.at_s[i], dst + TILE_BYTES + c * 256);
+        }
+    };
+    int jn = j;
+    auto advance = [&]() {                               // (a source past the last tile goes on copying its last k-tile)
+        if (!more) return;
+        if (s.kt + 1 < s.KT) { s.kt += 1; return; }
+        jn += grid >> 3;
+        Tile n;
+        if (find_tile<MODE, WALK>(p, groups, BM, OUT_N, bid, grid, jn, n)) aim(n);
+        else more = false;
+    };
+
+    // ---- the product side
+    auto b_block = [&](int jb) { return GLU ? (jb >= NO ? BN / 64 : 0) + wn * NO + (jb >= NO ? jb - NO : jb) : wn * NB + jb; };
+    auto fragment = [&](const unsigned char* op, int block, int half) -> v8i {
+        const int row = block * 32 + l32, x = (row >> 1) & 7;
+        const v4i lo = *reinterpret_cast<const v4i*>(op + row * 128 + ((4 * half + 2 * kh) ^ x) * 16);
+        const v4i hi = *reinterpret_cast<const v4i*>(op + row * 128 + ((4 * half + 2 * kh + 1) ^ x) * 16);
+        return v8i{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    };
+    f32x16 acc[MB][NB];
+    aim(t);
+#pragma unroll
+    for (int b = 0; b < NBUF - 1; ++b) { issue(b); advance(); }
+    int buf = 0;
+    for (;;) {
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+            for (int jb = 0; jb < NB; ++jb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[i][jb][v] = 0.f;
+        const int KT = MODE == WEIGHT ? max(__builtin_amdgcn_readlane(seg.blocks, t.e), 1) : p.blocks;
+        for (int kt = 0; kt < KT; ++kt) {
+            wait_copies<(NBUF - 2) * (CW + SW)>();       // this wave's part of the k-tile has landed
+            barrier();                                   // ... and everybody's; and everybody is done with the buffer before it
+            issue(buf == 0 ? NBUF - 1 : buf - 1);
+            advance();
+            const unsigned char* op = lds + buf * STAGE;
+            const uint32_t* sc = reinterpret_cast<const uint32_t*>(op + TILE_BYTES);
+            const int shift = 8 * (kt & 3);
+            int sa[MB], sb[NB];
+#pragma unroll
+            for (int i = 0; i < MB; ++i) sa[i] = static_cast<int>(sc[(wm * MB + i) * 32 + l32] >> shift) & 255;
+#pragma unroll
+            for (int jb = 0; jb < NB; ++jb) sb[jb] = static_cast<int>(sc[SA * 64 + b_block(jb) * 32 + l32] >> shift) & 255;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                v8i fa[MB], fb[NB];
+#pragma unroll
+                for (int jb = 0; jb < NB; ++jb) fb[jb] = fragment(op + A_BYTES, b_block(jb), half);
+#pragma unroll
+                for (int i = 0; i < MB; ++i) fa[i] = fragment(op, wm * MB + i, half);
+                if constexpr (!WIDE) {
+#pragma unroll
+                    for (int i = 0; i < MB; ++i)
+#pragma unroll
+                        for (int jb = 0; jb < NB; ++jb)
+                            acc[i][jb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[jb], fa[i], acc[i][jb], 0, 0, 0, sb[jb], 0, sa[i]);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        bf16x8 wa[MB], wb[NB];
+#pragma unroll
+                        for (int i = 0; i < MB; ++i) wa[i] = widen(fa[i][2 * q], fa[i][2 * q + 1], scale_value(sa[i]));
+#pragma unroll
+                        for (int jb = 0; jb < NB; ++jb) wb[jb] = widen(fb[jb][2 * q], fb[jb][2 * q + 1], scale_value(sb[jb]));
+#pragma unroll
+                        for (int i = 0; i < MB; ++i)
+#pragma unroll
+                            for (int jb = 0; jb < NB; ++jb) acc[i][jb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[jb], wa[i], acc[i][jb], 0, 0, 0);
+                    }
+                }
+            }
+            buf = buf + 1 == NBUF ? 0 : buf + 1;
+        }
+
+        // ---- the results: lane: row l32 of a block, columns 8 q + 4 kh ... + 3 of it for q = 0 ... 3
+        const int limit = t.limit - t.m0;
+        const int n_wave = t.n0 + wn * NO * 32;          // first output column of the wave
+        const size_t first = (MODE == WEIGHT ? static_cast<size_t>(t.e) * p.M : static_cast<size_t>(t.first)) + t.m0;
+        auto values = [&](int i, int jb, int q, float (&f)[4]) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) f[v] = acc[i][jb][4 * q + v];
+        };
+        // packs blocks j0 ... j0 + NO - 1 of the accumulators
+        auto pack = [&](uint8_t* to, uint8_t* scales, int j0) {
+            const int Np = blocks_of(p.N) * kBlock;
+#pragma unroll
+            for (int i = 0; i < MB; ++i) {
+                float top = 0.f;
+#pragma unroll
+                for (int jb = 0; jb < NO; ++jb)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (n_wave + jb * 32 + 8 * q + 4 * kh < p.N) {
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) top = fmaxf(top, finite_abs(acc[i][j0 + jb][4 * q + v]));
+                        }
+                top = fmaxf(top, __shfl_xor(top, 32));
+                if (kh == 0) tops[wn][(wm * MB + i) * 32 + l32] = top;
+            }
+            __syncthreads();
+            const int w0 = wn / kColumnWaves * kColumnWaves;
+#pragma unroll
+            for (int i = 0; i < MB; ++i) {
+                const int m = (wm * MB + i) * 32 + l32;
+                float top = tops[w0][m];
+#pragma unroll
+                for (int w = 1; w < kColumnWaves; ++w) top = fmaxf(top, tops[w0 + w][m]);
+                const uint32_t byte = scale_byte(top);
+                const float inverse = scale_inverse(byte);
+                if (m < limit) {
+#pragma unroll
+                    for (int jb = 0; jb < NO; ++jb)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int n = n_wave + jb * 32 + 8 * q + 4 * kh;
+                            float f[4];
+                            values(i, j0 + jb, q, f);
+                            if (n < Np) *reinterpret_cast<uint32_t*>(to + (first + m) * Np + n) = n < p.N ? to_e4m3(f[0] * inverse, f[1] * inverse, f[2] * inverse, f[3] * inverse) : 0u;
+                        }
+                    const int block = n_wave / kBlock;
+                    if (wn == w0 && kh == 0 && n_wave < p.N) {
+                        uint8_t* at = scales + (static_cast<size_t>(block >> 2) * p.rows + first + m) * 4;
+                        at[block & 3] = static_cast<uint8_t>(byte);
+                        if (block == blocks_of(p.N) - 1)
+                            for (int b = (block & 3) + 1; b < 4; ++b) at[b] = 127;
+                    }
+                }
+            }
+            __syncthreads();                             // (before the next ones are written)
+        };
+        if constexpr (MODE == FORWARD) {
+#pragma unroll
+            for (int h = 0; h < (GLU ? 2 : 1); ++h) {
+                if (p.bias[h]) {
+#pragma unroll
+                    for (int jb = 0; jb < NO; ++jb)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int n = n_wave + jb * 32 + 8 * q + 4 * kh;
+                            float b[4] = {0.f, 0.f, 0.f, 0.f};
+                            if (n < p.N) load4<true>(p.bias[h] + static_cast<size_t>(t.e) * p.N, n, b);
+#pragma unroll
+                            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                                for (int v = 0; v < 4; ++v) acc[i][h * NO + jb][4 * q + v] += b[v];
+                        }
+                }
+                if (p.P[1 + h]) pack(p.P[1 + h], p.Ps[1 + h], h * NO);
+            }
+            if (GLU || p.act != ETR_ACT_NONE || p.residual) {
+#pragma unroll
+                for (int i = 0; i < MB; ++i)
+#pragma unroll
+                    for (int jb = 0; jb < NO; ++jb)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int m = (wm * MB + i) * 32 + l32, n = n_wave + jb * 32 + 8 * q + 4 * kh;
+                            float r[4] = {0.f, 0.f, 0.f, 0.f};
+                            if (p.residual && m < limit && n < p.N) load4<WIDE>(p.residual, (first + m) * p.N + n, r);
+#pragma unroll
+                            for (int v = 0; v < 4; ++v)
+                                acc[i][jb][4 * q + v] = activate<WIDE>(p.act, acc[i][jb][4 * q + v], GLU ? acc[i][(GLU ? NO : 0) + jb][4 * q + v] : 1.0f, GLU) + r[v];
+                        }
+            }
+            if (p.P[0]) pack(p.P[0], p.Ps[0], 0);
+        }
+        void* C = p.C[MODE == WEIGHT ? t.half : 0];
+        if (C) {
+#pragma unroll
+            for (int i = 0; i < MB; ++i) {
+                const int m = (wm * MB + i) * 32 + l32;
+#pragma unroll
+                for (int jb = 0; jb < NO; ++jb)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int n = n_wave + jb * 32 + 8 * q + 4 * kh;
+                        float f[4];
+                        values(i, jb, q, f);
+                        if (m < limit && n < p.N) store4<WIDE>(C, (first + m) * p.N + n, f);
+                    }
+            }
+        }
+        j += grid >> 3;
+        if (!find_tile<MODE, WALK>(p, groups, BM, OUT_N, bid, grid, j, t)) break;
+        if constexpr (NBUF > 2) wait_copies<0>();        // (the stores too: the counted waits are for copies alone)
+    }
+    wait_copies<0>();                                    // the copies that nobody needed
+}
+
+// ---- few rows ----------------------------------------------------------------------------------------------------------
+//
+// 16 rows x 128 output columns to a workgroup: eight waves, or twice eight that share the contraction, with 16 columns each (SwiGLU: 16 gate
+// and 16 up), stream their weight rows straight into registers, a 16 x 16 x 128 MFMA to a k-tile.  Bound by the weights' bytes.  A lane has row
+// lane % 16 of a block and 16 bytes out of each half of the k-tile, so that a load takes 64 bytes of a row.
+template <bool WIDE, int KS, bool GLU>
+__global__ __launch_bounds__(512 * KS, 2) void packed_rows_kernel(PackedParams p) {
+    constexpr int BM = 16, NW = 8, NG = GLU ? 2 : 1;
+    __shared__ float tops[NW][BM];
+    __shared__ f32x4 sums[KS > 1 ? KS - 1 : 1][NG][KS > 1 ? NW * 64 : 1];
+    const int lane = threadIdx.x & 63, l16 = lane & 15, kq = lane >> 4;
+    const int wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = wave_all % NW, group = wave_all / NW;
+    Segments seg;
+    seg.load(p.offsets, p.rows, p.E, false);
+    Groups groups;
+    groups.first = seg.first; groups.count = seg.count;
+    groups.tiles = (seg.count + BM - 1) / BM;
+    groups.tiles_incl = wave_scan_incl(groups.tiles);
+    Tile t;
+    const int bid = blockIdx.x, grid = gridDim.x;
+    for (int j = bid >> 3; find_tile<FORWARD, false>(p, groups, BM, kBlock, bid, grid, j, t); j += grid >> 3) {
+        const size_t pitch = static_cast<size_t>(p.blocks) * kBlock, first = static_cast<size_t>(t.first) + t.m0;
+        const int rows_left = t.count - t.m0, n0 = t.n0 + wave * 16, G = (p.blocks + 3) / 4;
+        const size_t row_a = first + min(l16, rows_left - 1), row_b = min(n0 + l16, p.N - 1);
+        const uint8_t* a = p.A + row_a * pitch + kq * 16;
+        const uint32_t* as = reinterpret_cast<const uint32_t*>(p.As) + row_a;
+        const uint8_t* b[NG];
+        const uint32_t* bs[NG];
+#pragma unroll
+        for (int h = 0; h < NG; ++h) {
+            b[h] = p.B[h] + (static_cast<size_t>(t.e) * p.N + row_b) * pitch + kq * 16;
+            bs[h] = reinterpret_cast<const uint32_t*>(p.Bs[h]) + static_cast<size_t>(t.e) * G * p.N + row_b;
+        }
+        f32x4 acc[NG];
+#pragma unroll
+        for (int h = 0; h < NG; ++h) acc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+        // four k-tiles, whose scales are a dword, at a time; a group of waves takes every KS-th four
+        for (int g = group; g < G; g += KS) {
+            const uint32_t sa = as[static_cast<size_t>(g) * p.rows];
+            uint32_t sb[NG];
+#pragma unroll
+            for (int h = 0; h < NG; ++h) sb[h] = bs[h][static_cast<size_t>(g) * p.N];
+            v4i fa[4][2], fb[NG][4][2];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                // (past the last k-tile the last again, with nothing added for it)
+                const size_t at = static_cast<size_t>(min(4 * g + u, p.blocks - 1)) * kBlock;
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+#pragma unroll
+                    for (int h = 0; h < NG; ++h) fb[h][u][s] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(b[h] + at + s * 64));
+                    fa[u][s] = *reinterpret_cast<const v4i*>(a + at + s * 64);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (4 * g + u >= p.blocks) break;        // (uniform)
+                const uint32_t xa = (sa >> (8 * u)) & 255u;
+                if constexpr (!WIDE) {
+                    const v8i x{fa[u][0][0], fa[u][0][1], fa[u][0][2], fa[u][0][3], fa[u][1][0], fa[u][1][1], fa[u][1][2], fa[u][1][3]};
+#pragma unroll
+                    for (int h = 0; h < NG; ++h) {
+                        const v4i lo = fb[h][u][0], hi = fb[h][u][1];
+                        const v8i w{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                        acc[h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc[h], 0, 0, 0, static_cast<int>((sb[h] >> (8 * u)) & 255u), 0, static_cast<int>(xa));
+                    }
+                } else {
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            const bf16x8 x = widen(fa[u][s][2 * q], fa[u][s][2 * q + 1], scale_value(xa));
+#pragma unroll
+                            for (int h = 0; h < NG; ++h)
+                                acc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(fb[h][u][s][2 * q], fb[h][u][s][2 * q + 1], scale_value((sb[h] >> (8 * u)) & 255u)), x,
+                                                                                acc[h], 0, 0, 0);
+                        }
+                }
+            }
+        }
+        if constexpr (KS > 1) {
+            if (group > 0) {
+#pragma unroll
+                for (int h = 0; h < NG; ++h) sums[group - 1][h][threadIdx.x % (NW * 64)] = acc[h];
+            }
+            __syncthreads();
+            if (group == 0) {
+#pragma unroll
+                for (int s = 0; s < KS - 1; ++s)
+#pragma unroll
+                    for (int h = 0; h < NG; ++h) acc[h] += sums[s][h][threadIdx.x];
+            }
+            __syncthreads();
+        }
+        // lane: row l16, columns 4 kq ... + 3 of the wave's 16
+        const int n = n0 + 4 * kq, Np = blocks_of(p.N) * kBlock;
+        const bool mine = group == 0, row_in = mine && l16 < rows_left;
+        auto pack = [&](uint8_t* to, uint8_t* scales, const f32x4& v) {
+            float top = 0.f;
+            if (n < p.N) top = fmaxf(fmaxf(finite_abs(v[0]), finite_abs(v[1])), fmaxf(finite_abs(v[2]), finite_abs(v[3])));
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            if (mine && kq == 0) tops[wave][l16] = top;
+            __syncthreads();
+            top = tops[0][l16];
+#pragma unroll
+            for (int w = 1; w < NW; ++w) top = fmaxf(top, tops[w][l16]);
+            const uint32_t byte = scale_byte(top);
+            const float inverse = scale_inverse(byte);
+            if (row_in && n < Np)
+                *reinterpret_cast<uint32_t*>(to + (first + l16) * Np + n) = n < p.N ? to_e4m3(v[0] * inverse, v[1] * inverse, v[2] * inverse, v[3] * inverse) : 0u;
+            if (row_in && wave == 0 && kq == 0) {
+                const int block = t.n0 / kBlock;
+                uint8_t* at = scales + (static_cast<size_t>(block >> 2) * p.rows + first + l16) * 4;
+                at[block & 3] = static_cast<uint8_t>(byte);
+                if (block == blocks_of(p.N) - 1)
+                    for (int x = (block & 3) + 1; x < 4; ++x) at[x] = 127;
+            }
+            __syncthreads();
+        };
+#pragma unroll
+        for (int h = 0; h < NG; ++h) {
+            if (p.bias[h] && n < p.N) {
+                float f[4];
+                load4<true>(p.bias[h] + static_cast<size_t>(t.e) * p.N, n, f);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[h][v] += f[v];
+            }
+            if (p.P[1 + h]) pack(p.P[1 + h], p.Ps[1 + h], acc[h]);
+        }
+        float r[4] = {0.f, 0.f, 0.f, 0.f};
+        if (p.residual && row_in && n < p.N) load4<WIDE>(p.residual, (first + l16) * p.N + n, r);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) acc[0][v] = activate<WIDE>(p.act, acc[0][v], acc[NG - 1][v], GLU) + r[v];
+        if (p.P[0]) pack(p.P[0], p.Ps[0], acc[0]);
+        if (p.C[0] && row_in && n < p.N) {
+            const float f[4] = {acc[0][0], acc[0][1], acc[0][2], acc[0][3]};
+            store4<WIDE>(p.C[0], (first + l16) * p.N + n, f);
+        }
+    }
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+
+long long tiles_at_most(const PackedParams& p, int mode, int BM, int out_n) {
+    const long long columns = (p.N + out_n - 1) / out_n;
+    if (mode == WEIGHT) return columns * ((p.M + BM - 1) / BM) * p.E * (p.glu ? 2 : 1);
+    // full tiles of all rows together, and one more in part for each group
+    return columns * (p.rows / BM + std::min(p.E, p.rows));
+}
+
+template <bool WIDE, int BM, int BN, int WM, int WN, int NBUF, int MODE, bool GLU, bool WALK>
+hipError_t launch_tiles(PackedParams p, hipStream_t st) {
+    constexpr int out_n = GLU ? BN / 2 : BN;
+    constexpr size_t lds = static_cast<size_t>(NBUF) * ((BM + BN) * 128 + ((BM + 63) / 64 + BN / 64) * 256) + WN * BM * 4;
+    auto kern = packed_tiles_kernel<WIDE, BM, BN, WM, WN, NBUF, MODE, GLU, WALK>;
+    const hipError_t err = ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds);
+    if (err != hipSuccess) return err;
+    p.NT = (p.N + out_n - 1) / out_n;
+    const long long tiles = tiles_at_most(p, MODE, BM, out_n);
+    // one workgroup on each CU that walks the tiles (up to four parts of one), or one for each of them
+    const long long blocks = std::min<long long>((tiles + 7) / 8 * (WALK ? 4 : 1), WALK ? cu_count() / 8 : 1 << 17) * 8;
+    hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(blocks)), dim3(WM * WN * 64), lds, st, p);
+    return hipGetLastError();
+}
+template <bool WIDE, bool GLU>
+hipError_t launch_rows(PackedParams p, hipStream_t st) {
+    p.NT = blocks_of(p.N);
+    const long long tiles = tiles_at_most(p, FORWARD, 16, kBlock);
+    const long long blocks = std::min<long long>((tiles + 7) / 8, 1 << 17) * 8;
+    hipLaunchKernelGGL((packed_rows_kernel<WIDE, 1, GLU>), dim3(static_cast<unsigned>(blocks)), dim3(512), 0, st, p);
+    return hipGetLastError();
+}
+
+template <bool WIDE, bool GLU>
+hipError_t launch_forward(const PackedParams& p, hipStream_t st) {
+    const double rows_each = static_cast<double>(p.rows) / p.E;
+    if (rows_each <= 32) return launch_rows<WIDE, GLU>(p, st);
+    if (rows_each < 512) {
+        if constexpr (GLU) return launch_tiles<WIDE, 64, 256, 1, 4, 2, FORWARD, true, false>(p, st);
+        else return launch_tiles<WIDE, 128, 128, 2, 2, 2, FORWARD, false, false>(p, st);
+    }
+    return launch_tiles<WIDE, 256, 256, 2, 4, 2, FORWARD, GLU, true>(p, st);
+}
+template <bool WIDE>
+hipError_t launch_weight(const PackedParams& p, hipStream_t st) {
+    if (static_cast<long long>(p.M) * p.N * p.E * (p.glu ? 2 : 1) < 512ll * 256 * 256) return launch_tiles<WIDE, 128, 128, 2, 2, 2, WEIGHT, false, false>(p, st);
+    return launch_tiles<WIDE, 256, 256, 2, 4, 2, WEIGHT, false, true>(p, st);
+}
+
+}  // namespace
+
+hipError_t launch_packed_linear(const etr_linear_config& c, const etr_packed& x, const int32_t* offsets, const etr_packed* const w[2], const float* bias,
+                                 const float* bias_up, const void* residual, void* y, const etr_packed* const kept[3], hipStream_t st) {
+    PackedParams p{};
+    p.rows = c.rows; p.E = c.E; p.N = c.N; p.blocks = blocks_of(c.K); p.act = c.act; p.glu = c.act == ETR_ACT_SWIGLU;
+    p.A = static_cast<const uint8_t*>(x.values); p.As = static_cast<const uint8_t*>(x.scales);
+    for (int i = 0; i < 2; ++i)
+        if (w[i]) { p.B[i] = static_cast<const uint8_t*>(w[i]->values); p.Bs[i] = static_cast<const uint8_t*>(w[i]->scales); }
+    for (int i = 0; i < 3; ++i)
+        if (kept[i]) { p.P[i] = static_cast<uint8_t*>(kept[i]->values); p.Ps[i] = static_cast<uint8_t*>(kept[i]->scales); }
+    p.C[0] = y; p.offsets = offsets; p.bias[0] = bias; p.bias[1] = bias_up; p.residual = residual;
+    if (c.dtype == ETR_BF16) return p.glu ? launch_forward<false, true>(p, st) : launch_forward<false, false>(p, st);
+    return p.glu ? launch_forward<true, true>(p, st) : launch_forward<true, false>(p, st);
+}
+
+hipError_t launch_packed_weight_gradient(const etr_linear_config& c, const etr_packed& dt, const etr_packed& xt, const int32_t* offsets, void* dw, void* dw_up,
+                                   hipStream_t st) {
+    PackedParams p{};
+    p.rows = c.rows; p.E = c.E; p.M = c.N; p.N = c.K; p.glu = c.act == ETR_ACT_SWIGLU;
+    p.A = static_cast<const uint8_t*>(dt.values); p.As = static_cast<const uint8_t*>(dt.scales);
+    p.B[0] = static_cast<const uint8_t*>(xt.values); p.Bs[0] = static_cast<const uint8_t*>(xt.scales);
+    p.C[0] = dw; p.C[1] = dw_up; p.offsets = offsets;
+    return c.dtype == ETR_BF16 ? launch_weight<false>(p, st) : launch_weight<true>(p, st);
+}
+
+}  // namespace etr

@@ -1,0 +1,129 @@
+"""The backward from packed pre-activations, and the weights' gradient, against 64 bits.  The element-wise part is held to its definition; the products
+to the product of the values that their packed operands stand for."""
+import pytest
+import torch
+
+import operator_refs as O
+import packed_refs as R
+from paper_2406_00023_amd import binding as B
+from test_gpu_packed_linear import ACTS, DT, check_packed, gpu, operand, sum_error
+
+pytestmark = pytest.mark.gpu
+
+
+def derivative(act, dy, a, u):
+    """da, db in 64 bits, by torch's differentiation of the definition."""
+    a = a.clone().requires_grad_(True)
+    leaves = [a]
+    if act == "swiglu":
+        u = u.clone().requires_grad_(True)
+        leaves.append(u)
+    return torch.autograd.grad(O.activation(act, a, u), leaves, dy)
+
+
+def act_case(counts, N, dtype, act, seed=0, bias=True):
+    E, used = len(counts), sum(counts)
+    rows = used + 3
+    offsets = [sum(counts[:e]) for e in range(E + 1)]
+    glu, n = act == "swiglu", 2 if act == "swiglu" else 1
+    dy = O.randn(seed + 1, rows, N, dtype=DT[dtype], std=0.02)
+    pre8 = operand(seed + 2, rows, N, std=2.0) if act != "none" else None
+    up8 = operand(seed + 3, rows, N) if glu else None
+    cfg = B.make_linear_config(rows, 64, N, E, DT[dtype], act=ACTS[act])
+    Np = R.blocks(N) * 128
+    d8 = (torch.full((rows, n * Np), 0xA5, dtype=torch.uint8, device="cuda"), torch.full((R.blocks(n * Np // 4), rows, 4), 0xA5, dtype=torch.uint8, device="cuda"))
+    dt8 = B.alloc_packed_columns(B.make_pack_config(rows, n * N, DT[dtype], E=E, sorted=1))
+    sums = [torch.full((E, N), 9.0, device="cuda") for _ in range(n)] if bias else [None, None]
+    ws = B.alloc_workspace(B.etr_packed_act_workspace_bytes(cfg)) if bias else None
+    B.etr_packed_act_backward(cfg, dy.cuda(), torch.tensor(offsets, dtype=torch.int32, device="cuda"), ws, pre8=gpu(pre8) if pre8 else None,
+                              pre_up8=gpu(up8) if glu else None, d8=d8, dt8=dt8, dbias=sums[0], dbias_up=sums[1] if glu else None)
+    torch.cuda.synchronize()
+    if act == "none":
+        want = [dy.double()]
+    else:
+        want = derivative(act, dy.double(), R.values(*pre8, N), R.values(*up8, N) if glu else None)
+    # a derivative is off by the sums of a few terms of its own size, at most 1.2 |dy|, a dozen operations; dy |up| with SwiGLU
+    scale = dy.double().abs() * (1 + (R.values(*up8, N).abs() if glu else 0) + (R.values(*pre8, N).abs() if pre8 else 0))
+    err = [0 * w if act == "none" else 40 * O.U32 * scale for w in want]
+    live, what = slice(0, used), (counts, N, dtype, act)
+    q, s = d8[0].cpu(), d8[1].cpu()
+    flat = R.unlayout(s, n * R.blocks(N))
+    for h in range(n):
+        part_q, part_s = q[live, h * Np: (h + 1) * Np], R.layout(flat[live, h * R.blocks(N): (h + 1) * R.blocks(N)])
+        check_packed(part_q, part_s, want[h][live], err[h][live], what)
+    if (n * R.blocks(N)) % 4:
+        assert bool((s[-1, live, (n * R.blocks(N)) % 4:] == 127).all()), what
+    assert bool((q[used:] == 0xA5).all()) and bool((s[:, used:] == 0xA5).all()), what
+    parts = R.column_parts(dt8[0].cpu(), dt8[1].cpu(), n * N, offsets)
+    for e in range(E):
+        sl = slice(offsets[e], offsets[e + 1])
+        for h in range(n):
+            got, w, er = parts[e][h * N: (h + 1) * N], want[h][sl].t(), err[h][sl].t()
+            top = torch.nn.functional.pad(w.abs(), (0, -w.shape[1] % 128)).unflatten(1, (-1, 128)).amax(2) if w.shape[1] else w
+            unit = torch.exp2(R.scale_bytes(top * (1 + 2.0 ** -20)).double() - 127).repeat_interleave(128, 1)[:, : w.shape[1]] if w.shape[1] else w
+            O.assert_within(got, w, 2.0 ** -4 * (w.abs() + er) + 2.0 ** -10 * unit + er, what)
+            if bias:
+                # a half step for each of the rows' sums, and the terms' own errors
+                bound = (w.shape[1] + 2) * O.U32 * w.abs().sum(1) + er.sum(1)
+                O.assert_within(sums[h][e], w.sum(1), bound, what)
+    if act == "none":                                          # nothing is computed: the bytes are those of the definition
+        want_q, want_s = R.pack(dy.double()[live])
+        assert torch.equal(q[live], want_q) and torch.equal(s[:, live], want_s)
+        want_q, want_s = R.pack_columns(dy.double(), offsets)
+        assert torch.equal(dt8[0].cpu()[: want_q.numel()], want_q) and torch.equal(dt8[1].cpu()[: want_s.numel()], want_s)
+
+
+COUNTS = [[1], [3, 0, 1, 16, 17], [130, 1, 0, 300], [0, 0], [129, 513, 128]]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["none", "silu", "gelu", "swiglu"])
+@pytest.mark.parametrize("counts", COUNTS, ids=str)
+@pytest.mark.parametrize("N", [8, 136, 520])
+def test_element_wise_part(counts, N, act, dtype):
+    act_case(counts, N, dtype, act, seed=N)
+
+
+def test_without_the_biases():
+    act_case([130, 1, 0, 300], 264, "bf16", "swiglu", bias=False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("glu", [False, True])
+@pytest.mark.parametrize("counts", [[1], [3, 0, 1, 16, 17], [130, 1, 0, 300], [0, 0], [129, 513, 128], [2000, 700]], ids=str)
+@pytest.mark.parametrize("K,N", [(8, 8), (136, 264), (520, 136)])
+def test_weights(counts, K, N, glu, dtype):
+    weights_case(counts, K, N, glu, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_weights_of_large_matrices(dtype):
+    """Enough tiles for the largest kind."""
+    weights_case([257, 100], 4104, 4360, True, dtype)
+
+
+def weights_case(counts, K, N, glu, dtype):
+    E, used = len(counts), sum(counts)
+    rows, n = used + 3, 2 if glu else 1
+    offsets = [sum(counts[:e]) for e in range(E + 1)]
+    dev = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    x, d = O.randn(1, rows, K), O.randn(2, rows, n * N, std=0.02)
+    x[used:], d[used:] = float("nan"), float("nan")
+    t8 = []
+    for v in (d, x):
+        cfg = B.make_pack_config(rows, v.shape[1], torch.float32, E=E, sorted=1)
+        out = B.alloc_packed_columns(cfg)
+        B.etr_pack_columns(cfg, v.cuda(), dev, out)
+        t8.append(out)
+    dw = [torch.full((E, N, K), 5.0, dtype=DT[dtype], device="cuda") for _ in range(n)]
+    B.etr_packed_weight_gradient(B.make_linear_config(rows, K, N, E, DT[dtype], act=3 if glu else 0), t8[0], t8[1], dev, dw[0], dw_up=dw[1] if glu else None)
+    da = R.column_parts(t8[0][0].cpu(), t8[0][1].cpu(), n * N, offsets)
+    xt = R.column_parts(t8[1][0].cpu(), t8[1][1].cpu(), K, offsets)
+    for e in range(E):
+        for h in range(n):
+            a = da[e][h * N: (h + 1) * N]
+            want = a @ xt[e].t()
+            bound = sum_error(a, xt[e], dtype == "f32") + O.half_step(DT[dtype]) * 1.01 * want.abs() if a.shape[1] else torch.zeros_like(want)
+            O.assert_within(dw[h][e], want, bound, (counts, K, N, glu, dtype, e, h))
+            if dtype == "bf16" and a.shape[1]:
+                assert float((dw[h][e].cpu().double() - want).norm()) <= (O.half_step(DT[dtype]) + 2.0 ** -12) * float(want.norm())
