@@ -60,6 +60,11 @@ template <int N> __device__ __forceinline__ void wait_copies() {
     __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0070);
     asm volatile("" ::: "memory");
 }
+__device__ __forceinline__ void wait_reads() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);                  // lgkmcnt(0)
+    asm volatile("" ::: "memory");
+}
 __device__ __forceinline__ void barrier() {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
@@ -104,12 +109,6 @@ __device__ __forceinline__ void load4(const void* p, size_t at, float (&f)[4]) {
         f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xFFFF0000u);
     }
 }
-
-// A lane's results come in runs of four neighbouring columns of one row.  `Runs` says which: MB row places, NR runs each.
-//   acc(i, r): the run as a reference to its four values; row(i): row in the tile; column(r): first output column, in the tile
-// Packing needs the largest of a row's 128 columns: over a lane's runs, over the lanes that share the row (`fold`), and over the
-// waves that share the block, through LDS: tops[wave of the block's waves][row].
-struct PackPlace { uint8_t* values; uint8_t* scales; };
 
 // ---- tiles of 32 x 32 blocks -------------------------------------------------------------------------------------------
 //
@@ -245,6 +244,39 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void packed_tiles_kernel(PackedPara
         const v4i hi = *reinterpret_cast<const v4i*>(op + row * 128 + ((4 * half + 2 * kh + 1) ^ x) * 16);
         return v8i{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     };
+    auto multiply_row = [&](const v8i& fa, const v8i (&fb)[NB], int sa, const int (&sb)[NB], f32x16 (&c)[NB]) {
+        if constexpr (!WIDE) {
+#pragma unroll
+            for (int jb = 0; jb < NB; ++jb) c[jb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[jb], fa, c[jb], 0, 0, 0, sb[jb], 0, sa);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const bf16x8 wa = widen(fa[2 * q], fa[2 * q + 1], scale_value(sa));
+#pragma unroll
+                for (int jb = 0; jb < NB; ++jb)
+                    c[jb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(fb[jb][2 * q], fb[jb][2 * q + 1], scale_value(sb[jb])), wa, c[jb], 0, 0, 0);
+            }
+        }
+    };
+    auto multiply = [&](const v8i (&fa)[MB], const v8i (&fb)[NB], const int (&sa)[MB], const int (&sb)[NB], f32x16 (&c)[MB][NB]) {
+        if constexpr (!WIDE) {
+#pragma unroll
+            for (int i = 0; i < MB; ++i) multiply_row(fa[i], fb, sa[i], sb, c[i]);
+        } else {                                         // every fragment is converted once
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                bf16x8 wa[MB], wb[NB];
+#pragma unroll
+                for (int i = 0; i < MB; ++i) wa[i] = widen(fa[i][2 * q], fa[i][2 * q + 1], scale_value(sa[i]));
+#pragma unroll
+                for (int jb = 0; jb < NB; ++jb) wb[jb] = widen(fb[jb][2 * q], fb[jb][2 * q + 1], scale_value(sb[jb]));
+#pragma unroll
+                for (int i = 0; i < MB; ++i)
+#pragma unroll
+                    for (int jb = 0; jb < NB; ++jb) c[i][jb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[jb], wa[i], c[i][jb], 0, 0, 0);
+            }
+        }
+    };
     f32x16 acc[MB][NB];
     aim(t);
 #pragma unroll
@@ -258,156 +290,244 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void packed_tiles_kernel(PackedPara
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc[i][jb][v] = 0.f;
         const int KT = MODE == WEIGHT ? max(__builtin_amdgcn_readlane(seg.blocks, t.e), 1) : p.blocks;
-        for (int kt = 0; kt < KT; ++kt) {
-            wait_copies<(NBUF - 2) * (CW + SW)>();       // this wave's part of the k-tile has landed
-            barrier();                                   // ... and everybody's; and everybody is done with the buffer before it
-            issue(buf == 0 ? NBUF - 1 : buf - 1);
-            advance();
-            const unsigned char* op = lds + buf * STAGE;
-            const uint32_t* sc = reinterpret_cast<const uint32_t*>(op + TILE_BYTES);
-            const int shift = 8 * (kt & 3);
-            int sa[MB], sb[NB];
+        // row blocks of the wave that have a row to store at all: tiles at the end of an expert's rows multiply what they have, and the
+        // wave beside this one on the SIMD has the matrix pipe for itself meanwhile
+        const int live = t.n0 + wn * NO * 32 < p.N ? min(max((t.limit - t.m0 - wm * MB * 32 + 31) >> 5, 0), MB) : 0;
+        auto k_loop = [&](auto whole) {
+            for (int kt = 0; kt < KT; ++kt) {
+                wait_copies<(NBUF - 2) * (CW + SW)>();   // this wave's part of the k-tile has landed
+                barrier();                               // ... and everybody's; and everybody is done with the buffer before it
+                issue(buf == 0 ? NBUF - 1 : buf - 1);
+                advance();
+                const unsigned char* op = lds + buf * STAGE;
+                const uint32_t* sc = reinterpret_cast<const uint32_t*>(op + TILE_BYTES);
+                const int shift = 8 * (kt & 3);
+                int sa[MB], sb[NB];
 #pragma unroll
-            for (int i = 0; i < MB; ++i) sa[i] = static_cast<int>(sc[(wm * MB + i) * 32 + l32] >> shift) & 255;
+                for (int i = 0; i < MB; ++i) sa[i] = static_cast<int>(sc[(wm * MB + i) * 32 + l32] >> shift) & 255;
 #pragma unroll
-            for (int jb = 0; jb < NB; ++jb) sb[jb] = static_cast<int>(sc[SA * 64 + b_block(jb) * 32 + l32] >> shift) & 255;
+                for (int jb = 0; jb < NB; ++jb) sb[jb] = static_cast<int>(sc[SA * 64 + b_block(jb) * 32 + l32] >> shift) & 255;
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                v8i fa[MB], fb[NB];
+                for (int half = 0; half < 2; ++half) {
+                    v8i fa[MB], fb[NB];
 #pragma unroll
-                for (int jb = 0; jb < NB; ++jb) fb[jb] = fragment(op + A_BYTES, b_block(jb), half);
+                    for (int jb = 0; jb < NB; ++jb) fb[jb] = fragment(op + A_BYTES, b_block(jb), half);
+                    if constexpr (decltype(whole)::value) {
 #pragma unroll
-                for (int i = 0; i < MB; ++i) fa[i] = fragment(op, wm * MB + i, half);
-                if constexpr (!WIDE) {
-#pragma unroll
-                    for (int i = 0; i < MB; ++i)
-#pragma unroll
-                        for (int jb = 0; jb < NB; ++jb)
-                            acc[i][jb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[jb], fa[i], acc[i][jb], 0, 0, 0, sb[jb], 0, sa[i]);
-                } else {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        bf16x8 wa[MB], wb[NB];
-#pragma unroll
-                        for (int i = 0; i < MB; ++i) wa[i] = widen(fa[i][2 * q], fa[i][2 * q + 1], scale_value(sa[i]));
-#pragma unroll
-                        for (int jb = 0; jb < NB; ++jb) wb[jb] = widen(fb[jb][2 * q], fb[jb][2 * q + 1], scale_value(sb[jb]));
+                        for (int i = 0; i < MB; ++i) fa[i] = fragment(op, wm * MB + i, half);
+                        multiply(fa, fb, sa, sb, acc);
+                    } else {
 #pragma unroll
                         for (int i = 0; i < MB; ++i)
-#pragma unroll
-                            for (int jb = 0; jb < NB; ++jb) acc[i][jb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[jb], wa[i], acc[i][jb], 0, 0, 0);
+                            if (i < live) multiply_row(fragment(op, wm * MB + i, half), fb, sa[i], sb, acc[i]);
                     }
                 }
+                buf = buf + 1 == NBUF ? 0 : buf + 1;
             }
-            buf = buf + 1 == NBUF ? 0 : buf + 1;
-        }
+        };
+        if (live == MB) k_loop(std::true_type{});
+        else k_loop(std::false_type{});
 
-        // ---- the results: lane: row l32 of a block, columns 8 q + 4 kh ... + 3 of it for q = 0 ... 3
+        // ---- the results: lane: row l of a block, columns 8 q + 4 h ... + 3 of it for q = 0 ... 3
+        // They leave through the buffer that was multiplied last, which nobody copies into before the next k-tile's barrier.  What is optional
+        // goes over the accumulators in a pass of its own, a row block at a time (the barriers to the scheduler), so that few values live
+        // beside them; what depends on `lane_now` is made anew in each pass and takes no registers of the loop over k-tiles.
         const int limit = t.limit - t.m0;
         const int n_wave = t.n0 + wn * NO * 32;          // first output column of the wave
         const size_t first = (MODE == WEIGHT ? static_cast<size_t>(t.e) * p.M : static_cast<size_t>(t.first)) + t.m0;
-        auto values = [&](int i, int jb, int q, float (&f)[4]) {
+        unsigned char* room = lds + (buf == 0 ? NBUF - 1 : buf - 1) * STAGE;
+        auto lane_now = [&]() { int l = lane; asm volatile("" : "+v"(l)); return l; };
+        auto pin = [&]() {
 #pragma unroll
-            for (int v = 0; v < 4; ++v) f[v] = acc[i][jb][4 * q + v];
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int jb = 0; jb < NB; ++jb) asm volatile("" : "+v"(acc[i][jb]));
         };
-        // packs blocks j0 ... j0 + NO - 1 of the accumulators
-        auto pack = [&](uint8_t* to, uint8_t* scales, int j0) {
-            const int Np = blocks_of(p.N) * kBlock;
+        pin();
+        wait_reads();
+        barrier();                                       // everybody has read it
+        // packs blocks j0 ... j0 + NO - 1 of the accumulators.  room: [row][OUT_N bytes], the pieces of a row in an order of its own
+        auto pack = [&](uint8_t* to, uint8_t* scales, auto j0_) {
+            constexpr int PR = OUT_N / 16, j0 = decltype(j0_)::value;    // pieces of a row
+            static_assert(BM * OUT_N <= TILE_BYTES, "");
+            auto place = [](int row, int piece) { return row * OUT_N + ((piece ^ (OUT_N == 128 ? row >> 1 : row)) & (PR - 1)) * 16; };
+            const int Np = blocks_of(p.N) * kBlock, w0 = wn / kColumnWaves * kColumnWaves, block = n_wave / kBlock;
+            const bool ragged = n_wave + NO * 32 > p.N;                  // (uniform)
+            {
+                const int l = lane_now(), h = l >> 5;
 #pragma unroll
-            for (int i = 0; i < MB; ++i) {
-                float top = 0.f;
-#pragma unroll
-                for (int jb = 0; jb < NO; ++jb)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        if (n_wave + jb * 32 + 8 * q + 4 * kh < p.N) {
-#pragma unroll
-                            for (int v = 0; v < 4; ++v) top = fmaxf(top, finite_abs(acc[i][j0 + jb][4 * q + v]));
-                        }
-                top = fmaxf(top, __shfl_xor(top, 32));
-                if (kh == 0) tops[wn][(wm * MB + i) * 32 + l32] = top;
-            }
-            __syncthreads();
-            const int w0 = wn / kColumnWaves * kColumnWaves;
-#pragma unroll
-            for (int i = 0; i < MB; ++i) {
-                const int m = (wm * MB + i) * 32 + l32;
-                float top = tops[w0][m];
-#pragma unroll
-                for (int w = 1; w < kColumnWaves; ++w) top = fmaxf(top, tops[w0 + w][m]);
-                const uint32_t byte = scale_byte(top);
-                const float inverse = scale_inverse(byte);
-                if (m < limit) {
+                for (int i = 0; i < MB; ++i) {
+                    float top = 0.f;
 #pragma unroll
                     for (int jb = 0; jb < NO; ++jb)
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
-                            const int n = n_wave + jb * 32 + 8 * q + 4 * kh;
-                            float f[4];
-                            values(i, j0 + jb, q, f);
-                            if (n < Np) *reinterpret_cast<uint32_t*>(to + (first + m) * Np + n) = n < p.N ? to_e4m3(f[0] * inverse, f[1] * inverse, f[2] * inverse, f[3] * inverse) : 0u;
+                            float four = 0.f;
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) four = fmaxf(four, finite_abs(acc[i][j0 + jb][4 * q + v]));
+                            if (ragged && n_wave + jb * 32 + 8 * q + 4 * h >= p.N) four = 0.f;
+                            top = fmaxf(top, four);
                         }
-                    const int block = n_wave / kBlock;
-                    if (wn == w0 && kh == 0 && n_wave < p.N) {
+                    top = fmaxf(top, __shfl_xor(top, 32));
+                    if (h == 0) tops[wn][(wm * MB + i) * 32 + (l & 31)] = top;
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            __syncthreads();
+            {
+                const int l = lane_now(), h = l >> 5;
+#pragma unroll
+                for (int i = 0; i < MB; ++i) {
+                    const int m = (wm * MB + i) * 32 + (l & 31);
+                    float top = tops[w0][m];
+#pragma unroll
+                    for (int w = 1; w < kColumnWaves; ++w) top = fmaxf(top, tops[w0 + w][m]);
+                    const uint32_t byte = scale_byte(top);
+                    const float inverse = scale_inverse(byte);
+#pragma unroll
+                    for (int jb = 0; jb < NO; ++jb)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int c = wn * NO * 32 + jb * 32 + 8 * q + 4 * h;
+                            const f32x16& a = acc[i][j0 + jb];
+                            uint32_t four = to_e4m3(a[4 * q] * inverse, a[4 * q + 1] * inverse, a[4 * q + 2] * inverse, a[4 * q + 3] * inverse);
+                            if (ragged && t.n0 + c >= p.N) four = 0u;
+                            *reinterpret_cast<uint32_t*>(room + place(m, c >> 4) + (c & 15)) = four;
+                        }
+                    if (m < limit && wn == w0 && h == 0 && n_wave < p.N) {
                         uint8_t* at = scales + (static_cast<size_t>(block >> 2) * p.rows + first + m) * 4;
                         at[block & 3] = static_cast<uint8_t>(byte);
                         if (block == blocks_of(p.N) - 1)
                             for (int b = (block & 3) + 1; b < 4; ++b) at[b] = 127;
                     }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            __syncthreads();
+            {
+                int tid = threadIdx.x;
+                asm volatile("" : "+v"(tid));
+                const int c = tid % PR, m0 = tid / PR;
+                uint8_t* base = to + first * Np + t.n0;
+                static_assert(NW * 64 % PR == 0, "");
+#pragma unroll 4
+                for (int u = 0; u < BM * PR / (NW * 64); ++u) {
+                    const int m = u * (NW * 64 / PR) + m0;
+                    const piece_t v = *reinterpret_cast<const piece_t*>(room + place(m, c));
+                    if (m < limit && t.n0 + c * 16 < Np) *reinterpret_cast<piece_t*>(base + static_cast<size_t>(m) * Np + c * 16) = v;
                 }
             }
             __syncthreads();                             // (before the next ones are written)
         };
         if constexpr (MODE == FORWARD) {
-#pragma unroll
-            for (int h = 0; h < (GLU ? 2 : 1); ++h) {
-                if (p.bias[h]) {
-#pragma unroll
-                    for (int jb = 0; jb < NO; ++jb)
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const int n = n_wave + jb * 32 + 8 * q + 4 * kh;
-                            float b[4] = {0.f, 0.f, 0.f, 0.f};
-                            if (n < p.N) load4<true>(p.bias[h] + static_cast<size_t>(t.e) * p.N, n, b);
-#pragma unroll
-                            for (int i = 0; i < MB; ++i)
-#pragma unroll
-                                for (int v = 0; v < 4; ++v) acc[i][h * NO + jb][4 * q + v] += b[v];
-                        }
-                }
-                if (p.P[1 + h]) pack(p.P[1 + h], p.Ps[1 + h], h * NO);
-            }
-            if (GLU || p.act != ETR_ACT_NONE || p.residual) {
+            auto map = [&](auto&& f) {
 #pragma unroll
                 for (int i = 0; i < MB; ++i)
 #pragma unroll
                     for (int jb = 0; jb < NO; ++jb)
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
-                            const int m = (wm * MB + i) * 32 + l32, n = n_wave + jb * 32 + 8 * q + 4 * kh;
-                            float r[4] = {0.f, 0.f, 0.f, 0.f};
-                            if (p.residual && m < limit && n < p.N) load4<WIDE>(p.residual, (first + m) * p.N + n, r);
 #pragma unroll
-                            for (int v = 0; v < 4; ++v)
-                                acc[i][jb][4 * q + v] = activate<WIDE>(p.act, acc[i][jb][4 * q + v], GLU ? acc[i][(GLU ? NO : 0) + jb][4 * q + v] : 1.0f, GLU) + r[v];
+                            for (int v = 4 * q; v < 4 * q + 4; ++v) acc[i][jb][v] = f(acc[i][jb][v], GLU ? acc[i][(GLU ? NO : 0) + jb][v] : 1.0f);
+                            __builtin_amdgcn_sched_barrier(0);
                         }
+                pin();
+            };
+            auto half = [&](auto h_) {
+                constexpr int h = decltype(h_)::value;
+                if (p.bias[h]) {
+                    const int l = lane_now(), kq = 4 * (l >> 5);
+#pragma unroll
+                    for (int jb = 0; jb < NO; ++jb)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int n = n_wave + jb * 32 + 8 * q + kq;
+                            float b[4] = {0.f, 0.f, 0.f, 0.f};
+                            if (n < p.N) load4<true>(p.bias[h] + static_cast<size_t>(t.e) * p.N, n, b);
+#pragma unroll
+                            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                                for (int v = 0; v < 4; ++v) acc[i][h * NO + jb][4 * q + v] += b[v];
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    pin();
+                }
+                if (p.P[1 + h]) {
+                    pack(p.P[1 + h], p.Ps[1 + h], std::integral_constant<int, h * NO>{});
+                    pin();
+                }
+            };
+            half(std::integral_constant<int, 0>{});
+            if constexpr (GLU) {
+                half(std::integral_constant<int, 1>{});
+                map([](float a, float u) { return a * sigmoid<!WIDE>(a) * u; });
+            } else {
+                if (p.act == ETR_ACT_SILU) map([](float a, float) { return a * sigmoid<!WIDE>(a); });
+                pin();                                   // (or one pass is made of the two, with both results of every value alive)
+                if (p.act == ETR_ACT_GELU) map([](float a, float) { return a * normal_cdf<!WIDE>(a); });
             }
-            if (p.P[0]) pack(p.P[0], p.Ps[0], 0);
+            if (p.residual) {
+                const int l = lane_now(), kq = 4 * (l >> 5);
+                const char* base = static_cast<const char*>(p.residual) + first * p.N * (WIDE ? 4 : 2);
+#pragma unroll
+                for (int i = 0; i < MB; ++i) {
+                    // (past the ends the last row or columns again, not stored)
+                    const size_t row = static_cast<size_t>(max(min((wm * MB + i) * 32 + (l & 31), limit - 1), 0)) * p.N;
+                    float r[NO][4][4];
+#pragma unroll
+                    for (int jb = 0; jb < NO; ++jb)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) load4<WIDE>(base, row + min(n_wave + jb * 32 + 8 * q + kq, p.N - 4), r[jb][q]);
+#pragma unroll
+                    for (int jb = 0; jb < NO; ++jb)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) acc[i][jb][4 * q + v] += r[jb][q][v];
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                pin();
+            }
+            if (p.P[0]) {
+                pack(p.P[0], p.Ps[0], std::integral_constant<int, 0>{});
+                pin();
+            }
         }
         void* C = p.C[MODE == WEIGHT ? t.half : 0];
         if (C) {
+            // 32 rows of the wave's columns at a time through its own part of the room, so that they leave as whole pieces side by side
+            constexpr int ES = WIDE ? 4 : 2, RB = NO * 32 * ES, PR = RB / 16, RP = 64 / PR;                  // bytes, pieces of a row; rows to a store
+            static_assert(NW * 32 * RB <= TILE_BYTES, "");
+            const int l = lane_now(), h = l >> 5;
+            unsigned char* patch = room + wave * 32 * RB;
+            const int row_in = l / PR, piece = l % PR, n = n_wave + piece * (16 / ES);
+            char* base = static_cast<char*>(C) + first * p.N * ES;
 #pragma unroll
             for (int i = 0; i < MB; ++i) {
-                const int m = (wm * MB + i) * 32 + l32;
+                if ((wm * MB + i) * 32 < limit) {        // (uniform)
 #pragma unroll
-                for (int jb = 0; jb < NO; ++jb)
+                    for (int jb = 0; jb < NO; ++jb)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const int n = n_wave + jb * 32 + 8 * q + 4 * kh;
-                        float f[4];
-                        values(i, jb, q, f);
-                        if (m < limit && n < p.N) store4<WIDE>(C, (first + m) * p.N + n, f);
+                        for (int q = 0; q < 4; ++q) {
+                            const int at = (jb * 32 + 8 * q + 4 * h) * ES;
+                            const float f[4] = {acc[i][jb][4 * q], acc[i][jb][4 * q + 1], acc[i][jb][4 * q + 2], acc[i][jb][4 * q + 3]};
+                            store4<WIDE>(patch + (l & 31) * RB + ((at >> 4) ^ (l & (PR - 1))) * 16 + (at & 15), 0, f);
+                        }
+                    wave_sync();
+                    piece_t out[32 / RP];
+#pragma unroll
+                    for (int u = 0; u < 32 / RP; ++u) {
+                        const int row = u * RP + row_in;
+                        out[u] = *reinterpret_cast<const piece_t*>(patch + row * RB + (piece ^ (row & (PR - 1))) * 16);
                     }
+                    wave_sync();
+#pragma unroll
+                    for (int u = 0; u < 32 / RP; ++u) {
+                        const int m = (wm * MB + i) * 32 + u * RP + row_in;
+                        if (m < limit && n < p.N) *reinterpret_cast<piece_t*>(base + (static_cast<size_t>(m) * p.N + n) * ES) = out[u];
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         j += grid >> 3;
