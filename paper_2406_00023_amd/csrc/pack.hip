@@ -69,13 +69,10 @@ __global__ __launch_bounds__(kThreads) void pack_rows_kernel(RowsParams p, int m
         uint32_t s[kSteps];
 #pragma unroll
         for (int u = 0; u < kSteps; ++u) {
-            float top = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top = fmaxf(top, finite_abs(f[u][i]));
-            const uint32_t byte = scale_byte(row16_max(top));
-            const float inverse = scale_inverse(byte);
-            q[u].x = to_e4m3(f[u][0] * inverse, f[u][1] * inverse, f[u][2] * inverse, f[u][3] * inverse);
-            q[u].y = to_e4m3(f[u][4] * inverse, f[u][5] * inverse, f[u][6] * inverse, f[u][7] * inverse);
+            const uint32_t byte = scale_byte(row16_max(top_of<8>([&](int i) { return f[u][i]; })));
+            const float scale = scale_value(byte);
+            q[u].x = to_e4m3(f[u][0], f[u][1], f[u][2], f[u][3], scale);
+            q[u].y = to_e4m3(f[u][4], f[u][5], f[u][6], f[u][7], scale);
             s[u] = 0;
 #pragma unroll
             for (int b = 0; b < 4; ++b)
@@ -125,10 +122,8 @@ __global__ __launch_bounds__(kThreads) void unpack_rows_kernel(RowsParams p, int
             const int c = (g0 + u) * 512 + lane * 8;
             const float scale = scale_value((s[u] >> (8 * (lane >> 4))) & 255u);
             float f[8];
-            from_e4m3(q[u].x, f);
-            from_e4m3(q[u].y, f + 4);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] *= scale;
+            from_e4m3(q[u].x, scale, f);
+            from_e4m3(q[u].y, scale, f + 4);
             if (c < p.K) store8<BF16>(p.y, static_cast<size_t>(row) * p.K + c, f);
         }
     }
@@ -146,7 +141,6 @@ struct TileParams {
     const uint8_t* q[2]; const uint32_t* s[2];           // a matrix packed along rows; or the packed pre-activations
     const int32_t* offsets;
     int rows, E, K, stacked;                             // rows: of each matrix of a stack, or of all
-    int act;                                             // ETR_ACT_NONE: the values as they are
     uint8_t* row_q; uint8_t* row_s; int row_pitch;       // along rows: out, optional
     uint8_t* column_q; uint8_t* column_s; int column_rows;   // along columns: out, optional; rows of a segment's matrix
     int half_blocks;                                     // > 0: a pair of stacks beside each other: blocks of 128 rows to a half
@@ -170,9 +164,7 @@ __device__ __forceinline__ void pack_tile_columns(const float (&v)[8][8], TileLd
     float top[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        top[j] = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top[j] = fmaxf(top[j], finite_abs(v[i][j]));
+        top[j] = top_of<8>([&](int i) { return v[i][j]; });
         top[j] = fmaxf(top[j], __shfl_xor(top[j], 16));
         top[j] = fmaxf(top[j], __shfl_xor(top[j], 32));
     }
@@ -189,10 +181,8 @@ __device__ __forceinline__ void pack_tile_columns(const float (&v)[8][8], TileLd
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) t = fmaxf(t, lds.top[w][c]);
         const uint32_t byte = scale_byte(t);
-        const float inverse = scale_inverse(byte);
-        uint2 q;
-        q.x = to_e4m3(v[0][j] * inverse, v[1][j] * inverse, v[2][j] * inverse, v[3][j] * inverse);
-        q.y = to_e4m3(v[4][j] * inverse, v[5][j] * inverse, v[6][j] * inverse, v[7][j] * inverse);
+        const float scale = scale_value(byte);
+        const uint2 q = make_uint2(to_e4m3(v[0][j], v[1][j], v[2][j], v[3][j], scale), to_e4m3(v[4][j], v[5][j], v[6][j], v[7][j], scale));
         lds.column[c][rg ^ cg] = q;
         if (rg == 0 && c0 + c < limit) {
             uint8_t* at = scales + (static_cast<size_t>(block >> 2) * matrix_rows + base + c0 + c) * 4;
@@ -217,16 +207,12 @@ __device__ __forceinline__ void pack_tile_rows(const float (&v)[8][8], uint8_t* 
     const int cg = threadIdx.x & 15, rg = threadIdx.x >> 4;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        float top = 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) top = fmaxf(top, finite_abs(v[i][j]));
-        const uint32_t byte = scale_byte(row16_max(top));
-        const float inverse = scale_inverse(byte);
+        const uint32_t byte = scale_byte(row16_max(top_of<8>([&](int j) { return v[i][j]; })));
+        const float scale = scale_value(byte);
         if (rg * 8 + i < n_rows) {
             const size_t row = first + rg * 8 + i;
             *reinterpret_cast<uint2*>(values + row * pitch + static_cast<size_t>(block) * kBlock + cg * 8) =
-                make_uint2(to_e4m3(v[i][0] * inverse, v[i][1] * inverse, v[i][2] * inverse, v[i][3] * inverse),
-                           to_e4m3(v[i][4] * inverse, v[i][5] * inverse, v[i][6] * inverse, v[i][7] * inverse));
+                make_uint2(to_e4m3(v[i][0], v[i][1], v[i][2], v[i][3], scale), to_e4m3(v[i][4], v[i][5], v[i][6], v[i][7], scale));
             if (cg == 0) {
                 uint8_t* at = scales + (static_cast<size_t>(block >> 2) * matrix_rows + row) * 4;
                 at[block & 3] = static_cast<uint8_t>(byte);
@@ -256,24 +242,44 @@ __device__ __forceinline__ void tile_sums(const float (&v)[8][8], TileLds& lds, 
     if (tid < kBlock && c0 + tid < limit) out[c0 + tid] = (lds.top[0][tid] + lds.top[1][tid]) + (lds.top[2][tid] + lds.top[3][tid]);
 }
 
-template <int SOURCE>
-__device__ __forceinline__ void load_source(const TileParams& p, int which, size_t matrix_scales, size_t row, size_t scale_row, int matrix_rows, int c, float (&f)[8]) {
-    if constexpr (SOURCE == FROM_PACKED) {
-        const int pitch = blocks_of(p.K) * kBlock;
-        const uint2 q = *reinterpret_cast<const uint2*>(p.q[which] + row * pitch + c);
-        const uint32_t s = p.s[which][matrix_scales + static_cast<size_t>(c >> 9) * matrix_rows + scale_row];
-        const float scale = scale_value((s >> (8 * ((c >> 7) & 3))) & 255u);
-        from_e4m3(q.x, f);
-        from_e4m3(q.y, f + 4);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] *= scale;
-    } else {
-        load8<SOURCE == FROM_BF16>(p.x, row * p.K + c, f);
+// Eight neighbouring values of a row as they lie in memory.
+template <int SOURCE> struct Eight {
+    piece_t v[SOURCE == FROM_F32 ? 2 : 1];
+    __device__ __forceinline__ void load(const TileParams& p, size_t row, int c) {
+        const size_t at = row * p.K + c;
+        if constexpr (SOURCE == FROM_BF16) {
+            v[0] = *reinterpret_cast<const piece_t*>(static_cast<const uint16_t*>(p.x) + at);
+        } else {
+            v[0] = *reinterpret_cast<const piece_t*>(static_cast<const float*>(p.x) + at);
+            v[1] = *reinterpret_cast<const piece_t*>(static_cast<const float*>(p.x) + at + 4);
+        }
     }
-}
+    __device__ __forceinline__ void unpack(float (&f)[8]) const {
+        if constexpr (SOURCE == FROM_BF16) {
+            Piece<true>::unpack(v[0], f);
+        } else {
+            Piece<false>::unpack(v[0], f);
+            Piece<false>::unpack(v[1], f + 4);
+        }
+    }
+};
+struct EightPacked {
+    uint2 q; uint32_t s;
+    // matrix_scales: first dword of the matrix's scales; scale_row, of scale_rows: the row there
+    __device__ __forceinline__ void load(const uint8_t* values, const uint32_t* scales, int pitch, size_t row, int c, size_t matrix_scales, size_t scale_row, int scale_rows) {
+        q = *reinterpret_cast<const uint2*>(values + row * pitch + c);
+        s = scales[matrix_scales + static_cast<size_t>(c >> 9) * scale_rows + scale_row];
+    }
+    __device__ __forceinline__ void unpack(int c, float (&f)[8]) const {
+        const float scale = scale_value((s >> (8 * ((c >> 7) & 3))) & 255u);
+        from_e4m3(q.x, scale, f);
+        from_e4m3(q.y, scale, f + 4);
+    }
+};
+template <> struct Eight<FROM_PACKED> : EightPacked {};
 
-// ACT: dy in `x`, the packed pre-activations in q and s
-template <int SOURCE, bool ACT>
+// ACT (an etr_act): dy in `x`, the packed pre-activations in q and s
+template <int SOURCE, int ACT>
 __global__ __launch_bounds__(kThreads, 2) void pack_tiles_kernel(TileParams p) {
     __shared__ TileLds lds;
     const int tid = threadIdx.x, cg = tid & 15, rg = tid >> 4;
@@ -289,40 +295,66 @@ __global__ __launch_bounds__(kThreads, 2) void pack_tiles_kernel(TileParams p) {
     const int n_rows = min(kBlock, __builtin_amdgcn_readlane(g.count, e) - block * kBlock);
     const size_t first = static_cast<size_t>(__builtin_amdgcn_readlane(g.first, e)) + static_cast<size_t>(block) * kBlock;
     const bool nothing = direct && n_rows <= 0;          // an expert without rows: zeros for its sums, and no block
-    const int n_halves = ACT && p.act == ETR_ACT_SWIGLU ? 2 : 1;
+    constexpr bool FAST = SOURCE == FROM_BF16;           // (of the exponential's rounding 8 bits show nothing)
+    constexpr bool GLU = ACT == ETR_ACT_SWIGLU;
+    constexpr int n_halves = GLU ? 2 : 1;
 
+    // everything is requested before the first is used; past the ends the last row or columns again, which count as zeros
+    Eight<SOURCE> from[8];
+    EightPacked pre[ACT != ETR_ACT_NONE ? 8 : 1], up[GLU ? 8 : 1];
+    const int pitch = blocks_of(p.K) * kBlock, cc = min(c, p.K - 8);
+    if (!nothing) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const size_t row = first + min(rg * 8 + i, n_rows - 1);
+            if constexpr (SOURCE == FROM_PACKED) {
+                // a stack's matrices have scales of their own
+                from[i].load(p.q[0], p.s[0], pitch, row, cc, p.stacked ? static_cast<size_t>(e) * scale_groups_of(p.K) * p.rows : 0,
+                             p.stacked ? row - static_cast<size_t>(e) * p.rows : row, p.rows);
+            } else {
+                from[i].load(p, row, cc);
+            }
+            if constexpr (ACT != ETR_ACT_NONE) pre[i].load(p.q[0], p.s[0], pitch, row, cc, 0, row, p.rows);
+            if constexpr (GLU) up[i].load(p.q[1], p.s[1], pitch, row, cc, 0, row, p.rows);
+        }
+    }
     float v[8][8];
-    // (both halves load anew: the second time from the caches)
+#pragma unroll
     for (int h = 0; h < n_halves; ++h) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const bool in = rg * 8 + i < n_rows && c < p.K;
-            const size_t row = first + rg * 8 + i;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-            if (!in) continue;
-            if constexpr (SOURCE == FROM_PACKED) {
-                // a stack's matrices have scales of their own
-                const size_t matrix_scales = p.stacked ? static_cast<size_t>(e) * scale_groups_of(p.K) * p.rows : 0;
-                load_source<FROM_PACKED>(p, 0, matrix_scales, row, p.stacked ? row - static_cast<size_t>(e) * p.rows : row, p.rows, c, v[i]);
-            } else {
-                load_source<SOURCE>(p, 0, 0, row, row, p.rows, c, v[i]);
+            // (both halves begin with what was loaded: nothing worked out for the first is kept for the second, 64 registers a value)
+            if constexpr (GLU) {
+                asm volatile("" : "+v"(from[i].v[0]), "+v"(pre[i].q.x), "+v"(pre[i].q.y), "+v"(pre[i].s));
+                if constexpr (SOURCE == FROM_F32) asm volatile("" : "+v"(from[i].v[1]));
             }
-            if constexpr (ACT) {
+            if constexpr (SOURCE == FROM_PACKED) from[i].unpack(cc, v[i]);
+            else from[i].unpack(v[i]);
+            if constexpr (ACT != ETR_ACT_NONE) {
                 float a[8], b[8];
-                load_source<FROM_PACKED>(p, 0, 0, row, row, p.rows, c, a);
-                if (p.act == ETR_ACT_SWIGLU && h == 0) load_source<FROM_PACKED>(p, 1, 0, row, row, p.rows, c, b);
+                pre[i].unpack(cc, a);
+                if constexpr (ACT == ETR_ACT_GELU) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    if (p.act == ETR_ACT_GELU) {
-                        v[i][j] *= normal_cdf<false>(a[j]) + a[j] * 0.39894228040143268f * gaussian_f32(a[j]);
-                    } else {
-                        const float sg = sigmoid<false>(a[j]);
-                        if (h) v[i][j] *= a[j] * sg;
-                        else v[i][j] *= (p.act == ETR_ACT_SWIGLU ? b[j] : 1.0f) * (sg * (1.0f + a[j] * (1.0f - sg)));
+                    for (int j = 0; j < 8; ++j)
+                        v[i][j] *= normal_cdf<FAST>(a[j]) + a[j] * 0.39894228040143268f * (FAST ? __expf(-0.5f * a[j] * a[j]) : gaussian_f32(a[j]));
+                } else {
+                    if (GLU && h == 0) {
+                        up[i].unpack(cc, b);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) v[i][j] *= b[j];
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float sg = sigmoid<FAST>(a[j]);
+                        v[i][j] *= h ? a[j] * sg : sg * (1.0f + a[j] * (1.0f - sg));
                     }
                 }
             }
+            if (rg * 8 + i >= n_rows || c >= p.K) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+            }
+            __builtin_amdgcn_sched_barrier(0);           // one row at a time: keeps the live set small
         }
         if (p.row_q && !nothing) {
             pack_tile_rows(v, p.row_q, p.row_pitch, p.row_s, h * per_half + nb, h == n_halves - 1 && nb == per_half - 1, first, n_rows, p.rows);
@@ -382,7 +414,7 @@ dim3 rows_grid(const RowsParams& p, int matrices) {
 }
 int chunks_at_most(int rows, int E, bool stacked) { return stacked ? E * blocks_of(rows) : rows / kBlock + std::min(E, rows); }
 
-template <int SOURCE, bool ACT>
+template <int SOURCE, int ACT>
 hipError_t launch_tiles(const TileParams& p, int chunks, hipStream_t st) {
     hipLaunchKernelGGL((pack_tiles_kernel<SOURCE, ACT>), dim3(static_cast<unsigned>(blocks_of(p.K)) * chunks), dim3(kThreads), 0, st, p);
     return hipGetLastError();
@@ -435,8 +467,8 @@ hipError_t launch_pack_columns(const etr_pack_config& c, const void* x, const et
     p.column_q = static_cast<uint8_t*>(values); p.column_s = static_cast<uint8_t*>(scales); p.column_rows = c.K;
     if (half >= 0) { p.half_blocks = blocks_of(c.rows); p.half = half; }
     const int chunks = chunks_at_most(c.rows, c.E, p.stacked);
-    if (packed) return launch_tiles<FROM_PACKED, false>(p, chunks, st);
-    return c.dtype == ETR_BF16 ? launch_tiles<FROM_BF16, false>(p, chunks, st) : launch_tiles<FROM_F32, false>(p, chunks, st);
+    if (packed) return launch_tiles<FROM_PACKED, ETR_ACT_NONE>(p, chunks, st);
+    return c.dtype == ETR_BF16 ? launch_tiles<FROM_BF16, ETR_ACT_NONE>(p, chunks, st) : launch_tiles<FROM_F32, ETR_ACT_NONE>(p, chunks, st);
 }
 
 size_t packed_act_ws_bytes(const etr_linear_config& c) {
@@ -447,7 +479,7 @@ hipError_t launch_packed_act_backward(const etr_linear_config& c, const void* dy
                                 const etr_packed* d8, const etr_packed* dt8, float* dbias, float* dbias_up, void* ws, hipStream_t st) {
     const bool glu = c.act == ETR_ACT_SWIGLU, direct = dbias && c.rows <= kBlock;
     TileParams p{};
-    p.x = dy; p.offsets = offsets; p.rows = c.rows; p.E = c.E; p.K = c.N; p.act = c.act;
+    p.x = dy; p.offsets = offsets; p.rows = c.rows; p.E = c.E; p.K = c.N;
     const etr_packed* pre[2] = {pre8, pre_up8};
     for (int i = 0; i < 2; ++i)
         if (pre[i]) { p.q[i] = static_cast<const uint8_t*>(pre[i]->values); p.s[i] = static_cast<const uint32_t*>(pre[i]->scales); }
@@ -461,8 +493,13 @@ hipError_t launch_packed_act_backward(const etr_linear_config& c, const void* dy
     else if (dbias) p.part = static_cast<float*>(ws);
     const int chunks = direct ? c.E : p.chunks;
     const bool bf16 = c.dtype == ETR_BF16;
-    hipError_t err = c.act == ETR_ACT_NONE ? (bf16 ? launch_tiles<FROM_BF16, false>(p, chunks, st) : launch_tiles<FROM_F32, false>(p, chunks, st))
-                                           : (bf16 ? launch_tiles<FROM_BF16, true>(p, chunks, st) : launch_tiles<FROM_F32, true>(p, chunks, st));
+    hipError_t err = hipErrorInvalidValue;
+    switch (c.act) {
+        case ETR_ACT_NONE: err = bf16 ? launch_tiles<FROM_BF16, ETR_ACT_NONE>(p, chunks, st) : launch_tiles<FROM_F32, ETR_ACT_NONE>(p, chunks, st); break;
+        case ETR_ACT_SILU: err = bf16 ? launch_tiles<FROM_BF16, ETR_ACT_SILU>(p, chunks, st) : launch_tiles<FROM_F32, ETR_ACT_SILU>(p, chunks, st); break;
+        case ETR_ACT_GELU: err = bf16 ? launch_tiles<FROM_BF16, ETR_ACT_GELU>(p, chunks, st) : launch_tiles<FROM_F32, ETR_ACT_GELU>(p, chunks, st); break;
+        case ETR_ACT_SWIGLU: err = bf16 ? launch_tiles<FROM_BF16, ETR_ACT_SWIGLU>(p, chunks, st) : launch_tiles<FROM_F32, ETR_ACT_SWIGLU>(p, chunks, st); break;
+    }
     if (err != hipSuccess || !p.part) return err;
     hipLaunchKernelGGL(join_sums_kernel, dim3((c.N + 63) / 64, c.E, glu ? 2 : 1), dim3(1024), 0, st, p, dbias, dbias_up);
     return hipGetLastError();

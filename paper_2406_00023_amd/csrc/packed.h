@@ -17,24 +17,39 @@ inline size_t scale_bytes(size_t count, int K) { return count * 4 * static_cast<
 
 namespace {
 
-// The byte of the smallest power of two, 2^-127 at least, by which a magnitude comes to 448 = 1.75 x 2^8 or less, and the power's inverse.
+// The byte of the smallest power of two, 2^-127 at least, by which a magnitude comes to 448 = 1.75 x 2^8 or less.
 __device__ __forceinline__ uint32_t scale_byte(float top) {
     const uint32_t bits = __float_as_uint(top);
     return static_cast<uint32_t>(max(static_cast<int>(bits >> 23) - 8 + ((bits & 0x7FFFFFu) > 0x600000u ? 1 : 0), 0));
 }
-__device__ __forceinline__ float scale_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
 // 2^(byte - 127); byte 0 is below the normal numbers
 __device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(byte ? byte << 23 : 0x400000u); }
 // magnitude that takes part in a block's largest: NaN and infinities have none
 __device__ __forceinline__ float finite_abs(float v) { return fabsf(v) < __builtin_inff() ? fabsf(v) : 0.f; }
-// four values, lowest byte first.  (An infinity stays one under any power, and is converted to NaN, as NaN is; what is finite is 448 at most.)
-__device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d) {
-    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-    return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true));
+// Largest magnitude of what is finite among n values: NaN is no operand to a maximum, and infinities are looked at only where there are any.
+template <int N, class F>
+__device__ __forceinline__ float top_of(F&& value) {
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(value(i)));
+    if (__builtin_expect(__any(top == __builtin_inff()), 0)) {
+        top = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) top = fmaxf(top, finite_abs(value(i)));
+    }
+    return top;
 }
-__device__ __forceinline__ void from_e4m3(uint32_t v, float* f) {
-    f[0] = __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(v), 0); f[1] = __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(v), 1);
-    f[2] = __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(v), 2); f[3] = __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(v), 3);
+// four values divided by their power of two, lowest byte first.  (An infinity stays one under any power, and is converted to NaN, as NaN is;
+// what is finite is 448 at most.)
+__device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d, float scale) {
+    typedef short i16x2 __attribute__((ext_vector_type(2)));
+    const i16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(i16x2{0, 0}, a, b, scale, false);
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, c, d, scale, true));
+}
+// four packed values, times their power of two
+__device__ __forceinline__ void from_e4m3(uint32_t v, float scale, float* f) {
+    const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(v, scale, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(v, scale, true);
+    f[0] = lo[0]; f[1] = lo[1]; f[2] = hi[0]; f[3] = hi[1];
 }
 
 // Largest over the 16 lanes of a row of lanes, in all of them.  All lanes active.

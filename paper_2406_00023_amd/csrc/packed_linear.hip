@@ -362,11 +362,8 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void packed_tiles_kernel(PackedPara
                     for (int jb = 0; jb < NO; ++jb)
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
-                            float four = 0.f;
-#pragma unroll
-                            for (int v = 0; v < 4; ++v) four = fmaxf(four, finite_abs(acc[i][j0 + jb][4 * q + v]));
-                            if (ragged && n_wave + jb * 32 + 8 * q + 4 * h >= p.N) four = 0.f;
-                            top = fmaxf(top, four);
+                            const float four = top_of<4>([&](int v) { return acc[i][j0 + jb][4 * q + v]; });
+                            top = ragged && n_wave + jb * 32 + 8 * q + 4 * h >= p.N ? top : fmaxf(top, four);
                         }
                     top = fmaxf(top, __shfl_xor(top, 32));
                     if (h == 0) tops[wn][(wm * MB + i) * 32 + (l & 31)] = top;
@@ -383,14 +380,14 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void packed_tiles_kernel(PackedPara
 #pragma unroll
                     for (int w = 1; w < kColumnWaves; ++w) top = fmaxf(top, tops[w0 + w][m]);
                     const uint32_t byte = scale_byte(top);
-                    const float inverse = scale_inverse(byte);
+                    const float scale = scale_value(byte);
 #pragma unroll
                     for (int jb = 0; jb < NO; ++jb)
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
                             const int c = wn * NO * 32 + jb * 32 + 8 * q + 4 * h;
                             const f32x16& a = acc[i][j0 + jb];
-                            uint32_t four = to_e4m3(a[4 * q] * inverse, a[4 * q + 1] * inverse, a[4 * q + 2] * inverse, a[4 * q + 3] * inverse);
+                            uint32_t four = to_e4m3(a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3], scale);
                             if (ragged && t.n0 + c >= p.N) four = 0u;
                             *reinterpret_cast<uint32_t*>(room + place(m, c >> 4) + (c & 15)) = four;
                         }
@@ -645,9 +642,9 @@ __global__ __launch_bounds__(512 * KS, 2) void packed_rows_kernel(PackedParams p
 #pragma unroll
             for (int w = 1; w < NW; ++w) top = fmaxf(top, tops[w][l16]);
             const uint32_t byte = scale_byte(top);
-            const float inverse = scale_inverse(byte);
+            const float scale = scale_value(byte);
             if (row_in && n < Np)
-                *reinterpret_cast<uint32_t*>(to + (first + l16) * Np + n) = n < p.N ? to_e4m3(v[0] * inverse, v[1] * inverse, v[2] * inverse, v[3] * inverse) : 0u;
+                *reinterpret_cast<uint32_t*>(to + (first + l16) * Np + n) = n < p.N ? to_e4m3(v[0], v[1], v[2], v[3], scale) : 0u;
             if (row_in && wave == 0 && kq == 0) {
                 const int block = t.n0 / kBlock;
                 uint8_t* at = scales + (static_cast<size_t>(block >> 2) * p.rows + first + l16) * 4;
