@@ -3,7 +3,6 @@
 #pragma once
 
 #include "row_ops.h"
-#include "tiles.h"
 
 namespace etr {
 

@@ -38,6 +38,91 @@ struct PackedParams {
     int NT;                                              // column tiles
 };
 
+enum Product { FORWARD = 0, WEIGHT = 1 };                // y (or dx), dw
+
+// count: rows of the group; limit: the tile stores rows below it; half: WEIGHT with SwiGLU, which of the two outputs
+struct Tile { int e, first, m0, n0, count, limit, half; };
+
+// The tile list: experts one after the other; inside one bands of 8 row tiles, in a band the row tiles of a column tile next to
+// each other.  Each XCD (workgroups go round them) has a contiguous part of the list, so its 32 CUs work on some 8 x 4 tiles at once and share
+// 8 + 4 operand slabs in its L2.  The parts are equal in work: a tile of WEIGHT takes as long as its expert has rows (16 experts of 600 to 1700 rows,
+// 2048 x 11264: equal numbers of tiles 547 us, equal work see below).
+// SPLIT (one workgroup to a CU): where the last round over an XCD's CUs would keep half of them or fewer busy, its tiles go in halves or quarters
+// of their rows to as many workgroups.
+template <int MODE, bool SPLIT>
+struct TileList {
+    int tiles, tiles_incl;                               // of a lane's expert; WEIGHT: of every expert the same, and not used
+    int start, end, per_xcd;                             // this XCD's part of the list; workgroups that share it
+    __device__ __forceinline__ void load(const PackedParams& p, const Segments& seg, int BM, int bid, int grid) {
+        const int xcd = bid & 7;
+        per_xcd = grid >> 3;
+        tiles = tiles_incl = 0;
+        if (MODE == WEIGHT) {
+            const int each = (p.M + BM - 1) / BM * (p.glu ? 2 : 1) * p.NT, lane = threadIdx.x & 63;
+            const long long weight = lane < p.E ? seg.blocks + 4 : 0, incl = wave_scan_incl(weight * each);
+            auto at = [](long long v, int e) {
+                return static_cast<long long>(static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), e))) |
+                                              static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v >> 32), e))) << 32);
+            };
+            const long long all = at(incl, 63);
+            auto border = [&](int x) {                   // first tile of XCD x
+                if (x == 8) return p.E * each;
+                const long long target = all / 8 * x;
+                const int e = __builtin_ctzll(__ballot(incl > target));
+                const long long w = at(weight, e), in = target - (at(incl, e) - w * each);
+                return e * each + static_cast<int>((in + w - 1) / w);
+            };
+            start = border(xcd);
+            end = border(xcd + 1);
+        } else {
+            tiles = (seg.count + BM - 1) / BM;
+            tiles_incl = wave_scan_incl(tiles);
+            const int all = __builtin_amdgcn_readlane(tiles_incl, 63) * p.NT, share = (all + 7) >> 3;
+            start = xcd * share;
+            end = min(start + share, all);
+        }
+    }
+    __device__ __forceinline__ bool find(const PackedParams& p, const Segments& seg, int BM, int BN, int j, Tile& t) const {
+        const int share = end - start;
+        int part = 0, parts_log = 0;
+        if constexpr (SPLIT) {
+            const int full = share / per_xcd * per_xcd, rest = share - full;
+            if (j >= full) {
+                parts_log = rest * 4 <= per_xcd ? 2 : rest * 2 <= per_xcd ? 1 : 0;
+                part = (j - full) & ((1 << parts_log) - 1);
+                j = full + ((j - full) >> parts_log);
+            }
+        }
+        if (j >= share) return false;
+        const int q = start + j;
+        int in, rows, MTw = 0;
+        if (MODE == WEIGHT) {
+            MTw = (p.M + BM - 1) / BM;
+            rows = MTw * (p.glu ? 2 : 1);
+            t.e = q / (rows * p.NT);
+            in = q - t.e * (rows * p.NT);
+        } else {
+            t.e = __builtin_ctzll(__ballot(tiles_incl * p.NT > q));
+            rows = __builtin_amdgcn_readlane(tiles, t.e);
+            in = q - (__builtin_amdgcn_readlane(tiles_incl, t.e) - rows) * p.NT;
+        }
+        const int band = in / (8 * p.NT), in_band = in - band * 8 * p.NT, height = min(8, rows - band * 8);
+        const int nt = in_band / height, mt = band * 8 + in_band - nt * height;
+        t.first = __builtin_amdgcn_readlane(seg.first, t.e);
+        t.count = __builtin_amdgcn_readlane(seg.count, t.e);
+        t.half = MODE == WEIGHT && mt >= MTw ? 1 : 0;
+        t.m0 = (mt - t.half * MTw) * BM;
+        t.n0 = nt * BN;
+        t.limit = MODE == WEIGHT ? p.M : t.count;
+        if (SPLIT && parts_log) {                        // (a part past the last row stores nothing: it stays at the tile's start)
+            const int of_part = BM >> parts_log, m0 = t.m0 + part * of_part;
+            t.limit = m0 < t.limit ? min(t.limit, m0 + of_part) : t.m0;
+            t.m0 = t.limit > t.m0 ? m0 : t.m0;
+        }
+        return true;
+    }
+};
+
 // What the copies of one operand need: 64-bit base of a tile's first row in this k-tile, and the buffer bound.
 constexpr uint32_t kRange = 0xFFFFFF00u, kPast = 0xFFFFFF80u;         // an offset past any buffer: such a lane copies zeros
 
@@ -47,22 +132,28 @@ __device__ __forceinline__ v4i descriptor(uint64_t base) {
     return v4i{static_cast<int>(lo), static_cast<int>(hi & 0xFFFFu), static_cast<int>(kRange), 0x00027000};
 }
 // Copies into LDS, 16 or 4 bytes a lane, lane after lane from `at`.  In assembly, without an output: the compiler would otherwise take every
-// later read of LDS to wait for them; they are waited for by count (wait_copies).
+// later read of LDS to wait for them; they are waited for by hand.
 __device__ __forceinline__ void copy16(v4i from, uint32_t off, uint32_t at) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(from) : "memory", "m0");
 }
 __device__ __forceinline__ void copy4(v4i from, uint32_t off, uint32_t at) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(from) : "memory", "m0");
 }
-// at most n vector memory operations outstanding, and every read of LDS done
+// at most N of this wave's vector memory operations are outstanding
 template <int N> __device__ __forceinline__ void wait_copies() {
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0070);
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0F70);
     asm volatile("" ::: "memory");
 }
+// what stands before it, memory operations and MFMAs, stays there
+__device__ __forceinline__ void fence() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+// this wave's reads of LDS are done
 __device__ __forceinline__ void wait_reads() {
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0xC07F);                  // lgkmcnt(0)
+    __builtin_amdgcn_s_waitcnt(0xC07F);
     asm volatile("" ::: "memory");
 }
 __device__ __forceinline__ void barrier() {
@@ -70,6 +161,8 @@ __device__ __forceinline__ void barrier() {
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
+
+constexpr int kPatch = 2048;                             // LDS of a wave's own, through which its results leave
 
 // eight values of a block as bf16, exactly
 __device__ __forceinline__ bf16x8 widen(int lo, int hi, float scale) {
@@ -115,124 +208,124 @@ __device__ __forceinline__ void load4(const void* p, size_t at, float (&f)[4]) {
 // LDS, an operand of a k-tile: [row][8 pieces of 16 bytes]; the piece at place s of a row is s ^ (row / 2 % 8), so that the rows of a fragment
 // spread over the banks.  Behind both operands their scales, a dword (four k-tiles) for each row.  A fragment's lane has row lane % 32 of its
 // block and 32 of the 64 bytes of half a k-tile; which ones does not matter as long as it is the same for both operands.
-// A workgroup of WM x WN waves has a BM x BN tile at a time; NBUF buffers, of which all but one are on their way.
+// A workgroup of WM x WN waves has a BM x BN tile at a time, and two buffers: while one is multiplied the next k-tile is copied into the other.
 // The MFMAs take the columns' fragment first, so that a lane ends up with runs of four neighbouring columns of one row.
 // WIDE: results in fp32.
-template <bool WIDE, int BM, int BN, int WM, int WN, int NBUF, int MODE, bool GLU, bool WALK>
+template <bool WIDE, int BM, int BN, int WM, int WN, int MODE, bool GLU, bool WALK>
 __global__ __launch_bounds__(WM* WN * 64, 2) void packed_tiles_kernel(PackedParams p) {
     constexpr int NW = WM * WN, MB = BM / WM / 32, NB = BN / WN / 32, NO = GLU ? NB / 2 : NB;
     constexpr int OUT_N = GLU ? BN / 2 : BN;
     constexpr int CA = BM / 8, CB = BN / 8;              // copies of 64 pieces per operand and k-tile
     constexpr int SA = (BM + 63) / 64, SB = BN / 64;     // copies of 64 scales
-    constexpr int CW = (CA + CB) / NW, SW = (SA + SB + NW - 1) / NW;                        // of a wave
-    constexpr int A_BYTES = BM * 128, TILE_BYTES = (BM + BN) * 128, STAGE = TILE_BYTES + (SA + SB) * 256;
+    constexpr int SW = (SA + SB + NW - 1) / NW;
+    constexpr int A_BYTES = BM * kBlock, TILE_BYTES = (BM + BN) * kBlock, STAGE = TILE_BYTES + (SA + SB) * 256;
     constexpr int kColumnWaves = kBlock / (NO * 32);     // waves that share a block of 128 output columns
-    static_assert((CA + CB) % NW == 0 && BN % 64 == 0 && OUT_N % kBlock == 0 && kBlock % (NO * 32) == 0 && (!GLU || NB % 2 == 0), "");
+    static_assert(CA % NW == 0 && CB % NW == 0 && BN % 64 == 0 && OUT_N % kBlock == 0 && kBlock % (NO * 32) == 0 && (!GLU || NB % 2 == 0), "");
+    constexpr int TOPS = WN * BM * 4;                    // bytes of tops
+    // of what is stored: bytes of a value; blocks side by side in a patch; its row's bytes and pieces; rows to a store
+    constexpr bool PATCH = !WIDE;
+    constexpr int ES = WIDE ? 4 : 2, JC = PATCH || NW * 32 * NO * 32 * ES > TILE_BYTES ? 1 : NO, RB = JC * 32 * ES, PR = RB / 16, RP = 64 / PR;
+    constexpr int STORES = MB * NO / JC * (32 / RP);
+    static_assert(NO % JC == 0 && NW * 32 * RB <= TILE_BYTES && (!PATCH || 32 * RB <= kPatch), "");
+    auto spread = [](int row) { return PR == 4 ? (row >> 2) & 3 : row & (PR - 1); };         // rows of a patch over the banks
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    float (*tops)[BM] = reinterpret_cast<float (*)[BM]>(lds + NBUF * STAGE);                 // [WN][BM]
+    float (*tops)[BM] = reinterpret_cast<float (*)[BM]>(lds + 2 * STAGE);                 // [WN][BM]
     const int lane = threadIdx.x & 63, l32 = lane & 31, kh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
     const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr)lds));
 
-    // groups in rows (FORWARD) or in blocks of the contraction (WEIGHT)
     Segments seg;
     seg.load(p.offsets, p.rows, p.E, false);
-    Groups groups;
-    groups.first = seg.first; groups.count = seg.count;
-    groups.tiles = (seg.count + BM - 1) / BM;
-    groups.tiles_incl = wave_scan_incl(groups.tiles);
     Tile t;
     const int bid = blockIdx.x, grid = gridDim.x;
+    TileList<MODE, WALK> list;
+    list.load(p, seg, BM, bid, grid);
     int j = bid >> 3;
-    if (!find_tile<MODE, WALK>(p, groups, BM, OUT_N, bid, grid, j, t)) return;
+    if (!list.find(p, seg, BM, OUT_N, j, t)) return;
 
-    // ---- the copy side: a tile and a k-tile of its own, ahead of the products
-    struct Source { uint64_t base[2], up, scales[2], scales_up; size_t stride[2]; uint32_t at[CW], at_s[SW]; int KT, kt; bool empty; };
+    // ---- the copy side: a tile and a k-tile of its own, ahead of the products.  A wave copies CA / NW and CB / NW times 64 pieces, of B rows that
+    // belong to one of the two weights, and 64 scales (or twice that).
+    constexpr int WA = CA / NW, WB = CB / NW;
+    struct Source { uint64_t a, b, scales[SW], stride[SW]; uint32_t at_a[WA], at_b[WB], at_s[SW]; int KT, kt; };
     Source s;
     bool more = true;                                    // s is a tile that is still to be copied
-    auto row_piece = [&](int c) { return (lane & 7) ^ (((8 * c + (lane >> 3)) >> 1) & 7); };
+    auto copy_row = [&](int c) { return 8 * c + (lane >> 3); };
+    auto copy_piece = [&](int c) { return (lane & 7) ^ ((copy_row(c) >> 1) & 7); };
     auto aim = [&](const Tile& x) {
-        s.kt = 0;
+        uint64_t row_a, row_b, group_a, group_b;         // rows, and dwords of scales, before the tile's
         uint32_t pitch;
-        int last_a, last_b, halves = p.glu ? 2 : 1;
+        uint64_t rows_a;                                 // of the packed matrix
         if constexpr (MODE == WEIGHT) {
             const int blocks = __builtin_amdgcn_readlane(seg.blocks, x.e), before = __builtin_amdgcn_readlane(seg.blocks_incl, x.e) - blocks;
-            const int groups_before = __builtin_amdgcn_readlane(seg.groups_incl, x.e) - __builtin_amdgcn_readlane(seg.groups, x.e);
-            const size_t rows_a = static_cast<size_t>(p.M) * halves;
-            s.empty = blocks == 0;
-            s.KT = max(blocks, 1);
+            const uint64_t groups_before = __builtin_amdgcn_readlane(seg.groups_incl, x.e) - __builtin_amdgcn_readlane(seg.groups, x.e);
+            rows_a = static_cast<uint64_t>(p.M) * (p.glu ? 2 : 1);
+            s.KT = blocks;
             pitch = static_cast<uint32_t>(blocks) * kBlock;
-            const size_t row_a = static_cast<size_t>(x.half) * p.M + x.m0;
-            s.base[0] = reinterpret_cast<uint64_t>(p.A) + static_cast<uint64_t>(before) * kBlock * rows_a + row_a * pitch;
-            s.base[1] = reinterpret_cast<uint64_t>(p.B[0]) + static_cast<uint64_t>(before) * kBlock * p.N + static_cast<uint64_t>(x.n0) * pitch;
-            s.scales[0] = reinterpret_cast<uint64_t>(p.As) + (static_cast<uint64_t>(groups_before) * rows_a + row_a) * 4;
-            s.scales[1] = reinterpret_cast<uint64_t>(p.Bs[0]) + (static_cast<uint64_t>(groups_before) * p.N + x.n0) * 4;
-            s.stride[0] = rows_a * 4;
-            s.stride[1] = static_cast<size_t>(p.N) * 4;
-            last_a = p.M - 1 - x.m0;
+            row_a = static_cast<uint64_t>(x.half) * p.M + x.m0;
+            group_a = groups_before * rows_a + row_a;
+            group_b = groups_before * p.N + x.n0;
+            s.a = reinterpret_cast<uint64_t>(p.A) + static_cast<uint64_t>(before) * kBlock * rows_a + row_a * pitch;
+            s.b = reinterpret_cast<uint64_t>(p.B[0]) + static_cast<uint64_t>(before) * kBlock * p.N + static_cast<uint64_t>(x.n0) * pitch;
         } else {
-            s.empty = false;
+            const int which = GLU && wave >= NW / 2 ? 1 : 0;
+            rows_a = static_cast<uint64_t>(p.rows);
             s.KT = p.blocks;
             pitch = static_cast<uint32_t>(p.blocks) * kBlock;
-            const uint64_t row_a = static_cast<uint64_t>(x.first) + x.m0, row_b = static_cast<uint64_t>(x.e) * p.N + x.n0;
-            const uint64_t groups_b = static_cast<uint64_t>(x.e) * ((p.blocks + 3) / 4) * p.N + x.n0;
-            s.base[0] = reinterpret_cast<uint64_t>(p.A) + row_a * pitch;
-            s.base[1] = reinterpret_cast<uint64_t>(p.B[0]) + row_b * pitch;
-            s.scales[0] = reinterpret_cast<uint64_t>(p.As) + row_a * 4;
-            s.scales[1] = reinterpret_cast<uint64_t>(p.Bs[0]) + groups_b * 4;
-            s.stride[0] = static_cast<size_t>(p.rows) * 4;
-            s.stride[1] = static_cast<size_t>(p.N) * 4;
-            s.up = GLU ? reinterpret_cast<uint64_t>(p.B[1]) + row_b * pitch : 0;
-            s.scales_up = GLU ? reinterpret_cast<uint64_t>(p.Bs[1]) + groups_b * 4 : 0;
-            last_a = x.count - 1 - x.m0;
+            row_a = static_cast<uint64_t>(x.first) + x.m0;
+            row_b = static_cast<uint64_t>(x.e) * p.N + x.n0;
+            group_a = row_a;
+            group_b = static_cast<uint64_t>(x.e) * ((p.blocks + 3) / 4) * p.N + x.n0;
+            s.a = reinterpret_cast<uint64_t>(p.A) + row_a * pitch;
+            s.b = reinterpret_cast<uint64_t>(p.B[which]) + row_b * pitch;
         }
-        last_b = p.N - 1 - x.n0;
-        // (rows past the last one: the last again, whose results are not stored)
+        s.kt = 0;
+        // rows that are not stored are not read, nor is a contraction without a block: zeros
+        const int rows_in = s.KT ? x.limit - x.m0 : 0, columns_in = s.KT ? p.N - x.n0 : 0;
 #pragma unroll
-        for (int i = 0; i < CW; ++i) {
-            const int c = wave * CW + i;
-            if (c < CA) {
-                s.at[i] = static_cast<uint32_t>(min(8 * c + (lane >> 3), last_a)) * pitch + row_piece(c) * 16u;
-            } else {
-                const int r = 8 * (c - CA) + (lane >> 3);
-                s.at[i] = static_cast<uint32_t>(min(GLU && r >= BN / 2 ? r - BN / 2 : r, last_b)) * pitch + row_piece(c - CA) * 16u;
-            }
-            if (s.empty) s.at[i] = kPast;
+        for (int i = 0; i < WA; ++i) {
+            const int c = wave * WA + i, r = copy_row(c);
+            s.at_a[i] = r < rows_in ? static_cast<uint32_t>(r) * pitch + copy_piece(c) * 16u : kPast;
         }
 #pragma unroll
-        for (int i = 0; i < SW; ++i) {
-            const int c = min(wave + i * NW, SA + SB - 1);
-            if (c < SA) {
-                s.at_s[i] = static_cast<uint32_t>(min(64 * c + lane, last_a)) * 4;
-            } else {
-                const int r = 64 * (c - SA) + lane;
-                s.at_s[i] = static_cast<uint32_t>(min(GLU && r >= BN / 2 ? r - BN / 2 : r, last_b)) * 4;
-            }
-            if (s.empty) s.at_s[i] = kPast;
-        }
-    };
-    auto issue = [&](int buf) {
-        const uint32_t dst = lds0 + buf * STAGE;
-#pragma unroll
-        for (int i = 0; i < CW; ++i) {
-            const int c = wave * CW + i;
-            const uint64_t base = c < CA ? s.base[0] : GLU && c >= CA + CB / 2 ? s.up : s.base[1];
-            copy16(descriptor(base + static_cast<uint64_t>(s.kt) * kBlock), s.at[i], dst + c * 1024);
+        for (int i = 0; i < WB; ++i) {
+            const int c = wave * WB + i, r = copy_row(c), n = GLU && r >= BN / 2 ? r - BN / 2 : r;
+            s.at_b[i] = n < columns_in ? static_cast<uint32_t>(n) * pitch + copy_piece(c) * 16u : kPast;
         }
 #pragma unroll
         for (int i = 0; i < SW; ++i) {                   // (waves without one of their own copy the last again)
-            const int c = min(wave + i * NW, SA + SB - 1);
-            const uint64_t base = c < SA ? s.scales[0] : GLU && c >= SA + SB / 2 ? s.scales_up : s.scales[1];
-            copy4(descriptor(base + static_cast<uint64_t>(s.kt >> 2) * s.stride[c < SA ? 0 : 1]), s.at_s[i], dst + TILE_BYTES + c * 256);
+            const int c = min(wave + i * NW, SA + SB - 1), r = 64 * (c < SA ? c : c - SA) + lane, n = GLU && c >= SA && r >= BN / 2 ? r - BN / 2 : r;
+            s.scales[i] = c < SA ? reinterpret_cast<uint64_t>(p.As) + group_a * 4 : reinterpret_cast<uint64_t>(p.Bs[GLU && c >= SA + SB / 2 ? 1 : 0]) + group_b * 4;
+            s.stride[i] = (c < SA ? rows_a : static_cast<uint64_t>(p.N)) * 4;
+            s.at_s[i] = n < (c < SA ? rows_in : columns_in) ? static_cast<uint32_t>(n) * 4 : kPast;
         }
+        s.KT = max(s.KT, 1);
+    };
+    auto issue = [&](int buf) {
+        const uint32_t dst = lds0 + buf * STAGE;
+        const v4i a = descriptor(s.a), b = descriptor(s.b);
+#pragma unroll
+        for (int i = 0; i < WA; ++i) copy16(a, s.at_a[i], dst + (wave * WA + i) * 1024);
+#pragma unroll
+        for (int i = 0; i < WB; ++i) copy16(b, s.at_b[i], dst + A_BYTES + (wave * WB + i) * 1024);
+#pragma unroll
+        for (int i = 0; i < SW; ++i) copy4(descriptor(s.scales[i]), s.at_s[i], dst + TILE_BYTES + min(wave + i * NW, SA + SB - 1) * 256);
     };
     int jn = j;
     auto advance = [&]() {                               // (a source past the last tile goes on copying its last k-tile)
         if (!more) return;
-        if (s.kt + 1 < s.KT) { s.kt += 1; return; }
+        if (s.kt + 1 < s.KT) {
+            s.kt += 1;
+            s.a += kBlock;
+            s.b += kBlock;
+            if ((s.kt & 3) == 0) {
+#pragma unroll
+                for (int i = 0; i < SW; ++i) s.scales[i] += s.stride[i];
+            }
+            return;
+        }
         jn += grid >> 3;
         Tile n;
-        if (find_tile<MODE, WALK>(p, groups, BM, OUT_N, bid, grid, jn, n)) aim(n);
+        if (list.find(p, seg, BM, OUT_N, jn, n)) aim(n);
         else more = false;
     };
 
@@ -240,28 +333,20 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void packed_tiles_kernel(PackedPara
     auto b_block = [&](int jb) { return GLU ? (jb >= NO ? BN / 64 : 0) + wn * NO + (jb >= NO ? jb - NO : jb) : wn * NB + jb; };
     auto fragment = [&](const unsigned char* op, int block, int half) -> v8i {
         const int row = block * 32 + l32, x = (row >> 1) & 7;
-        const v4i lo = *reinterpret_cast<const v4i*>(op + row * 128 + ((4 * half + 2 * kh) ^ x) * 16);
-        const v4i hi = *reinterpret_cast<const v4i*>(op + row * 128 + ((4 * half + 2 * kh + 1) ^ x) * 16);
+        const v4i lo = *reinterpret_cast<const v4i*>(op + row * kBlock + ((4 * half + 2 * kh) ^ x) * 16);
+        const v4i hi = *reinterpret_cast<const v4i*>(op + row * kBlock + ((4 * half + 2 * kh + 1) ^ x) * 16);
         return v8i{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     };
-    auto multiply_row = [&](const v8i& fa, const v8i (&fb)[NB], int sa, const int (&sb)[NB], f32x16 (&c)[NB]) {
+    // first: the sums begin here
+    auto multiply = [&](const v8i (&fa)[MB], const v8i (&fb)[NB], const int (&sa)[MB], const int (&sb)[NB], f32x16 (&c)[MB][NB], auto first) {
+        constexpr f32x16 none{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        constexpr bool FIRST = decltype(first)::value;
         if constexpr (!WIDE) {
 #pragma unroll
-            for (int jb = 0; jb < NB; ++jb) c[jb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[jb], fa, c[jb], 0, 0, 0, sb[jb], 0, sa);
-        } else {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const bf16x8 wa = widen(fa[2 * q], fa[2 * q + 1], scale_value(sa));
+            for (int i = 0; i < MB; ++i)
 #pragma unroll
                 for (int jb = 0; jb < NB; ++jb)
-                    c[jb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(fb[jb][2 * q], fb[jb][2 * q + 1], scale_value(sb[jb])), wa, c[jb], 0, 0, 0);
-            }
-        }
-    };
-    auto multiply = [&](const v8i (&fa)[MB], const v8i (&fb)[NB], const int (&sa)[MB], const int (&sb)[NB], f32x16 (&c)[MB][NB]) {
-        if constexpr (!WIDE) {
-#pragma unroll
-            for (int i = 0; i < MB; ++i) multiply_row(fa[i], fb, sa[i], sb, c[i]);
+                    c[i][jb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[jb], fa[i], FIRST ? none : c[i][jb], 0, 0, 0, sb[jb], 0, sa[i]);
         } else {                                         // every fragment is converted once
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -273,32 +358,31 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void packed_tiles_kernel(PackedPara
 #pragma unroll
                 for (int i = 0; i < MB; ++i)
 #pragma unroll
-                    for (int jb = 0; jb < NB; ++jb) c[i][jb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[jb], wa[i], c[i][jb], 0, 0, 0);
+                    for (int jb = 0; jb < NB; ++jb)
+                        c[i][jb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[jb], wa[i], FIRST && q == 0 ? none : c[i][jb], 0, 0, 0);
             }
         }
     };
     f32x16 acc[MB][NB];
     aim(t);
-#pragma unroll
-    for (int b = 0; b < NBUF - 1; ++b) { issue(b); advance(); }
+    issue(0);
+    advance();
+    wait_copies<0>();
     int buf = 0;
+    bool ahead = false;                                  // the tile's second k-tile is on its way, and behind it
+    bool behind = false;                                 // exactly STORES stores of this wave
     for (;;) {
-#pragma unroll
-        for (int i = 0; i < MB; ++i)
-#pragma unroll
-            for (int jb = 0; jb < NB; ++jb)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) acc[i][jb][v] = 0.f;
         const int KT = MODE == WEIGHT ? max(__builtin_amdgcn_readlane(seg.blocks, t.e), 1) : p.blocks;
-        // row blocks of the wave that have a row to store at all: tiles at the end of an expert's rows multiply what they have, and the
-        // wave beside this one on the SIMD has the matrix pipe for itself meanwhile
-        const int live = t.n0 + wn * NO * 32 < p.N ? min(max((t.limit - t.m0 - wm * MB * 32 + 31) >> 5, 0), MB) : 0;
-        auto k_loop = [&](auto whole) {
-            for (int kt = 0; kt < KT; ++kt) {
-                wait_copies<(NBUF - 2) * (CW + SW)>();   // this wave's part of the k-tile has landed
-                barrier();                               // ... and everybody's; and everybody is done with the buffer before it
-                issue(buf == 0 ? NBUF - 1 : buf - 1);
+        // a wave none of whose rows is stored multiplies nothing (tiles at the end of an expert's rows), and the wave beside it on the SIMD has the
+        // matrix pipe for itself meanwhile
+        const bool live = t.n0 + wn * NO * 32 < p.N && t.limit - t.m0 > wm * MB * 32;
+        for (int kt = 0; kt < KT; ++kt) {
+            barrier();                                   // everybody's part of the k-tile has landed, and everybody is done with the other buffer
+            if (kt > 0 || !ahead) {
+                issue(buf ^ 1);
                 advance();
+            }
+            if (live) {
                 const unsigned char* op = lds + buf * STAGE;
                 const uint32_t* sc = reinterpret_cast<const uint32_t*>(op + TILE_BYTES);
                 const int shift = 8 * (kt & 3);
@@ -312,21 +396,18 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void packed_tiles_kernel(PackedPara
                     v8i fa[MB], fb[NB];
 #pragma unroll
                     for (int jb = 0; jb < NB; ++jb) fb[jb] = fragment(op + A_BYTES, b_block(jb), half);
-                    if constexpr (decltype(whole)::value) {
 #pragma unroll
-                        for (int i = 0; i < MB; ++i) fa[i] = fragment(op, wm * MB + i, half);
-                        multiply(fa, fb, sa, sb, acc);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < MB; ++i)
-                            if (i < live) multiply_row(fragment(op, wm * MB + i, half), fb, sa[i], sb, acc[i]);
-                    }
+                    for (int i = 0; i < MB; ++i) fa[i] = fragment(op, wm * MB + i, half);
+                    if (half == 0 && kt == 0) multiply(fa, fb, sa, sb, acc, std::true_type{});
+                    else multiply(fa, fb, sa, sb, acc, std::false_type{});
                 }
-                buf = buf + 1 == NBUF ? 0 : buf + 1;
             }
-        };
-        if (live == MB) k_loop(std::true_type{});
-        else k_loop(std::false_type{});
+            // this wave's part of the next k-tile has landed, of the next tile's first one too; stores behind it may still be on their way
+            if (kt == 0 && behind) wait_copies<STORES>();
+            else wait_copies<0>();
+            wait_reads();
+            buf ^= 1;
+        }
 
         // ---- the results: lane: row l of a block, columns 8 q + 4 h ... + 3 of it for q = 0 ... 3
         // They leave through the buffer that was multiplied last, which nobody copies into before the next k-tile's barrier.  What is optional
@@ -335,7 +416,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void packed_tiles_kernel(PackedPara
         const int limit = t.limit - t.m0;
         const int n_wave = t.n0 + wn * NO * 32;          // first output column of the wave
         const size_t first = (MODE == WEIGHT ? static_cast<size_t>(t.e) * p.M : static_cast<size_t>(t.first)) + t.m0;
-        unsigned char* room = lds + (buf == 0 ? NBUF - 1 : buf - 1) * STAGE;
+        unsigned char* room = lds + (buf ^ 1) * STAGE;
         auto lane_now = [&]() { int l = lane; asm volatile("" : "+v"(l)); return l; };
         auto pin = [&]() {
 #pragma unroll
@@ -344,12 +425,19 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void packed_tiles_kernel(PackedPara
                 for (int jb = 0; jb < NB; ++jb) asm volatile("" : "+v"(acc[i][jb]));
         };
         pin();
-        wait_reads();
         barrier();                                       // everybody has read it
-        // packs blocks j0 ... j0 + NO - 1 of the accumulators.  room: [row][OUT_N bytes], the pieces of a row in an order of its own
+        // without packed results only the waves' own patches are written, and the next tile's second k-tile can be on its way meanwhile
+        ahead = PATCH && !(MODE == FORWARD && (p.P[0] || p.P[1] || p.P[2]));
+        if (ahead) {
+            issue(buf ^ 1);
+            advance();
+        }
+        // packs blocks j0 ... j0 + NO - 1 of the accumulators, as many row blocks of each wave at a time as there is room for.
+        // room: [row][OUT_N bytes], the pieces of a row in an order of its own
         auto pack = [&](uint8_t* to, uint8_t* scales, auto j0_) {
             constexpr int PR = OUT_N / 16, j0 = decltype(j0_)::value;    // pieces of a row
-            static_assert(BM * OUT_N <= TILE_BYTES, "");
+            constexpr int CI = MB * WM * 32 * OUT_N <= TILE_BYTES ? MB : MB / 2, ROWS = CI * WM * 32;
+            static_assert(MB % CI == 0 && ROWS * OUT_N <= TILE_BYTES && ROWS * PR % (NW * 64) == 0 && NW * 64 % PR == 0, "");
             auto place = [](int row, int piece) { return row * OUT_N + ((piece ^ (OUT_N == 128 ? row >> 1 : row)) & (PR - 1)) * 16; };
             const int Np = blocks_of(p.N) * kBlock, w0 = wn / kColumnWaves * kColumnWaves, block = n_wave / kBlock;
             const bool ragged = n_wave + NO * 32 > p.N;                  // (uniform)
@@ -370,12 +458,13 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void packed_tiles_kernel(PackedPara
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            __syncthreads();
-            {
+#pragma unroll
+            for (int i0 = 0; i0 < MB; i0 += CI) {
+                __syncthreads();
                 const int l = lane_now(), h = l >> 5;
 #pragma unroll
-                for (int i = 0; i < MB; ++i) {
-                    const int m = (wm * MB + i) * 32 + (l & 31);
+                for (int i = i0; i < i0 + CI; ++i) {
+                    const int m = (wm * MB + i) * 32 + (l & 31), row = (wm * CI + i - i0) * 32 + (l & 31);
                     float top = tops[w0][m];
 #pragma unroll
                     for (int w = 1; w < kColumnWaves; ++w) top = fmaxf(top, tops[w0 + w][m]);
@@ -389,7 +478,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void packed_tiles_kernel(PackedPara
                             const f32x16& a = acc[i][j0 + jb];
                             uint32_t four = to_e4m3(a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3], scale);
                             if (ragged && t.n0 + c >= p.N) four = 0u;
-                            *reinterpret_cast<uint32_t*>(room + place(m, c >> 4) + (c & 15)) = four;
+                            *reinterpret_cast<uint32_t*>(room + place(row, c >> 4) + (c & 15)) = four;
                         }
                     if (m < limit && wn == w0 && h == 0 && n_wave < p.N) {
                         uint8_t* at = scales + (static_cast<size_t>(block >> 2) * p.rows + first + m) * 4;
@@ -399,18 +488,15 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void packed_tiles_kernel(PackedPara
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
-            }
-            __syncthreads();
-            {
+                __syncthreads();
                 int tid = threadIdx.x;
                 asm volatile("" : "+v"(tid));
-                const int c = tid % PR, m0 = tid / PR;
+                const int c = tid % PR;
                 uint8_t* base = to + first * Np + t.n0;
-                static_assert(NW * 64 % PR == 0, "");
 #pragma unroll 4
-                for (int u = 0; u < BM * PR / (NW * 64); ++u) {
-                    const int m = u * (NW * 64 / PR) + m0;
-                    const piece_t v = *reinterpret_cast<const piece_t*>(room + place(m, c));
+                for (int u = 0; u < ROWS * PR / (NW * 64); ++u) {
+                    const int row = u * (NW * 64 / PR) + tid / PR, m = (row / (CI * 32) * MB + i0) * 32 + row % (CI * 32);
+                    const piece_t v = *reinterpret_cast<const piece_t*>(room + place(row, c));
                     if (m < limit && t.n0 + c * 16 < Np) *reinterpret_cast<piece_t*>(base + static_cast<size_t>(m) * Np + c * 16) = v;
                 }
             }
@@ -492,44 +578,56 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void packed_tiles_kernel(PackedPara
         }
         void* C = p.C[MODE == WEIGHT ? t.half : 0];
         if (C) {
-            // 32 rows of the wave's columns at a time through its own part of the room, so that they leave as whole pieces side by side
-            constexpr int ES = WIDE ? 4 : 2, RB = NO * 32 * ES, PR = RB / 16, RP = 64 / PR;                  // bytes, pieces of a row; rows to a store
-            static_assert(NW * 32 * RB <= TILE_BYTES, "");
+            // 32 rows of the wave's columns (JC blocks of them) at a time through its patch, or through its part of the room, so that they leave as
+            // whole pieces side by side
             const int l = lane_now(), h = l >> 5;
-            unsigned char* patch = room + wave * 32 * RB;
-            const int row_in = l / PR, piece = l % PR, n = n_wave + piece * (16 / ES);
+            unsigned char* patch = PATCH ? lds + 2 * STAGE + TOPS + wave * kPatch : room + wave * 32 * RB;
+            const int row_in = l / PR, piece = l % PR;
             char* base = static_cast<char*>(C) + first * p.N * ES;
+            const bool full = (wm + 1) * MB * 32 <= limit && n_wave + NO * 32 <= p.N;        // (uniform over the wave)
+            behind = PATCH && ahead && full;
 #pragma unroll
             for (int i = 0; i < MB; ++i) {
                 if ((wm * MB + i) * 32 < limit) {        // (uniform)
 #pragma unroll
-                    for (int jb = 0; jb < NO; ++jb)
+                    for (int j0 = 0; j0 < NO; j0 += JC) {
+                        const int n = n_wave + j0 * 32 + piece * (16 / ES);
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const int at = (jb * 32 + 8 * q + 4 * h) * ES;
-                            const float f[4] = {acc[i][jb][4 * q], acc[i][jb][4 * q + 1], acc[i][jb][4 * q + 2], acc[i][jb][4 * q + 3]};
-                            store4<WIDE>(patch + (l & 31) * RB + ((at >> 4) ^ (l & (PR - 1))) * 16 + (at & 15), 0, f);
+                        for (int jb = 0; jb < JC; ++jb)
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                const int at = (jb * 32 + 8 * q + 4 * h) * ES;
+                                const f32x16& a = acc[i][j0 + jb];
+                                const float f[4] = {a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
+                                store4<WIDE>(patch + (l & 31) * RB + ((at >> 4) ^ spread(l & 31)) * 16 + (at & 15), 0, f);
+                            }
+                        wave_sync();
+                        piece_t out[32 / RP];
+#pragma unroll
+                        for (int u = 0; u < 32 / RP; ++u) {
+                            const int row = u * RP + row_in;
+                            out[u] = *reinterpret_cast<const piece_t*>(patch + row * RB + (piece ^ spread(row)) * 16);
                         }
-                    wave_sync();
-                    piece_t out[32 / RP];
+                        wave_sync();
+                        char* at = base + (static_cast<size_t>((wm * MB + i) * 32 + row_in) * p.N + n) * ES;
+                        if (full) {
 #pragma unroll
-                    for (int u = 0; u < 32 / RP; ++u) {
-                        const int row = u * RP + row_in;
-                        out[u] = *reinterpret_cast<const piece_t*>(patch + row * RB + (piece ^ (row & (PR - 1))) * 16);
-                    }
-                    wave_sync();
+                            for (int u = 0; u < 32 / RP; ++u) *reinterpret_cast<piece_t*>(at + static_cast<size_t>(u * RP) * p.N * ES) = out[u];
+                        } else {
 #pragma unroll
-                    for (int u = 0; u < 32 / RP; ++u) {
-                        const int m = (wm * MB + i) * 32 + u * RP + row_in;
-                        if (m < limit && n < p.N) *reinterpret_cast<piece_t*>(base + (static_cast<size_t>(m) * p.N + n) * ES) = out[u];
+                            for (int u = 0; u < 32 / RP; ++u)
+                                if ((wm * MB + i) * 32 + u * RP + row_in < limit && n < p.N) *reinterpret_cast<piece_t*>(at + static_cast<size_t>(u * RP) * p.N * ES) = out[u];
+                        }
                     }
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
+        } else {
+            behind = false;
         }
         j += grid >> 3;
-        if (!find_tile<MODE, WALK>(p, groups, BM, OUT_N, bid, grid, j, t)) break;
-        if constexpr (NBUF > 2) wait_copies<0>();        // (the stores too: the counted waits are for copies alone)
+        if (!list.find(p, seg, BM, OUT_N, j, t)) break;
+        wait_reads();
     }
     wait_copies<0>();                                    // the copies that nobody needed
 }
@@ -548,13 +646,10 @@ __global__ __launch_bounds__(512 * KS, 2) void packed_rows_kernel(PackedParams p
     const int wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = wave_all % NW, group = wave_all / NW;
     Segments seg;
     seg.load(p.offsets, p.rows, p.E, false);
-    Groups groups;
-    groups.first = seg.first; groups.count = seg.count;
-    groups.tiles = (seg.count + BM - 1) / BM;
-    groups.tiles_incl = wave_scan_incl(groups.tiles);
+    TileList<FORWARD, false> list;
+    list.load(p, seg, BM, blockIdx.x, gridDim.x);
     Tile t;
-    const int bid = blockIdx.x, grid = gridDim.x;
-    for (int j = bid >> 3; find_tile<FORWARD, false>(p, groups, BM, kBlock, bid, grid, j, t); j += grid >> 3) {
+    for (int j = blockIdx.x >> 3; list.find(p, seg, BM, kBlock, j, t); j += gridDim.x >> 3) {
         const size_t pitch = static_cast<size_t>(p.blocks) * kBlock, first = static_cast<size_t>(t.first) + t.m0;
         const int rows_left = t.count - t.m0, n0 = t.n0 + wave * 16, G = (p.blocks + 3) / 4;
         const size_t row_a = first + min(l16, rows_left - 1), row_b = min(n0 + l16, p.N - 1);
@@ -685,11 +780,11 @@ long long tiles_at_most(const PackedParams& p, int mode, int BM, int out_n) {
     return columns * (p.rows / BM + std::min(p.E, p.rows));
 }
 
-template <bool WIDE, int BM, int BN, int WM, int WN, int NBUF, int MODE, bool GLU, bool WALK>
+template <bool WIDE, int BM, int BN, int WM, int WN, int MODE, bool GLU, bool WALK>
 hipError_t launch_tiles(PackedParams p, hipStream_t st) {
     constexpr int out_n = GLU ? BN / 2 : BN;
-    constexpr size_t lds = static_cast<size_t>(NBUF) * ((BM + BN) * 128 + ((BM + 63) / 64 + BN / 64) * 256) + WN * BM * 4;
-    auto kern = packed_tiles_kernel<WIDE, BM, BN, WM, WN, NBUF, MODE, GLU, WALK>;
+    constexpr size_t lds = 2 * static_cast<size_t>((BM + BN) * kBlock + ((BM + 63) / 64 + BN / 64) * 256) + WN * BM * 4 + (WIDE ? 0 : WM * WN * kPatch);
+    auto kern = packed_tiles_kernel<WIDE, BM, BN, WM, WN, MODE, GLU, WALK>;
     const hipError_t err = ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds);
     if (err != hipSuccess) return err;
     p.NT = (p.N + out_n - 1) / out_n;
@@ -713,15 +808,15 @@ hipError_t launch_forward(const PackedParams& p, hipStream_t st) {
     const double rows_each = static_cast<double>(p.rows) / p.E;
     if (rows_each <= 32) return launch_rows<WIDE, GLU>(p, st);
     if (rows_each < 512) {
-        if constexpr (GLU) return launch_tiles<WIDE, 64, 256, 1, 4, 2, FORWARD, true, false>(p, st);
-        else return launch_tiles<WIDE, 128, 128, 2, 2, 2, FORWARD, false, false>(p, st);
+        if constexpr (GLU) return launch_tiles<WIDE, 64, 256, 1, 4, FORWARD, true, false>(p, st);
+        else return launch_tiles<WIDE, 128, 128, 2, 2, FORWARD, false, false>(p, st);
     }
-    return launch_tiles<WIDE, 256, 256, 2, 4, 2, FORWARD, GLU, true>(p, st);
+    return launch_tiles<WIDE, 256, 256, 2, 4, FORWARD, GLU, true>(p, st);
 }
 template <bool WIDE>
 hipError_t launch_weight(const PackedParams& p, hipStream_t st) {
-    if (static_cast<long long>(p.M) * p.N * p.E * (p.glu ? 2 : 1) < 512ll * 256 * 256) return launch_tiles<WIDE, 128, 128, 2, 2, 2, WEIGHT, false, false>(p, st);
-    return launch_tiles<WIDE, 256, 256, 2, 4, 2, WEIGHT, false, true>(p, st);
+    if (static_cast<long long>(p.M) * p.N * p.E * (p.glu ? 2 : 1) < 512ll * 256 * 256) return launch_tiles<WIDE, 128, 128, 2, 2, WEIGHT, false, false>(p, st);
+    return launch_tiles<WIDE, 256, 256, 2, 4, WEIGHT, false, true>(p, st);
 }
 
 }  // namespace
