@@ -318,58 +318,53 @@ __global__ __launch_bounds__(kThreads, 2) void pack_tiles_kernel(TileParams p) {
             if constexpr (GLU) up[i].load(p.q[1], p.s[1], pitch, row, cc, 0, row, p.rows);
         }
     }
-    float v[8][8];
+    float v[n_halves][8][8];
 #pragma unroll
-    for (int h = 0; h < n_halves; ++h) {
+    for (int i = 0; i < 8; ++i) {
+        float (&d)[8] = v[0][i];
+        if constexpr (SOURCE == FROM_PACKED) from[i].unpack(cc, d);
+        else from[i].unpack(d);
+        if constexpr (ACT != ETR_ACT_NONE) {
+            float a[8], b[8];
+            pre[i].unpack(cc, a);
+            if constexpr (GLU) up[i].unpack(cc, b);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            // (both halves begin with what was loaded: nothing worked out for the first is kept for the second, 64 registers a value)
-            if constexpr (GLU) {
-                asm volatile("" : "+v"(from[i].v[0]), "+v"(pre[i].q.x), "+v"(pre[i].q.y), "+v"(pre[i].s));
-                if constexpr (SOURCE == FROM_F32) asm volatile("" : "+v"(from[i].v[1]));
-            }
-            if constexpr (SOURCE == FROM_PACKED) from[i].unpack(cc, v[i]);
-            else from[i].unpack(v[i]);
-            if constexpr (ACT != ETR_ACT_NONE) {
-                float a[8], b[8];
-                pre[i].unpack(cc, a);
+            for (int j = 0; j < 8; ++j) {
                 if constexpr (ACT == ETR_ACT_GELU) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        v[i][j] *= normal_cdf<FAST>(a[j]) + a[j] * 0.39894228040143268f * (FAST ? __expf(-0.5f * a[j] * a[j]) : gaussian_f32(a[j]));
+                    d[j] *= normal_cdf<FAST>(a[j]) + a[j] * 0.39894228040143268f * (FAST ? __expf(-0.5f * a[j] * a[j]) : gaussian_f32(a[j]));
                 } else {
-                    if (GLU && h == 0) {
-                        up[i].unpack(cc, b);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) v[i][j] *= b[j];
-                    }
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float sg = sigmoid<FAST>(a[j]);
-                        v[i][j] *= h ? a[j] * sg : sg * (1.0f + a[j] * (1.0f - sg));
+                    const float sg = sigmoid<FAST>(a[j]), slope = sg * (1.0f + a[j] * (1.0f - sg));
+                    if constexpr (GLU) {
+                        v[n_halves - 1][i][j] = d[j] * (a[j] * sg);
+                        d[j] *= b[j] * slope;
+                    } else {
+                        d[j] *= slope;
                     }
                 }
             }
-            if (rg * 8 + i >= n_rows || c >= p.K) {
+        }
+        if (rg * 8 + i >= n_rows || c >= p.K) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-            }
-            __builtin_amdgcn_sched_barrier(0);           // one row at a time: keeps the live set small
+            for (int h = 0; h < n_halves; ++h)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[h][i][j] = 0.f;
         }
-        if (p.row_q && !nothing) {
-            pack_tile_rows(v, p.row_q, p.row_pitch, p.row_s, h * per_half + nb, h == n_halves - 1 && nb == per_half - 1, first, n_rows, p.rows);
-        }
+        __builtin_amdgcn_sched_barrier(0);               // one row at a time: keeps the live set small
+    }
+#pragma unroll
+    for (int h = 0; h < n_halves; ++h) {
+        if (p.row_q && !nothing) pack_tile_rows(v[h], p.row_q, p.row_pitch, p.row_s, h * per_half + nb, h == n_halves - 1 && nb == per_half - 1, first, n_rows, p.rows);
         if (p.part || direct) {
             float* out = direct ? p.sums[h] + static_cast<size_t>(e) * p.K : p.part + (static_cast<size_t>(h) * p.chunks + chunk) * p.K;
-            tile_sums(v, lds, out, c0, p.K);
+            tile_sums(v[h], lds, out, c0, p.K);
         }
         if (p.column_q && !nothing) {
             if (p.half_blocks) {                         // a pair of stacks: the matrix has 2 half_blocks blocks
                 const int all = 2 * p.half_blocks, at = p.half * p.half_blocks + block;
-                pack_tile_columns(v, lds, p.column_q + static_cast<size_t>(e) * p.K * all * kBlock, static_cast<size_t>(all) * kBlock,
+                pack_tile_columns(v[h], lds, p.column_q + static_cast<size_t>(e) * p.K * all * kBlock, static_cast<size_t>(all) * kBlock,
                                   p.column_s + static_cast<size_t>(e) * ((all + 3) / 4) * p.K * 4, at, at == all - 1, c0, p.K, p.K, 0);
             } else {
-                pack_tile_columns(v, lds, p.column_q + static_cast<size_t>(blocks_before) * kBlock * p.column_rows, static_cast<size_t>(blocks) * kBlock,
+                pack_tile_columns(v[h], lds, p.column_q + static_cast<size_t>(blocks_before) * kBlock * p.column_rows, static_cast<size_t>(blocks) * kBlock,
                                   p.column_s + static_cast<size_t>(groups_before) * 4 * p.column_rows, block, block == blocks - 1, c0, p.K, p.column_rows,
                                   h * p.K);
             }

@@ -17,12 +17,10 @@ inline size_t scale_bytes(size_t count, int K) { return count * 4 * static_cast<
 namespace {
 
 // The byte of the smallest power of two, 2^-127 at least, by which a magnitude comes to 448 = 1.75 x 2^8 or less.
-__device__ __forceinline__ uint32_t scale_byte(float top) {
-    const uint32_t bits = __float_as_uint(top);
-    return static_cast<uint32_t>(max(static_cast<int>(bits >> 23) - 8 + ((bits & 0x7FFFFFu) > 0x600000u ? 1 : 0), 0));
-}
+// (448 has the mantissa 0x600000: what is added carries into the exponent exactly where the mantissa is larger.)
+__device__ __forceinline__ uint32_t scale_byte(float top) { return max((__float_as_uint(top) + 0x1FFFFFu) >> 23, 8u) - 8u; }
 // 2^(byte - 127); byte 0 is below the normal numbers
-__device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(byte ? byte << 23 : 0x400000u); }
+__device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(max(byte << 23, 0x400000u)); }
 // magnitude that takes part in a block's largest: NaN and infinities have none
 __device__ __forceinline__ float finite_abs(float v) { return fabsf(v) < __builtin_inff() ? fabsf(v) : 0.f; }
 // Largest magnitude of what is finite among n values: NaN is no operand to a maximum, and infinities are looked at only where there are any.
