@@ -203,6 +203,10 @@ extern "C" int etr_ffn_plan(const etr_config* c, int product, int gathered, long
 // in one launch of 64-row tiles: 0 no, 1 yes, 2 with shared contractions.
 extern "C" int etr_linear_plan(const etr_linear_config* c, int product);
 
+// Likewise the form of a product of packed operands (0 forward, 1 forward with packed results, 2 the weights' gradient): 0 / 1 / 2 of 16 rows and 16 / 32 /
+// 128 columns, 3 / 4 / 5 / 6 tiles of 32 / 64 / 128 / 256 rows.
+extern "C" int etr_packed_plan(const etr_linear_config* c, int product);
+
 // ---- device helpers -----------------------------------------------------------
 // Inclusive prefix sum over the 64 lanes of a wave, lane 0 first, by data-parallel-primitive moves: shifts by
 // 1, 2, 4, 8 inside each row of 16 lanes (a lane whose source lies outside its row adds nothing), then lane 15 of

@@ -8,6 +8,7 @@
 // largest of some 16 neighbours (measured: 1.5e-5 of a result's size on normal data).  Results in fp32 go without it: the values are
 // converted to bf16, which holds them and their scale exactly, and multiplied there, with sums in fp32 (6e-8).
 #include <algorithm>
+#include <cmath>
 
 #include "activation.h"
 #include "packed.h"
@@ -162,7 +163,8 @@ __device__ __forceinline__ void barrier() {
     asm volatile("" ::: "memory");
 }
 
-constexpr int kPatch = 2048;                             // LDS of a wave's own, through which its results leave
+// LDS of a wave's own, through which its results leave.  (Four waves of a SwiGLU have half as much, so that two workgroups of them fit a CU.)
+constexpr int patch_bytes(bool glu, int waves) { return glu && waves == 4 ? 1024 : 2048; }
 
 // eight values of a block as bf16, exactly
 __device__ __forceinline__ bf16x8 widen(int lo, int hi, float scale) {
@@ -226,7 +228,8 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void packed_tiles_kernel(PackedPara
     constexpr bool PATCH = !WIDE;
     constexpr int ES = WIDE ? 4 : 2, JC = PATCH || NW * 32 * NO * 32 * ES > TILE_BYTES ? 1 : NO, RB = JC * 32 * ES, PR = RB / 16, RP = 64 / PR;
     constexpr int STORES = MB * NO / JC * (32 / RP);
-    static_assert(NO % JC == 0 && NW * 32 * RB <= TILE_BYTES && (!PATCH || 32 * RB <= kPatch), "");
+    constexpr int kPatch = patch_bytes(GLU, NW), PROWS = PATCH ? std::min(32, kPatch / RB) : 32;         // rows of a patch
+    static_assert(NO % JC == 0 && NW * 32 * RB <= TILE_BYTES && PROWS % RP == 0, "");
     auto spread = [](int row) { return PR == 4 ? (row >> 2) & 3 : row & (PR - 1); };         // rows of a patch over the banks
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     float (*tops)[BM] = reinterpret_cast<float (*)[BM]>(lds + 2 * STAGE);                 // [WN][BM]
@@ -593,30 +596,37 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void packed_tiles_kernel(PackedPara
                     for (int j0 = 0; j0 < NO; j0 += JC) {
                         const int n = n_wave + j0 * 32 + piece * (16 / ES);
 #pragma unroll
-                        for (int jb = 0; jb < JC; ++jb)
+                        for (int r0 = 0; r0 < 32; r0 += PROWS) {
+                            const int row = (l & 31) - r0;
+                            if (PROWS == 32 || (row >= 0 && row < PROWS)) {
 #pragma unroll
-                            for (int q = 0; q < 4; ++q) {
-                                const int at = (jb * 32 + 8 * q + 4 * h) * ES;
-                                const f32x16& a = acc[i][j0 + jb];
-                                const float f[4] = {a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
-                                store4<WIDE>(patch + (l & 31) * RB + ((at >> 4) ^ spread(l & 31)) * 16 + (at & 15), 0, f);
+                                for (int jb = 0; jb < JC; ++jb)
+#pragma unroll
+                                    for (int q = 0; q < 4; ++q) {
+                                        const int at = (jb * 32 + 8 * q + 4 * h) * ES;
+                                        const f32x16& a = acc[i][j0 + jb];
+                                        const float f[4] = {a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
+                                        store4<WIDE>(patch + row * RB + ((at >> 4) ^ spread(row)) * 16 + (at & 15), 0, f);
+                                    }
                             }
-                        wave_sync();
-                        piece_t out[32 / RP];
+                            wave_sync();
+                            piece_t out[PROWS / RP];
 #pragma unroll
-                        for (int u = 0; u < 32 / RP; ++u) {
-                            const int row = u * RP + row_in;
-                            out[u] = *reinterpret_cast<const piece_t*>(patch + row * RB + (piece ^ spread(row)) * 16);
-                        }
-                        wave_sync();
-                        char* at = base + (static_cast<size_t>((wm * MB + i) * 32 + row_in) * p.N + n) * ES;
-                        if (full) {
+                            for (int u = 0; u < PROWS / RP; ++u) {
+                                const int from = u * RP + row_in;
+                                out[u] = *reinterpret_cast<const piece_t*>(patch + from * RB + (piece ^ spread(from)) * 16);
+                            }
+                            wave_sync();
+                            const int m = (wm * MB + i) * 32 + r0 + row_in;
+                            char* at = base + (static_cast<size_t>(m) * p.N + n) * ES;
+                            if (full) {
 #pragma unroll
-                            for (int u = 0; u < 32 / RP; ++u) *reinterpret_cast<piece_t*>(at + static_cast<size_t>(u * RP) * p.N * ES) = out[u];
-                        } else {
+                                for (int u = 0; u < PROWS / RP; ++u) *reinterpret_cast<piece_t*>(at + static_cast<size_t>(u * RP) * p.N * ES) = out[u];
+                            } else {
 #pragma unroll
-                            for (int u = 0; u < 32 / RP; ++u)
-                                if ((wm * MB + i) * 32 + u * RP + row_in < limit && n < p.N) *reinterpret_cast<piece_t*>(at + static_cast<size_t>(u * RP) * p.N * ES) = out[u];
+                                for (int u = 0; u < PROWS / RP; ++u)
+                                    if (m + u * RP < limit && n < p.N) *reinterpret_cast<piece_t*>(at + static_cast<size_t>(u * RP) * p.N * ES) = out[u];
+                            }
                         }
                     }
                 }
@@ -634,12 +644,14 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void packed_tiles_kernel(PackedPara
 
 // ---- few rows ----------------------------------------------------------------------------------------------------------
 //
-// 16 rows x 128 output columns to a workgroup: eight waves, or twice eight that share the contraction, with 16 columns each (SwiGLU: 16 gate
-// and 16 up), stream their weight rows straight into registers, a 16 x 16 x 128 MFMA to a k-tile.  Bound by the weights' bytes.  A lane has row
+// 16 rows x 16 NW output columns to a workgroup: waves with 16 columns each (SwiGLU: 16 gate and 16 up), KS of them to share a
+// contraction, stream their weight rows straight into registers, a 16 x 16 x 128 MFMA to a k-tile.  Bound by the weights' bytes.  A lane has row
 // lane % 16 of a block and 16 bytes out of each half of the k-tile, so that a load takes 64 bytes of a row.
-template <bool WIDE, int KS, bool GLU>
-__global__ __launch_bounds__(512 * KS, 2) void packed_rows_kernel(PackedParams p) {
-    constexpr int BM = 16, NW = 8, NG = GLU ? 2 : 1;
+// PACK: results are packed too, which takes a workgroup with all 128 columns of a block.
+template <bool WIDE, int NW, int KS, bool GLU, bool PACK>
+__global__ __launch_bounds__(64 * NW * KS, NW * KS > 8 ? 4 : 2) void packed_rows_kernel(PackedParams p) {
+    constexpr int BM = 16, NG = GLU ? 2 : 1;
+    static_assert(!PACK || NW == 8, "");
     __shared__ float tops[NW][BM];
     __shared__ f32x4 sums[KS > 1 ? KS - 1 : 1][NG][KS > 1 ? NW * 64 : 1];
     const int lane = threadIdx.x & 63, l16 = lane & 15, kq = lane >> 4;
@@ -649,7 +661,7 @@ __global__ __launch_bounds__(512 * KS, 2) void packed_rows_kernel(PackedParams p
     TileList<FORWARD, false> list;
     list.load(p, seg, BM, blockIdx.x, gridDim.x);
     Tile t;
-    for (int j = blockIdx.x >> 3; list.find(p, seg, BM, kBlock, j, t); j += gridDim.x >> 3) {
+    for (int j = blockIdx.x >> 3; list.find(p, seg, BM, 16 * NW, j, t); j += gridDim.x >> 3) {
         const size_t pitch = static_cast<size_t>(p.blocks) * kBlock, first = static_cast<size_t>(t.first) + t.m0;
         const int rows_left = t.count - t.m0, n0 = t.n0 + wave * 16, G = (p.blocks + 3) / 4;
         const size_t row_a = first + min(l16, rows_left - 1), row_b = min(n0 + l16, p.N - 1);
@@ -679,7 +691,7 @@ __global__ __launch_bounds__(512 * KS, 2) void packed_rows_kernel(PackedParams p
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
 #pragma unroll
-                    for (int h = 0; h < NG; ++h) fb[h][u][s] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(b[h] + at + s * 64));
+                    for (int h = 0; h < NG; ++h) fb[h][u][s] = *reinterpret_cast<const v4i*>(b[h] + at + s * 64);
                     fa[u][s] = *reinterpret_cast<const v4i*>(a + at + s * 64);
                 }
             }
@@ -757,13 +769,13 @@ __global__ __launch_bounds__(512 * KS, 2) void packed_rows_kernel(PackedParams p
 #pragma unroll
                 for (int v = 0; v < 4; ++v) acc[h][v] += f[v];
             }
-            if (p.P[1 + h]) pack(p.P[1 + h], p.Ps[1 + h], acc[h]);
+            if (PACK && p.P[1 + h]) pack(p.P[1 + h], p.Ps[1 + h], acc[h]);
         }
         float r[4] = {0.f, 0.f, 0.f, 0.f};
         if (p.residual && row_in && n < p.N) load4<WIDE>(p.residual, (first + l16) * p.N + n, r);
 #pragma unroll
         for (int v = 0; v < 4; ++v) acc[0][v] = activate<WIDE>(p.act, acc[0][v], acc[NG - 1][v], GLU) + r[v];
-        if (p.P[0]) pack(p.P[0], p.Ps[0], acc[0]);
+        if (PACK && p.P[0]) pack(p.P[0], p.Ps[0], acc[0]);
         if (p.C[0] && row_in && n < p.N) {
             const float f[4] = {acc[0][0], acc[0][1], acc[0][2], acc[0][3]};
             store4<WIDE>(p.C[0], (first + l16) * p.N + n, f);
@@ -783,7 +795,7 @@ long long tiles_at_most(const PackedParams& p, int mode, int BM, int out_n) {
 template <bool WIDE, int BM, int BN, int WM, int WN, int MODE, bool GLU, bool WALK>
 hipError_t launch_tiles(PackedParams p, hipStream_t st) {
     constexpr int out_n = GLU ? BN / 2 : BN;
-    constexpr size_t lds = 2 * static_cast<size_t>((BM + BN) * kBlock + ((BM + 63) / 64 + BN / 64) * 256) + WN * BM * 4 + (WIDE ? 0 : WM * WN * kPatch);
+    constexpr size_t lds = 2 * static_cast<size_t>((BM + BN) * kBlock + ((BM + 63) / 64 + BN / 64) * 256) + WN * BM * 4 + (WIDE ? 0 : WM * WN * patch_bytes(GLU, WM * WN));
     auto kern = packed_tiles_kernel<WIDE, BM, BN, WM, WN, MODE, GLU, WALK>;
     const hipError_t err = ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds);
     if (err != hipSuccess) return err;
@@ -794,37 +806,119 @@ hipError_t launch_tiles(PackedParams p, hipStream_t st) {
     hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(blocks)), dim3(WM * WN * 64), lds, st, p);
     return hipGetLastError();
 }
-template <bool WIDE, bool GLU>
+template <bool WIDE, int NW, int KS, bool GLU, bool PACK>
 hipError_t launch_rows(PackedParams p, hipStream_t st) {
-    p.NT = blocks_of(p.N);
-    const long long tiles = tiles_at_most(p, FORWARD, 16, kBlock);
+    p.NT = (p.N + 16 * NW - 1) / (16 * NW);
+    const long long tiles = tiles_at_most(p, FORWARD, 16, 16 * NW);
     const long long blocks = std::min<long long>((tiles + 7) / 8, 1 << 17) * 8;
-    hipLaunchKernelGGL((packed_rows_kernel<WIDE, 1, GLU>), dim3(static_cast<unsigned>(blocks)), dim3(512), 0, st, p);
+    hipLaunchKernelGGL((packed_rows_kernel<WIDE, NW, KS, GLU, PACK>), dim3(static_cast<unsigned>(blocks)), dim3(64 * NW * KS), 0, st, p);
     return hipGetLastError();
+}
+
+// The form of a product, by estimate.  ROWS16: 16 rows x 16 columns, eight waves to share the contraction; ROWS32: x 32, four of them; ROWS128: x 128,
+// a wave for 16 columns each, where results are packed; T32 ... T256: tiles of that many rows, x 128 columns, T256 x 256 (weight rows of a SwiGLU: twice
+// as many for T32 and T64, and no T128).
+enum class Form { ROWS16, ROWS32, ROWS128, T32, T64, T128, T256 };
+struct Choice { Form form; double us; };
+// Microseconds: rounds of tiles over the places that they have on the chip, each a time per k-tile (alone ... chip full) and a time besides; and the
+// weights' bytes at 5 TB/s at least.  ROWS: the weights' bytes for every 16 rows, at 5.5 TB/s.  (bf16; fp32 takes longer with all of them.)  Measured, us, in this order:
+// ROWS16 / 32, T32, T64, T128, T256 (SwiGLU without T128):
+//   18 rows dense, 3840 x 1472          6.3  9.5                       2048 in 16 groups, 5632 x 2048         59   57   42   48
+//   96 in 4, 2816 x 1024               10.3 12.6  12.0 14.6 18.2 24.8  4096 in 16, 2048 x 2048                44   37   34   30
+//   64 in 16, 5632 x 2048              32.5 32.3  29.0 29.6 32.6 44.7  300 dense, 4096 x 4096                 20.1 19.7 25.1 33.9
+//   64 in 16, 2048 x 5632 SwiGLU       92   65    74   77        82    1024 dense, 4096 x 4096                42   25   27   35
+//   32 in 8, 4096 x 1408 SwiGLU        18.5 21                         512 in 8, 2048 x 1408 SwiGLU           16.8 18.1      21.2
+//   1 in 64, 2048 x 1408 SwiGLU         5.9  7.3  14.5 17.3      20.9  32768 in 8, 2816 x 4096                775  574  428  369
+double estimate_us(Form f, double tiles, double k_tiles, bool glu) {
+    double places = 1, alone = 0, full = 0, besides = 0;
+    switch (f) {
+        case Form::T256: alone = 0.87; full = 1.75; besides = 6.0; break;
+        case Form::T128: places = 2; alone = 0.6; full = 1.1; besides = 4.5; break;
+        case Form::T64: places = glu ? 1 : 3; alone = glu ? 0.85 : 0.45; full = glu ? 1.2 : 1.15; besides = glu ? 4.0 : 3.5; break;
+        case Form::T32: places = glu ? 2 : 3; alone = glu ? 0.7 : 0.33; full = glu ? 1.2 : 0.78; besides = glu ? 4.0 : 3.0; break;
+        default: break;
+    }
+    const double r = tiles / (places * cu_count()), rest = r - std::floor(r);
+    double rounds = r <= 1 ? 1.0 : f == Form::T256 ? std::ceil(r) : r < 4 ? std::ceil(2 * r) / 2 : r + 0.25;
+    if (f == Form::T256 && r > 1 && rest > 0) rounds = std::floor(r) + (rest <= 0.25 ? 0.55 : rest <= 0.5 ? 0.7 : 1.0);
+    double crowd = std::min(1.0, r);                     // half of it the chip's, half from where tiles share a CU
+    if (places > 1) crowd = 0.5 * crowd + 0.5 * std::max(0.0, std::min(1.0, (r * places - 1) / (places - 1)));
+    return rounds * (k_tiles * (alone + (full - alone) * crowd) + besides);
+}
+template <int MODE, bool GLU>
+Choice choose_form(const PackedParams& p, bool packs) {
+    const double rows_each = MODE == WEIGHT ? p.M : static_cast<double>(p.rows) / p.E;               // rows of a group, on average
+    const double groups = MODE == WEIGHT ? p.E * (p.glu ? 2 : 1) : std::min(p.E, p.rows);
+    const double k_tiles = MODE == WEIGHT ? std::ceil(static_cast<double>(p.rows) / p.E / kBlock) : p.blocks;
+    const double weights = MODE == WEIGHT ? 0 : groups * p.N * p.blocks * kBlock * (GLU ? 2 : 1);    // bytes
+    // row tiles of a group: half a tile more than its rows fill, on average, where they are the batch's
+    auto row_tiles = [&](int BM) {
+        const double whole = std::ceil(rows_each / BM);
+        return MODE == WEIGHT || rows_each < 1 ? whole : std::max(whole, rows_each / BM + (p.E > 1 ? 0.5 : 0.0));
+    };
+    Choice best{Form::T256, 1e30};
+    auto offer = [&](Form f, double us) { if (us < best.us) best = {f, us}; };
+    auto offer_tiles = [&](Form f, int BM, int out_n) {
+        const double us = estimate_us(f, groups * row_tiles(BM) * ((p.N + out_n - 1) / out_n), k_tiles, GLU);
+        offer(f, std::max(us, 3.0 + weights / 5.0e6));
+    };
+    offer_tiles(Form::T256, 256, GLU ? 128 : 256);
+    if (!GLU) offer_tiles(Form::T128, 128, 128);
+    offer_tiles(Form::T64, 64, 128);
+    offer_tiles(Form::T32, 32, 128);
+    if (MODE != WEIGHT) {
+        const double bytes = weights * row_tiles(16), us = 3.5 + bytes / 5.5e6;
+        // (a CU alone takes in 27 KB a microsecond)
+        if (packs) offer(Form::ROWS128, std::max(us, 3.5 + std::ceil(groups * row_tiles(16) * blocks_of(p.N) / cu_count()) * kBlock * p.blocks * kBlock * (GLU ? 2 : 1) / 27e3));
+        else offer(groups * row_tiles(16) * p.N / 16 < 2048 ? Form::ROWS16 : Form::ROWS32, us);
+    }
+    return best;
 }
 
 template <bool WIDE, bool GLU>
 hipError_t launch_forward(const PackedParams& p, hipStream_t st) {
-    const double rows_each = static_cast<double>(p.rows) / p.E;
-    if (rows_each <= 32) return launch_rows<WIDE, GLU>(p, st);
-    if (rows_each < 512) {
-        if constexpr (GLU) return launch_tiles<WIDE, 64, 256, 1, 4, FORWARD, true, false>(p, st);
-        else return launch_tiles<WIDE, 128, 128, 2, 2, FORWARD, false, false>(p, st);
+    const bool packs = p.P[0] || p.P[1] || p.P[2];
+    switch (choose_form<FORWARD, GLU>(p, packs).form) {
+        case Form::ROWS16: return launch_rows<WIDE, 1, 8, GLU, false>(p, st);
+        case Form::ROWS32: return launch_rows<WIDE, 2, 4, GLU, false>(p, st);
+        case Form::ROWS128: return launch_rows<WIDE, 8, 1, GLU, true>(p, st);
+        case Form::T32: return launch_tiles<WIDE, 32, GLU ? 256 : 128, 1, 4, FORWARD, GLU, false>(p, st);
+        case Form::T64: return launch_tiles<WIDE, 64, GLU ? 256 : 128, 1, 4, FORWARD, GLU, false>(p, st);
+        case Form::T128:
+            if constexpr (!GLU) return launch_tiles<WIDE, 128, 128, 2, 2, FORWARD, false, false>(p, st);
+            break;
+        case Form::T256: return launch_tiles<WIDE, 256, 256, 2, 4, FORWARD, GLU, true>(p, st);
     }
-    return launch_tiles<WIDE, 256, 256, 2, 4, FORWARD, GLU, true>(p, st);
+    return hipErrorInvalidValue;
 }
 template <bool WIDE>
 hipError_t launch_weight(const PackedParams& p, hipStream_t st) {
-    if (static_cast<long long>(p.M) * p.N * p.E * (p.glu ? 2 : 1) < 512ll * 256 * 256) return launch_tiles<WIDE, 128, 128, 2, 2, WEIGHT, false, false>(p, st);
-    return launch_tiles<WIDE, 256, 256, 2, 4, WEIGHT, false, true>(p, st);
+    switch (choose_form<WEIGHT, false>(p, false).form) {
+        case Form::T32: return launch_tiles<WIDE, 32, 128, 1, 4, WEIGHT, false, false>(p, st);
+        case Form::T64: return launch_tiles<WIDE, 64, 128, 1, 4, WEIGHT, false, false>(p, st);
+        case Form::T128: return launch_tiles<WIDE, 128, 128, 2, 2, WEIGHT, false, false>(p, st);
+        case Form::T256: return launch_tiles<WIDE, 256, 256, 2, 4, WEIGHT, false, true>(p, st);
+        default: return hipErrorInvalidValue;
+    }
+}
+
+// sizes of the products
+PackedParams forward_sizes(const etr_linear_config& c) {
+    PackedParams p{};
+    p.rows = c.rows; p.E = c.E; p.N = c.N; p.blocks = blocks_of(c.K); p.act = c.act; p.glu = c.act == ETR_ACT_SWIGLU;
+    return p;
+}
+PackedParams weight_sizes(const etr_linear_config& c) {
+    PackedParams p{};
+    p.rows = c.rows; p.E = c.E; p.M = c.N; p.N = c.K; p.glu = c.act == ETR_ACT_SWIGLU;
+    return p;
 }
 
 }  // namespace
 
 hipError_t launch_packed_linear(const etr_linear_config& c, const etr_packed& x, const int32_t* offsets, const etr_packed* const w[2], const float* bias,
                                  const float* bias_up, const void* residual, void* y, const etr_packed* const kept[3], hipStream_t st) {
-    PackedParams p{};
-    p.rows = c.rows; p.E = c.E; p.N = c.N; p.blocks = blocks_of(c.K); p.act = c.act; p.glu = c.act == ETR_ACT_SWIGLU;
+    PackedParams p = forward_sizes(c);
     p.A = static_cast<const uint8_t*>(x.values); p.As = static_cast<const uint8_t*>(x.scales);
     for (int i = 0; i < 2; ++i)
         if (w[i]) { p.B[i] = static_cast<const uint8_t*>(w[i]->values); p.Bs[i] = static_cast<const uint8_t*>(w[i]->scales); }
@@ -837,8 +931,7 @@ hipError_t launch_packed_linear(const etr_linear_config& c, const etr_packed& x,
 
 hipError_t launch_packed_weight_gradient(const etr_linear_config& c, const etr_packed& dt, const etr_packed& xt, const int32_t* offsets, void* dw, void* dw_up,
                                    hipStream_t st) {
-    PackedParams p{};
-    p.rows = c.rows; p.E = c.E; p.M = c.N; p.N = c.K; p.glu = c.act == ETR_ACT_SWIGLU;
+    PackedParams p = weight_sizes(c);
     p.A = static_cast<const uint8_t*>(dt.values); p.As = static_cast<const uint8_t*>(dt.scales);
     p.B[0] = static_cast<const uint8_t*>(xt.values); p.Bs[0] = static_cast<const uint8_t*>(xt.scales);
     p.C[0] = dw; p.C[1] = dw_up; p.offsets = offsets;
@@ -846,3 +939,10 @@ hipError_t launch_packed_weight_gradient(const etr_linear_config& c, const etr_p
 }
 
 }  // namespace etr
+
+extern "C" int etr_packed_plan(const etr_linear_config* c, int product) {
+    using namespace etr;
+    if (product == 2) return static_cast<int>(choose_form<WEIGHT, false>(weight_sizes(*c), false).form);
+    const PackedParams p = forward_sizes(*c);
+    return static_cast<int>(p.glu ? choose_form<FORWARD, true>(p, product == 1).form : choose_form<FORWARD, false>(p, product == 1).form);
+}
