@@ -60,6 +60,16 @@ __device__ __forceinline__ float row16_max(float v) {
     return fmaxf(v, dpp(v, std::integral_constant<int, 0x140>{}));   // row mirror
 }
 
+// Inclusive running maximum over the 64 lanes of numbers from 0 up, by the moves of wave_scan_incl.  All lanes active.
+__device__ __forceinline__ int wave_max_incl(int v) {
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false));   // row_shr:1
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false));   // row_shr:2
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false));   // row_shr:4
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false));   // row_shr:8
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false));   // row_bcast:15 -> rows 1, 3
+    return max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false));   // row_bcast:31 -> rows 2, 3
+}
+
 // Rows of the groups, one group per lane, for operands whose groups lie one behind the other: the offsets' running maximum, so that
 // the groups' rows are `rows` in all whatever the offsets say.  blocks: of 128 rows, a last one in part; groups: of four blocks, whose scales
 // are a dword; _incl: those of the groups before and of this one.
@@ -74,12 +84,8 @@ struct Segments {
         } else {
             int begin = lane < E && offsets ? min(max(offsets[lane], 0), rows) : 0;
             end = lane < E ? (offsets ? min(max(offsets[lane + 1], 0), rows) : rows) : 0;
-#pragma unroll
-            for (int s = 1; s < 64; s <<= 1) {
-                const int a = __shfl_up(begin, s), b = __shfl_up(end, s);
-                if (lane >= s) { begin = max(begin, a); end = max(end, b); }
-            }
-            end = max(begin, end);
+            begin = wave_max_incl(begin);
+            end = max(begin, wave_max_incl(end));
             first = begin;
             count = lane < E ? end - begin : 0;
         }
