@@ -102,9 +102,9 @@ def test_weights_of_large_matrices(dtype):
     weights_case([257, 100], 4104, 4360, True, dtype)
 
 
-def weights_case(counts, K, N, glu, dtype):
+def weights_case(counts, K, N, glu, dtype, extra=3):
     E, used = len(counts), sum(counts)
-    rows, n = used + 3, 2 if glu else 1
+    rows, n = used + extra, 2 if glu else 1
     offsets = [sum(counts[:e]) for e in range(E + 1)]
     dev = torch.tensor(offsets, dtype=torch.int32, device="cuda")
     x, d = O.randn(1, rows, K), O.randn(2, rows, n * N, std=0.02)
