@@ -46,9 +46,9 @@ struct Tile { int e, first, m0, n0, count, limit, half; };
 
 // The tile list: experts one after the other; inside one bands of 8 row tiles, in a band the row tiles of a column tile next to
 // each other.  Each XCD (workgroups go round them) has a contiguous part of the list, so its 32 CUs work on some 8 x 4 tiles at once and share
-// 8 + 4 operand slabs in its L2.  The parts are equal in work: a tile of WEIGHT takes as long as its expert has rows (16 experts of 600 to 1700 rows,
-// 2048 x 11264: equal numbers of tiles 547 us, equal work see below).
-// SPLIT (one workgroup to a CU): where the last round over an XCD's CUs would keep half of them or fewer busy, its tiles go in halves or quarters
+// 8 + 4 operand slabs in its L2.
+// SPLIT (one workgroup to a CU): the parts are equal in work, where a tile of WEIGHT takes as long as its expert has rows (16 experts of 600 to 1700
+// rows, 2048 x 11264: 547 us with equal numbers of tiles, 498 so); and where the last round over an XCD's CUs would keep half of them or fewer busy, its tiles go in halves or quarters
 // of their rows to as many workgroups.
 template <int MODE, bool SPLIT>
 struct TileList {
@@ -58,7 +58,7 @@ struct TileList {
         const int xcd = bid & 7;
         per_xcd = grid >> 3;
         tiles = tiles_incl = 0;
-        if (MODE == WEIGHT) {
+        if (MODE == WEIGHT && SPLIT) {
             const int each = (p.M + BM - 1) / BM * (p.glu ? 2 : 1) * p.NT, lane = threadIdx.x & 63;
             const long long weight = lane < p.E ? seg.blocks + 4 : 0, incl = wave_scan_incl(weight * each);
             auto at = [](long long v, int e) {
@@ -71,14 +71,18 @@ struct TileList {
                 const long long target = all / 8 * x;
                 const int e = __builtin_ctzll(__ballot(incl > target));
                 const long long w = at(weight, e), in = target - (at(incl, e) - w * each);
-                return e * each + static_cast<int>((in + w - 1) / w);
+                return e * each + min(static_cast<int>(static_cast<double>(in + w - 1) / static_cast<double>(w)), each);
             };
             start = border(xcd);
             end = border(xcd + 1);
         } else {
-            tiles = (seg.count + BM - 1) / BM;
-            tiles_incl = wave_scan_incl(tiles);
-            const int all = __builtin_amdgcn_readlane(tiles_incl, 63) * p.NT, share = (all + 7) >> 3;
+            int all = p.E * ((p.M + BM - 1) / BM) * (p.glu ? 2 : 1) * p.NT;
+            if (MODE != WEIGHT) {
+                tiles = (seg.count + BM - 1) / BM;
+                tiles_incl = wave_scan_incl(tiles);
+                all = __builtin_amdgcn_readlane(tiles_incl, 63) * p.NT;
+            }
+            const int share = (all + 7) >> 3;
             start = xcd * share;
             end = min(start + share, all);
         }
@@ -132,13 +136,25 @@ __device__ __forceinline__ v4i descriptor(uint64_t base) {
     const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(base >> 32));
     return v4i{static_cast<int>(lo), static_cast<int>(hi & 0xFFFFu), static_cast<int>(kRange), 0x00027000};
 }
-// Copies into LDS, 16 or 4 bytes a lane, lane after lane from `at`.  In assembly, without an output: the compiler would otherwise take every
-// later read of LDS to wait for them; they are waited for by hand.
-__device__ __forceinline__ void copy16(v4i from, uint32_t off, uint32_t at) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(from) : "memory", "m0");
+// Copies into LDS, 16 or 4 bytes a lane, lane after lane from `at`; N of them, 1 KiB apart there.  In assembly, without an output: the compiler would
+// otherwise take every later read of LDS to wait for them; they are waited for by hand.  What the compiler does not see in it either: five wait
+// states between a vector instruction's write of a scalar register (a spilled one comes back that way) and a memory operation that
+// reads it, and one behind M0's.
+template <int N> __device__ __forceinline__ void copy16(v4i from, const uint32_t* off, uint32_t at) {
+    if constexpr (N >= 4) {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %5, 0 offen lds\n\t"
+                     "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %5, 0 offen lds\n\t"
+                     "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %5, 0 offen lds\n\t"
+                     "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %5, 0 offen lds"
+                     ::"s"(at), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(from) : "memory", "m0", "scc");
+        copy16<N - 4>(from, off + 4, at + 4096);
+    } else if constexpr (N > 0) {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(off[0]), "s"(from) : "memory", "m0");
+        copy16<N - 1>(from, off + 1, at + 1024);
+    }
 }
 __device__ __forceinline__ void copy4(v4i from, uint32_t off, uint32_t at) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(from) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(from) : "memory", "m0");
 }
 // at most N of this wave's vector memory operations are outstanding
 template <int N> __device__ __forceinline__ void wait_copies() {
@@ -306,10 +322,8 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void packed_tiles_kernel(PackedPara
     auto issue = [&](int buf) {
         const uint32_t dst = lds0 + buf * STAGE;
         const v4i a = descriptor(s.a), b = descriptor(s.b);
-#pragma unroll
-        for (int i = 0; i < WA; ++i) copy16(a, s.at_a[i], dst + (wave * WA + i) * 1024);
-#pragma unroll
-        for (int i = 0; i < WB; ++i) copy16(b, s.at_b[i], dst + A_BYTES + (wave * WB + i) * 1024);
+        copy16<WA>(a, s.at_a, dst + wave * WA * 1024);
+        copy16<WB>(b, s.at_b, dst + A_BYTES + wave * WB * 1024);
 #pragma unroll
         for (int i = 0; i < SW; ++i) copy4(descriptor(s.scales[i]), s.at_s[i], dst + TILE_BYTES + min(wave + i * NW, SA + SB - 1) * 256);
     };
