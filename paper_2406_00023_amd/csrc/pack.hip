@@ -22,9 +22,10 @@ struct RowsParams {
     int rows, k;            // rows in; pack of tokens: rows of x, and k rows of the result for each
     int out_rows;           // rows of the packed matrix (the stride of its scales)
     int K, blocks, groups;
-    int parts;              // of a row, each a wave's
+    int walkers;            // rows that are under way at once
 };
-constexpr int kSteps = 4;                                // of 512 columns that a wave has on their way at once
+// Steps of 512 columns that a wave has on their way at once: 4, or 1 where that leaves CUs without a wave (32 tokens x 2048, top-2: 4.3 and 3.2 us).
+// A row's parts go to neighbouring waves, which walk the rows together.
 
 template <bool BF16>
 __device__ __forceinline__ void load8(const void* x, size_t at, float (&f)[8]) {
@@ -45,13 +46,11 @@ __device__ __forceinline__ void store8(void* y, size_t at, const float (&f)[8]) 
     }
 }
 
-template <bool BF16, bool TOKENS>
+template <bool BF16, bool TOKENS, int kSteps>
 __global__ __launch_bounds__(kThreads) void pack_rows_kernel(RowsParams p, int matrices) {
-    const int lane = threadIdx.x & 63;
-    const long long units = static_cast<long long>(p.rows) * matrices * p.parts;
-    for (long long unit = static_cast<long long>(blockIdx.x) * kWaves + (threadIdx.x >> 6); unit < units; unit += static_cast<long long>(gridDim.x) * kWaves) {
-        const long long row = unit / p.parts;
-        const int g0 = static_cast<int>(unit - row * p.parts) * kSteps;
+    const int lane = threadIdx.x & 63, wave = blockIdx.x * kWaves + (threadIdx.x >> 6), parts = (p.groups + kSteps - 1) / kSteps, g0 = wave % parts * kSteps;
+    if (wave >= p.walkers * parts) return;
+    for (long long row = wave / parts; row < static_cast<long long>(p.rows) * matrices; row += p.walkers) {
         float f[kSteps][8];
 #pragma unroll
         for (int u = 0; u < kSteps; ++u) {
@@ -62,7 +61,7 @@ __global__ __launch_bounds__(kThreads) void pack_rows_kernel(RowsParams p, int m
         }
         int mine = -1;
         if constexpr (TOKENS) {
-            mine = lane < p.k ? p.row_of[row * p.k + lane] : -1;
+            mine = lane < p.k ? p.row_of[static_cast<size_t>(row) * p.k + lane] : -1;
             if (mine >= p.out_rows) mine = -1;
         }
         uint2 q[kSteps];
@@ -92,19 +91,18 @@ __global__ __launch_bounds__(kThreads) void pack_rows_kernel(RowsParams p, int m
                 if (r >= 0) put(static_cast<size_t>(r) * p.blocks * kBlock, r, p.out_rows);
             }
         } else {
-            const long long matrix = row / p.rows, r = row - matrix * p.rows;
+            const int matrix = matrices > 1 ? static_cast<int>(row) / p.rows : 0, r = static_cast<int>(row) - matrix * p.rows;
             put(static_cast<size_t>(row) * p.blocks * kBlock, static_cast<size_t>(matrix) * p.groups * p.rows + r, p.rows);
         }
     }
 }
 
-template <bool BF16>
+template <bool BF16, int kSteps>
 __global__ __launch_bounds__(kThreads) void unpack_rows_kernel(RowsParams p, int matrices) {
-    const int lane = threadIdx.x & 63;
-    const long long units = static_cast<long long>(p.rows) * matrices * p.parts;
-    for (long long unit = static_cast<long long>(blockIdx.x) * kWaves + (threadIdx.x >> 6); unit < units; unit += static_cast<long long>(gridDim.x) * kWaves) {
-        const long long row = unit / p.parts, matrix = row / p.rows, r = row - matrix * p.rows;
-        const int g0 = static_cast<int>(unit - row * p.parts) * kSteps;
+    const int lane = threadIdx.x & 63, wave = blockIdx.x * kWaves + (threadIdx.x >> 6), parts = (p.groups + kSteps - 1) / kSteps, g0 = wave % parts * kSteps;
+    if (wave >= p.walkers * parts) return;
+    for (long long row = wave / parts; row < static_cast<long long>(p.rows) * matrices; row += p.walkers) {
+        const int matrix = matrices > 1 ? static_cast<int>(row) / p.rows : 0, r = static_cast<int>(row) - matrix * p.rows;
         uint2 q[kSteps];
         uint32_t s[kSteps];
 #pragma unroll
@@ -400,12 +398,26 @@ RowsParams rows_params(int rows, int K) {
     RowsParams p{};
     p.rows = p.out_rows = rows;
     p.K = K; p.blocks = blocks_of(K); p.groups = scale_groups_of(K);
-    p.parts = (p.groups + kSteps - 1) / kSteps;
     return p;
 }
-dim3 rows_grid(const RowsParams& p, int matrices) {
-    const long long units = static_cast<long long>(p.rows) * matrices * p.parts;
-    return dim3(static_cast<unsigned>(std::min<long long>((units + kWaves - 1) / kWaves, 1 << 20)));
+template <class F4, class F1>
+hipError_t launch_rows(F4 four, F1 one, RowsParams p, int matrices, hipStream_t st) {
+    const long long rows = static_cast<long long>(p.rows) * matrices;                        // (2^30 at most)
+    const bool few = rows * p.groups <= 16ll * cu_count();
+    const int parts = few ? p.groups : (p.groups + 3) / 4;
+    p.walkers = static_cast<int>(std::min<long long>(rows, std::max(1, (1 << 22) / parts)));
+    const dim3 grid(static_cast<unsigned>((static_cast<long long>(p.walkers) * parts + kWaves - 1) / kWaves));
+    if (few) hipLaunchKernelGGL(one, grid, dim3(kThreads), 0, st, p, matrices);
+    else hipLaunchKernelGGL(four, grid, dim3(kThreads), 0, st, p, matrices);
+    return hipGetLastError();
+}
+template <bool BF16, bool TOKENS>
+hipError_t launch_pack(const RowsParams& p, int matrices, hipStream_t st) {
+    return launch_rows(pack_rows_kernel<BF16, TOKENS, 4>, pack_rows_kernel<BF16, TOKENS, 1>, p, matrices, st);
+}
+template <bool BF16>
+hipError_t launch_unpack(const RowsParams& p, int matrices, hipStream_t st) {
+    return launch_rows(unpack_rows_kernel<BF16, 4>, unpack_rows_kernel<BF16, 1>, p, matrices, st);
 }
 int chunks_at_most(int rows, int E, bool stacked) { return stacked ? E * blocks_of(rows) : rows / kBlock + std::min(E, rows); }
 
@@ -430,27 +442,21 @@ hipError_t launch_pack_rows(const etr_pack_config& c, const void* x, void* value
     RowsParams p = rows_params(c.rows, c.K);
     const int matrices = c.sorted ? 1 : c.E;
     p.x = x; p.q = static_cast<uint8_t*>(values); p.s = static_cast<uint32_t*>(scales);
-    if (c.dtype == ETR_BF16) hipLaunchKernelGGL((pack_rows_kernel<true, false>), rows_grid(p, matrices), dim3(kThreads), 0, st, p, matrices);
-    else hipLaunchKernelGGL((pack_rows_kernel<false, false>), rows_grid(p, matrices), dim3(kThreads), 0, st, p, matrices);
-    return hipGetLastError();
+    return c.dtype == ETR_BF16 ? launch_pack<true, false>(p, matrices, st) : launch_pack<false, false>(p, matrices, st);
 }
 
 hipError_t launch_pack_sorted_rows(const etr_sort_config& c, const void* x, const int32_t* row_of, void* values, void* scales, hipStream_t st) {
     RowsParams p = rows_params(c.T, c.d);
     p.k = c.k; p.out_rows = c.T * c.k; p.row_of = row_of;
     p.x = x; p.q = static_cast<uint8_t*>(values); p.s = static_cast<uint32_t*>(scales);
-    if (c.dtype == ETR_BF16) hipLaunchKernelGGL((pack_rows_kernel<true, true>), rows_grid(p, 1), dim3(kThreads), 0, st, p, 1);
-    else hipLaunchKernelGGL((pack_rows_kernel<false, true>), rows_grid(p, 1), dim3(kThreads), 0, st, p, 1);
-    return hipGetLastError();
+    return c.dtype == ETR_BF16 ? launch_pack<true, true>(p, 1, st) : launch_pack<false, true>(p, 1, st);
 }
 
 hipError_t launch_unpack_rows(const etr_pack_config& c, const void* values, const void* scales, void* y, hipStream_t st) {
     RowsParams p = rows_params(c.rows, c.K);
     const int matrices = c.sorted ? 1 : c.E;
     p.q = static_cast<uint8_t*>(const_cast<void*>(values)); p.s = static_cast<uint32_t*>(const_cast<void*>(scales)); p.y = y;
-    if (c.dtype == ETR_BF16) hipLaunchKernelGGL(unpack_rows_kernel<true>, rows_grid(p, matrices), dim3(kThreads), 0, st, p, matrices);
-    else hipLaunchKernelGGL(unpack_rows_kernel<false>, rows_grid(p, matrices), dim3(kThreads), 0, st, p, matrices);
-    return hipGetLastError();
+    return c.dtype == ETR_BF16 ? launch_unpack<true>(p, matrices, st) : launch_unpack<false>(p, matrices, st);
 }
 
 hipError_t launch_pack_columns(const etr_pack_config& c, const void* x, const etr_packed* packed, const int32_t* offsets, int half, void* values, void* scales,

@@ -116,6 +116,21 @@ def test_past_4_gib():
     assert torch.equal(xt[0][at: at + tq.numel()].cpu(), tq.reshape(-1)) and torch.equal(xt[1][at_s: at_s + ts.numel()].cpu(), ts.reshape(-1))
 
 
+def test_more_rows_than_waves():
+    """The row kernels walk what is over 2^22 rows."""
+    rows, K = (1 << 22) + 1001, 8
+    x = torch.randn(rows, K, device="cuda")
+    cfg = B.make_pack_config(rows, K, torch.float32)
+    x8 = B.alloc_packed_rows(cfg)
+    B.etr_pack_rows(cfg, x, x8)
+    back = torch.zeros_like(x)
+    B.etr_unpack_rows(cfg, x8, back)
+    for part in (slice(0, 500), slice((1 << 22) - 250, (1 << 22) + 250), slice(rows - 500, rows)):
+        want_q, want_s = R.pack(x[part].cpu().double())
+        assert torch.equal(x8[0].reshape(rows, 128)[part].cpu(), want_q) and torch.equal(x8[1].reshape(1, rows, 4)[:, part].cpu(), want_s)
+        assert torch.equal(back[part].cpu().double(), R.values(want_q, want_s, K))
+
+
 # relative 2-norms.  A rounding to e4m3 is off by 2^-4 at most; roundings along a path add up in squares.  Outputs: tokens, weights, activation, weights
 # again: sqrt(4) 2^-4.  Gradients: those that they multiply (the outputs' share of the activations included), two gradients, two weights: sqrt(9) 2^-4
 TOL_OUT, TOL_GRAD = 2 * 2.0 ** -4, 3 * 2.0 ** -4
