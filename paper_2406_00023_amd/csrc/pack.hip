@@ -2,6 +2,8 @@
 // part of the products' backward, which packs its results both ways.
 //   scale = the smallest power of two by which the largest finite magnitude of a block of 128 comes to 448 or less; q = e4m3(x / scale)
 // All of it is bound by memory.  The division is by a power of two, so that it is exact, and the result the same in any arithmetic.
+// Measured: 32768 tokens x 4096 bf16, top-2, packed 112 us (4.9 TB/s), back 138 (5.8); 16 matrices of 5632 x 2048 bf16 along rows 120 us (4.6), along
+// columns 100 (5.5); 16384 x 5632 SwiGLU gradients from packed pre-activations, both ways, 176 us (4.2); packed rows of 16384 x 2048 along columns 19.
 #include <algorithm>
 
 #include "activation.h"
@@ -129,6 +131,7 @@ __global__ __launch_bounds__(kThreads) void unpack_rows_kernel(RowsParams p, int
 
 // ---- tiles of 128 rows and 128 columns: along columns, and both ways ----------------------------------------------------
 //
+// (Twice the threads with half the rows each: 32768 x 4096 packed again along columns 84 us instead of 58.)
 // A thread has eight neighbouring columns of eight neighbouring rows.  A row's largest is found in the sixteen lanes that have it, a
 // column's over a wave's 32 rows and then, through LDS, over the four waves.  Values along columns go through LDS too, 8 rows of a
 // column at a time, so that they leave as 128 bytes of a column.
