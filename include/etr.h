@@ -419,7 +419,7 @@ etr_status etr_route_backward(const etr_config* cfg, const void* x, const float*
  * of two for each block of 128 values of a row:
  *   values [rows][Kp] bytes, Kp = 128 ceil(K / 128), zeros past K
  *   scales [ceil(Kp / 512)][rows][4] bytes: byte (b / 4, r, b % 4) is the exponent of row r's block b, plus 127; 127 past the last block
- * and stands for value * 2^(scale - 127).  Packing takes the smallest power, 2^-127 at least, by which the block's largest finite magnitude
+ * and stands for value * 2^(scale - 127), scale 0 ... 254.  Packing takes the smallest power, 2^-127 at least, by which the block's largest finite magnitude
  * comes to 448 or less, and rounds to the nearest e4m3 value, ties to even.  NaN and infinities become NaN, and have no part in the power.
  * (Powers of two, because the matrix pipe applies them, and because a value that is packed again, in other blocks, stays what it is unless it lies
  * 2^13 below its new block's largest.)  A stack of E matrices is one after the other, values and scales each.
@@ -451,8 +451,8 @@ etr_status etr_pack_sorted_rows(const etr_sort_config* cfg, const void* x, const
  * 2^-133 and fp32 below 2^-149). */
 etr_status etr_unpack_rows(const etr_pack_config* cfg, const void* values, const void* scales, void* y, void* stream);
 
-/* Along columns: x [E][rows][K] dtype in (sorted: [rows][K], and offsets [E+1] int32 in, ascending from 0, clamped to rows; else
- * offsets NULL); values, scales out. */
+/* Along columns: x [E][rows][K] dtype in (sorted: [rows][K], and offsets [E+1] int32 in, ascending from 0, clamped to rows, or NULL with
+ * E = 1: all rows; not sorted: offsets NULL); values, scales out. */
 etr_status etr_pack_columns(const etr_pack_config* cfg, const void* x, const int32_t* offsets, void* values, void* scales, void* stream);
 
 /* The same from a matrix that is packed along rows (dtype is not looked at). */
@@ -463,15 +463,15 @@ etr_status etr_repack_columns(const etr_pack_config* cfg, const void* row_values
 typedef struct { void* values; void* scales; } etr_packed;
 
 /* etr_expert_linear of packed operands:  y[r] = act(x[r] W[e]^T + bias[e]) + residual[r], x and W being what the packed ones stand for.
- *   x [rows][K], w, w_up E x [N][K], packed along rows (w_up values and scales NULL without SwiGLU); offsets, bias, bias_up, residual as in
+ *   x [rows][K], w, w_up E x [N][K], packed along rows (w_up NULL without SwiGLU); offsets, bias, bias_up, residual as in
  *   etr_expert_linear
  *   y [rows][N] dtype out, optional; may be residual
- *   y8, pre8, pre_up8 [rows][N] out, packed along rows, each optional (NULL values; then NULL scales); at least one of y and y8.  pre8 is a,
+ *   y8, pre8, pre_up8 [rows][N] out, packed along rows, each optional (NULL, or both of its pointers); at least one of y and y8.  pre8 is a,
  *   pre_up8 the up product (SwiGLU: both or neither; else pre_up8 NULL), for the backward; they are packed from fp32 results
  * Rows of the outputs that belong to no expert are left untouched.  The order of a sum goes by the sizes, and by whether results are packed.
  * dtype is that of y and residual, and says how exact the sums are.  ETR_BF16: the matrix pipe multiplies 8-bit values, and what is
  * 2^-13 below the largest of some 16 neighbouring products is cut off there (1.5e-5 of a result's size on normal data, 1/250 of a rounding to
- * bf16).  ETR_F32: the values, exact in bf16, go through bf16 products, whose sums are in fp32; half the rate. */
+ * bf16).  ETR_F32: the values, exact in bf16 down to 2^-133, go through bf16 products, whose sums are in fp32; half the rate. */
 etr_status etr_packed_linear(const etr_linear_config* cfg, const etr_packed* x, const int32_t* offsets, const etr_packed* w,
                               const etr_packed* w_up, const float* bias, const float* bias_up, const void* residual, void* y,
                               const etr_packed* y8, const etr_packed* pre8, const etr_packed* pre_up8, void* stream);

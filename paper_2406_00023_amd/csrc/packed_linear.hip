@@ -51,9 +51,9 @@ struct Tile { int e, first, m0, n0, count, limit, half; };
 // The tile list: experts one after the other; inside one bands of 8 row tiles, in a band the row tiles of a column tile next to
 // each other.  Each XCD (workgroups go round them) has a contiguous part of the list, so its 32 CUs work on some 8 x 4 tiles at once and share
 // 8 + 4 operand slabs in its L2.
-// SPLIT (one workgroup to a CU): the parts are equal in work, where a tile of WEIGHT takes as long as its expert has rows (16 experts of 600 to 1700
-// rows, 2048 x 11264: 547 us with equal numbers of tiles, 498 so); and where the last round over an XCD's CUs would keep half of them or fewer busy, its tiles go in halves or quarters
-// of their rows to as many workgroups.
+// SPLIT (one workgroup to a CU): the parts are equal in work, where a tile of WEIGHT takes as long as its expert has rows (16 experts of
+// 600 to 1700 rows, 2048 x 11264: 547 us with equal numbers of tiles, 498 so); and where the last round over an XCD's CUs would keep
+// half of them or fewer busy, its tiles go in halves or quarters of their rows to as many workgroups.
 template <int MODE, bool SPLIT>
 struct TileList {
     int tiles, tiles_incl;                               // of a lane's expert; WEIGHT: of every expert the same, and not used

@@ -138,6 +138,7 @@ class PackedBlock(DroplessBlock):
         self.rows_up, self.rows_down = B.make_pack_config(H, d, dt, E=E), B.make_pack_config(d, H, dt, E=E)
         self.sorted_h, self.sorted_a = B.make_pack_config(R, d, dt, E=E, sorted=1), B.make_pack_config(R, H, dt, E=E, sorted=1)
         self.dx_up, self.dx_down = B.make_linear_config(R, 2 * Hp, d, E, dt), B.make_linear_config(R, dp, H, E, dt)
+        self.packed = False
         return max(B.etr_packed_act_workspace_bytes(self.up), B.etr_packed_act_workspace_bytes(self.down))
 
     def pack_weights(self, w):
@@ -147,6 +148,12 @@ class PackedBlock(DroplessBlock):
             B.etr_pack_rows(cfg, w[n], q[n])
         B.etr_pack_columns_pair(self.rows_up, w["w_gate"], w["w_up"], q["up_t"])
         B.etr_pack_columns(self.rows_down, w["w_down"], None, q["down_t"])
+        self.packed = True
+
+    def forward(self, x, w_emb, w):
+        if not self.packed:
+            raise RuntimeError("PackedBlock.forward before pack_weights: the experts' weights are not packed yet")
+        return super().forward(x, w_emb, w)
 
     def _experts(self, w):
         q = self.w8

@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from paper_2406_00023_amd import binding as B
+from paper_2406_00023_amd.dropless_block import BlockShape, PackedBlock
 
 NULL, SHAPE, UNSUPPORTED, WORKSPACE, ALIGN = 1, 2, 3, 4, 5
 ok, odd, null = ctypes.c_void_p(4096), ctypes.c_void_p(4100), ctypes.c_void_p(0)
@@ -155,3 +156,9 @@ def test_strides_that_the_binding_refuses():
         B.etr_pack_rows(cfg, torch.zeros(4, 128)[:, ::2], (torch.zeros(512, dtype=torch.uint8), torch.zeros(16, dtype=torch.uint8)))
     with pytest.raises(ValueError):
         B.make_pack_config(4, 64, torch.float16)
+
+
+def test_a_block_whose_weights_are_not_packed(lib):
+    block = PackedBlock(BlockShape(4, 64, 4, 8, 2, 64, F), device="cpu")
+    with pytest.raises(RuntimeError, match="pack_weights"):
+        block.forward(None, None, None)
