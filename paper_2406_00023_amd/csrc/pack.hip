@@ -280,7 +280,8 @@ struct EightPacked {
 template <> struct Eight<FROM_PACKED> : EightPacked {};
 
 // ACT (an etr_act): dy in `x`, the packed pre-activations in q and s
-template <int SOURCE, int ACT>
+// SPLIT: few tiles, whose latency counts: workgroups of their own (blockIdx.y) for each direction and, with SwiGLU, for each half.
+template <int SOURCE, int ACT, bool SPLIT>
 __global__ __launch_bounds__(kThreads, 2) void pack_tiles_kernel(TileParams p) {
     __shared__ TileLds lds;
     const int tid = threadIdx.x, cg = tid & 15, rg = tid >> 4;
@@ -298,7 +299,10 @@ __global__ __launch_bounds__(kThreads, 2) void pack_tiles_kernel(TileParams p) {
     const bool nothing = direct && n_rows <= 0;          // an expert without rows: zeros for its sums, and no block
     constexpr bool FAST = SOURCE == FROM_BF16;           // (of the exponential's rounding 8 bits show nothing)
     constexpr bool GLU = ACT == ETR_ACT_SWIGLU;
-    constexpr int n_halves = GLU ? 2 : 1;
+    constexpr int n_halves = GLU ? 2 : 1, parts = SPLIT ? 1 : n_halves;                     // parts: halves at a time
+    const int half = SPLIT ? blockIdx.y % n_halves : 0;
+    const bool along_rows = !SPLIT || static_cast<int>(blockIdx.y) < n_halves, along_columns = !SPLIT || !along_rows;
+    if (SPLIT && !(along_rows ? p.row_q || p.part || direct : p.column_q != nullptr)) return;
 
     // everything is requested before the first is used; past the ends the last row or columns again, which count as zeros
     Eight<SOURCE> from[8];
@@ -319,7 +323,7 @@ __global__ __launch_bounds__(kThreads, 2) void pack_tiles_kernel(TileParams p) {
             if constexpr (GLU) up[i].load(p.q[1], p.s[1], pitch, row, cc, 0, row, p.rows);
         }
     }
-    float v[n_halves][8][8];
+    float v[parts][8][8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         float (&d)[8] = v[0][i];
@@ -335,8 +339,10 @@ __global__ __launch_bounds__(kThreads, 2) void pack_tiles_kernel(TileParams p) {
                     d[j] *= normal_cdf<FAST>(a[j]) + a[j] * 0.39894228040143268f * (FAST ? __expf(-0.5f * a[j] * a[j]) : gaussian_f32(a[j]));
                 } else {
                     const float sg = sigmoid<FAST>(a[j]), slope = sg * (1.0f + a[j] * (1.0f - sg));
-                    if constexpr (GLU) {
-                        v[n_halves - 1][i][j] = d[j] * (a[j] * sg);
+                    if constexpr (GLU && SPLIT) {
+                        d[j] *= half ? a[j] * sg : b[j] * slope;
+                    } else if constexpr (GLU) {
+                        v[parts - 1][i][j] = d[j] * (a[j] * sg);
                         d[j] *= b[j] * slope;
                     } else {
                         d[j] *= slope;
@@ -346,26 +352,27 @@ __global__ __launch_bounds__(kThreads, 2) void pack_tiles_kernel(TileParams p) {
         }
         if (rg * 8 + i >= n_rows || c >= p.K) {
 #pragma unroll
-            for (int h = 0; h < n_halves; ++h)
+            for (int u = 0; u < parts; ++u)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[h][i][j] = 0.f;
+                for (int j = 0; j < 8; ++j) v[u][i][j] = 0.f;
         }
         __builtin_amdgcn_sched_barrier(0);               // one row at a time: keeps the live set small
     }
 #pragma unroll
-    for (int h = 0; h < n_halves; ++h) {
-        if (p.row_q && !nothing) pack_tile_rows(v[h], p.row_q, p.row_pitch, p.row_s, h * per_half + nb, h == n_halves - 1 && nb == per_half - 1, first, n_rows, p.rows);
-        if (p.part || direct) {
+    for (int u = 0; u < parts; ++u) {
+        const int h = half + u;
+        if (p.row_q && along_rows && !nothing) pack_tile_rows(v[u], p.row_q, p.row_pitch, p.row_s, h * per_half + nb, h == n_halves - 1 && nb == per_half - 1, first, n_rows, p.rows);
+        if (along_rows && (p.part || direct)) {
             float* out = direct ? p.sums[h] + static_cast<size_t>(e) * p.K : p.part + (static_cast<size_t>(h) * p.chunks + chunk) * p.K;
-            tile_sums(v[h], lds, out, c0, p.K);
+            tile_sums(v[u], lds, out, c0, p.K);
         }
-        if (p.column_q && !nothing) {
+        if (p.column_q && along_columns && !nothing) {
             if (p.half_blocks) {                         // a pair of stacks: the matrix has 2 half_blocks blocks
                 const int all = 2 * p.half_blocks, at = p.half * p.half_blocks + block;
-                pack_tile_columns(v[h], lds, p.column_q + static_cast<size_t>(e) * p.K * all * kBlock, static_cast<size_t>(all) * kBlock,
+                pack_tile_columns(v[u], lds, p.column_q + static_cast<size_t>(e) * p.K * all * kBlock, static_cast<size_t>(all) * kBlock,
                                   p.column_s + static_cast<size_t>(e) * ((all + 3) / 4) * p.K * 4, at, at == all - 1, c0, p.K, p.K, 0);
             } else {
-                pack_tile_columns(v[h], lds, p.column_q + static_cast<size_t>(blocks_before) * kBlock * p.column_rows, static_cast<size_t>(blocks) * kBlock,
+                pack_tile_columns(v[u], lds, p.column_q + static_cast<size_t>(blocks_before) * kBlock * p.column_rows, static_cast<size_t>(blocks) * kBlock,
                                   p.column_s + static_cast<size_t>(groups_before) * 4 * p.column_rows, block, block == blocks - 1, c0, p.K, p.column_rows,
                                   h * p.K);
             }
@@ -426,7 +433,17 @@ int chunks_at_most(int rows, int E, bool stacked) { return stacked ? E * blocks_
 
 template <int SOURCE, int ACT>
 hipError_t launch_tiles(const TileParams& p, int chunks, hipStream_t st) {
-    hipLaunchKernelGGL((pack_tiles_kernel<SOURCE, ACT>), dim3(static_cast<unsigned>(blocks_of(p.K)) * chunks), dim3(kThreads), 0, st, p);
+    const unsigned tiles = static_cast<unsigned>(blocks_of(p.K)) * chunks;
+    // A tile for each direction and half once a tile of all leaves half of the CUs idle; chip filled, what they compute twice costs more.  us, of all / split:
+    // SwiGLU bf16 44 tiles 13.9 / 9.1, 130 14.4 / 11.2, 304 15.5 / 17.5; SiLU 44 8.9 / 7.4, 165 9.3 / 9.5; GELU fp32 110 11.6 / 10.1, 165 11.8 / 13.6
+    if constexpr (SOURCE != FROM_PACKED) {
+        const bool both = (p.row_q || p.part || p.sums[0]) && p.column_q;
+        if (2ll * tiles <= cu_count() && (ACT == ETR_ACT_SWIGLU || both)) {
+            hipLaunchKernelGGL((pack_tiles_kernel<SOURCE, ACT, true>), dim3(tiles, ACT == ETR_ACT_SWIGLU ? 4 : 2), dim3(kThreads), 0, st, p);
+            return hipGetLastError();
+        }
+    }
+    hipLaunchKernelGGL((pack_tiles_kernel<SOURCE, ACT, false>), dim3(tiles), dim3(kThreads), 0, st, p);
     return hipGetLastError();
 }
 

@@ -6,6 +6,7 @@ import torch
 import operator_refs as O
 import packed_refs as R
 from paper_2406_00023_amd import binding as B
+from test_gpu_packed_backward import act_case
 from test_gpu_packed_linear import ACTS, DT, gpu, operand, sum_error
 
 pytestmark = pytest.mark.gpu
@@ -82,6 +83,38 @@ def test_one_expert_without_a_table(rows):
         runs.append([*xt8, *again8, *d8, *dt8, dbias, dw])
     assert all(torch.equal(a, b) for a, b in zip(*runs))
     assert float(runs[0][-1].float().abs().max()) > 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["none", "silu", "gelu", "swiglu"])
+@pytest.mark.parametrize("counts,N,bias", [([1000, 0, 700, 1], 1160, True), ([128, 1, 129], 264, False), ([40, 0, 88], 136, True)])
+def test_few_tiles_and_many_of_the_element_wise_part(counts, N, bias, act, dtype):
+    """A tile's directions and halves go to workgroups of their own as long as half of a chip of 256 CUs is idle otherwise."""
+    act_case(counts, N, dtype, act, seed=N, bias=bias)
+
+
+@pytest.mark.parametrize("act", ["none", "swiglu"])
+@pytest.mark.parametrize("rows,N", [(300, 264), (2100, 1160)])
+def test_some_of_the_gradients(rows, N, act):
+    """Each result of the element-wise part by itself is what it is beside the others."""
+    E, dt, n = 3, torch.bfloat16, 2 if act == "swiglu" else 1
+    offsets = torch.tensor([0, rows // 2, rows // 2, rows - 5], dtype=torch.int32, device="cuda")
+    dy, pre = O.randn(1, rows, N, dtype=dt).cuda(), [gpu(operand(2 + i, rows, N)) if act == "swiglu" else None for i in range(2)]
+    cfg = B.make_linear_config(rows, 64, N, E, dt, act=ACTS[act])
+    ws = B.alloc_workspace(B.etr_packed_act_workspace_bytes(cfg))
+
+    def call(along_rows, along_columns, sums):
+        got = {"d8": B.alloc_packed_rows(B.make_pack_config(rows, n * R.blocks(N) * 128, dt)) if along_rows else None,
+               "dt8": B.alloc_packed_columns(B.make_pack_config(rows, n * N, dt, E=E, sorted=1)) if along_columns else None}
+        for i, name in enumerate(("dbias", "dbias_up")[:n]):
+            got[name] = torch.full((E, N), 3.0, device="cuda") if sums else None
+        B.etr_packed_act_backward(cfg, dy, offsets, ws, pre8=pre[0], pre_up8=pre[1], **got)
+        return {k: v if isinstance(v, tuple) else (v,) for k, v in got.items() if v is not None}
+
+    whole = call(True, True, True)
+    for asked in ((True, False, False), (False, True, False), (False, False, True), (True, True, False), (False, True, True), (True, False, True)):
+        for k, v in call(*asked).items():
+            assert all(torch.equal(a, b) for a, b in zip(v, whole[k])), (asked, k)
 
 
 def test_two_calls_at_once():
