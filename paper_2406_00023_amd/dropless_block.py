@@ -18,6 +18,7 @@ from __future__ import annotations
 from dataclasses import dataclass
 
 import torch
+from torch.multiprocessing.reductions import StorageWeakRef
 
 from . import binding as B
 from . import inputs as I
@@ -116,8 +117,20 @@ class DroplessBlock:
         return self.dx
 
 
+EXPERT_WEIGHTS = ("w_gate", "w_up", "w_down")
+
+
+def _identity(t: torch.Tensor):
+    """Whose memory a tensor looks at, which part of it, and how often torch has changed that in place.  (The weak reference keeps the memory's
+    number from being given to another one.)"""
+    return StorageWeakRef(t.untyped_storage()), t.storage_offset(), t.shape, t.dtype, None if t.is_inference() else t._version
+
+
 class PackedBlock(DroplessBlock):
-    """The block with the experts in 8 bits.  pack_weights has to follow every change of the weights."""
+    """The block with the experts in 8 bits.  Its products take the weights as pack_weights last packed them, forward and backward, so that it has to
+    follow every change of the experts' weights.  forward refuses experts' weights that are not what was packed: other tensors, or the same ones after an
+    operation of torch in place.  What torch does not count it cannot see (a replayed graph, `.data`, inference tensors, writes through an address).
+    A caller who keeps the packed weights only leaves the experts' out of w."""
 
     def _prepare_experts(self, device):
         s, R, E, d, H, dt = self.s, self.s.T * self.s.k, self.s.E, self.s.d, self.s.H, self.s.dtype
@@ -138,21 +151,25 @@ class PackedBlock(DroplessBlock):
         self.rows_up, self.rows_down = B.make_pack_config(H, d, dt, E=E), B.make_pack_config(d, H, dt, E=E)
         self.sorted_h, self.sorted_a = B.make_pack_config(R, d, dt, E=E, sorted=1), B.make_pack_config(R, H, dt, E=E, sorted=1)
         self.dx_up, self.dx_down = B.make_linear_config(R, 2 * Hp, d, E, dt), B.make_linear_config(R, dp, H, E, dt)
-        self.packed = False
+        self.packed = None                                     # the weights that are packed, by name; they only say what forward refuses
         return max(B.etr_packed_act_workspace_bytes(self.up), B.etr_packed_act_workspace_bytes(self.down))
 
     def pack_weights(self, w):
         """The experts' weights along rows, for the forward products, and along columns, for their input's gradients."""
+        self.packed = None                                     # (until all of them are)
         q = self.w8
         for n, cfg in (("w_gate", self.rows_up), ("w_up", self.rows_up), ("w_down", self.rows_down)):
             B.etr_pack_rows(cfg, w[n], q[n])
         B.etr_pack_columns_pair(self.rows_up, w["w_gate"], w["w_up"], q["up_t"])
         B.etr_pack_columns(self.rows_down, w["w_down"], None, q["down_t"])
-        self.packed = True
+        self.packed = {n: _identity(w[n]) for n in EXPERT_WEIGHTS}
 
     def forward(self, x, w_emb, w):
-        if not self.packed:
+        if self.packed is None:
             raise RuntimeError("PackedBlock.forward before pack_weights: the experts' weights are not packed yet")
+        for n in EXPERT_WEIGHTS:
+            if n in w and _identity(w[n]) != self.packed[n]:
+                raise RuntimeError(f"PackedBlock.forward: {n} is not what pack_weights has packed, or has changed since; pack it again")
         return super().forward(x, w_emb, w)
 
     def _experts(self, w):
