@@ -166,11 +166,6 @@ template <int N> __device__ __forceinline__ void wait_copies() {
     __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0F70);
     asm volatile("" ::: "memory");
 }
-// what stands before it, memory operations and MFMAs, stays there
-__device__ __forceinline__ void fence() {
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-}
 // this wave's reads of LDS are done
 __device__ __forceinline__ void wait_reads() {
     asm volatile("" ::: "memory");
