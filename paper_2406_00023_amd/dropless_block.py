@@ -130,7 +130,14 @@ class PackedBlock(DroplessBlock):
     """The block with the experts in 8 bits.  Its products take the weights as pack_weights last packed them, forward and backward, so that it has to
     follow every change of the experts' weights.  forward refuses experts' weights that are not what was packed: other tensors, or the same ones after an
     operation of torch in place.  What torch does not count it cannot see (a replayed graph, `.data`, inference tensors, writes through an address).
-    A caller who keeps the packed weights only leaves the experts' out of w."""
+    A caller who keeps the packed weights only leaves the experts' out of w.
+
+    exact_sums: the product whose results are packed (pre-activations and activation) sums in fp32 also in a bf16 block, at half the rate of the 8-bit
+    matrix pipe.  Without it some 1 in 600 to 1200 of these values, next to a tie, is packed a step of e4m3 away from the nearest."""
+
+    def __init__(self, s: BlockShape, device="cuda", exact_sums: bool = False):
+        self.exact_sums = exact_sums
+        super().__init__(s, device)
 
     def _prepare_experts(self, device):
         s, R, E, d, H, dt = self.s, self.s.T * self.s.k, self.s.E, self.s.d, self.s.H, self.s.dtype
@@ -151,6 +158,7 @@ class PackedBlock(DroplessBlock):
         self.rows_up, self.rows_down = B.make_pack_config(H, d, dt, E=E), B.make_pack_config(d, H, dt, E=E)
         self.sorted_h, self.sorted_a = B.make_pack_config(R, d, dt, E=E, sorted=1), B.make_pack_config(R, H, dt, E=E, sorted=1)
         self.dx_up, self.dx_down = B.make_linear_config(R, 2 * Hp, d, E, dt), B.make_linear_config(R, dp, H, E, dt)
+        self.up_packing = B.make_linear_config(R, d, H, E, torch.float32 if self.exact_sums else dt, act=B.ACT_SWIGLU)
         self.packed = None                                     # the weights that are packed, by name; they only say what forward refuses
         return max(B.etr_packed_act_workspace_bytes(self.up), B.etr_packed_act_workspace_bytes(self.down))
 
@@ -175,7 +183,7 @@ class PackedBlock(DroplessBlock):
     def _experts(self, w):
         q = self.w8
         B.etr_pack_sorted_rows(self.sort, self.h, self.row_of, self.hs8)
-        B.etr_packed_linear(self.up, self.hs8, self.offsets, q["w_gate"], w_up8=q["w_up"], y8=self.a8, pre8=self.pre8, pre_up8=self.pre_up8)
+        B.etr_packed_linear(self.up_packing, self.hs8, self.offsets, q["w_gate"], w_up8=q["w_up"], y8=self.a8, pre8=self.pre8, pre_up8=self.pre_up8)
         B.etr_packed_linear(self.down, self.a8, self.offsets, q["w_down"], y=self.ys)
 
     def _experts_backward(self, w):
