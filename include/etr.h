@@ -470,8 +470,10 @@ typedef struct { void* values; void* scales; } etr_packed;
  *   pre_up8 the up product (SwiGLU: both or neither; else pre_up8 NULL), for the backward; they are packed from fp32 results
  * Rows of the outputs that belong to no expert are left untouched.  The order of a sum goes by the sizes, and by whether results are packed.
  * dtype is that of y and residual, and says how exact the sums are.  ETR_BF16: the matrix pipe multiplies 8-bit values, and what is
- * 2^-13 below the largest of some 16 neighbouring products is cut off there (1.5e-5 of a result's size on normal data, 1/250 of a rounding to
- * bf16).  ETR_F32: the values, exact in bf16 down to 2^-133, go through bf16 products, whose sums are in fp32; half the rate. */
+ * 2^-13 below the largest of some 16 neighbouring products is cut off there (1.5e-5 of a result's size on normal data), which a rounding to
+ * bf16 covers.  Packed results go without that rounding: 1 in 600 to 1200 of them, next to a tie, is a step of e4m3 away from the nearest.  ETR_F32: the
+ * values, exact in bf16 down to 2^-133, go through bf16 products, whose sums are in fp32; half the rate.  With packed results alone (y and
+ * residual NULL) the caller is free to choose. */
 etr_status etr_packed_linear(const etr_linear_config* cfg, const etr_packed* x, const int32_t* offsets, const etr_packed* w,
                               const etr_packed* w_up, const float* bias, const float* bias_up, const void* residual, void* y,
                               const etr_packed* y8, const etr_packed* pre8, const etr_packed* pre_up8, void* stream);

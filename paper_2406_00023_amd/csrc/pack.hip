@@ -26,8 +26,9 @@ struct RowsParams {
     int K, blocks, groups;
     int walkers;            // rows that are under way at once
 };
-// Steps of 512 columns that a wave has on their way at once: 4, or 1 where that leaves CUs without a wave (32 tokens x 2048, top-2: 4.3 and 3.2 us).
-// A row's parts go to neighbouring waves, which walk the rows together.
+// Steps of 512 columns of a wave: 4, or 1 where that leaves CUs without a wave (32 tokens x 2048, top-2: packed in 4.4 and 2.9 us, back in 3.2 and 2.4).
+// All four are on their way at once but in packing from bf16, whose conversion stands behind the bound of its load, with a wait for it: there a CU's
+// other waves are what hides the latency (4.6 TB/s).  A row's parts go to neighbouring waves, which walk the rows together.
 
 template <bool BF16>
 __device__ __forceinline__ void load8(const void* x, size_t at, float (&f)[8]) {
@@ -297,7 +298,9 @@ __global__ __launch_bounds__(kThreads, 2) void pack_tiles_kernel(TileParams p) {
     const int n_rows = min(kBlock, __builtin_amdgcn_readlane(g.count, e) - block * kBlock);
     const size_t first = static_cast<size_t>(__builtin_amdgcn_readlane(g.first, e)) + static_cast<size_t>(block) * kBlock;
     const bool nothing = direct && n_rows <= 0;          // an expert without rows: zeros for its sums, and no block
-    constexpr bool FAST = SOURCE == FROM_BF16;           // (of the exponential's rounding 8 bits show nothing)
+    // FAST: the exponential's exponent without its lower part, a term off by some (|a| + 4) 2^-24 of its size.  Far below what dy's own rounding to
+    // bf16 (2^-8) has left open, for the packed results and for the sums over rows alike; the sums have these terms' errors, beside their own in fp32.
+    constexpr bool FAST = SOURCE == FROM_BF16;
     constexpr bool GLU = ACT == ETR_ACT_SWIGLU;
     constexpr int n_halves = GLU ? 2 : 1, parts = SPLIT ? 1 : n_halves;                     // parts: halves at a time
     const int half = SPLIT ? blockIdx.y % n_halves : 0;
@@ -339,7 +342,7 @@ __global__ __launch_bounds__(kThreads, 2) void pack_tiles_kernel(TileParams p) {
                     d[j] *= normal_cdf<FAST>(a[j]) + a[j] * 0.39894228040143268f * (FAST ? __expf(-0.5f * a[j] * a[j]) : gaussian_f32(a[j]));
                 } else {
                     const float sg = sigmoid<FAST>(a[j]), slope = sg * (1.0f + a[j] * (1.0f - sg));
-                    if constexpr (GLU && SPLIT) {
+                    if constexpr (GLU && SPLIT) {        // (compiled to uniform branches, 16 to a row of eight)
                         d[j] *= half ? a[j] * sg : b[j] * slope;
                     } else if constexpr (GLU) {
                         v[parts - 1][i][j] = d[j] * (a[j] * sg);
@@ -435,7 +438,9 @@ template <int SOURCE, int ACT>
 hipError_t launch_tiles(const TileParams& p, int chunks, hipStream_t st) {
     const unsigned tiles = static_cast<unsigned>(blocks_of(p.K)) * chunks;
     // A tile for each direction and half once a tile of all leaves half of the CUs idle; chip filled, what they compute twice costs more.  us, of all / split:
-    // SwiGLU bf16 44 tiles 13.9 / 9.1, 130 14.4 / 11.2, 304 15.5 / 17.5; SiLU 44 8.9 / 7.4, 165 9.3 / 9.5; GELU fp32 110 11.6 / 10.1, 165 11.8 / 13.6
+    // SwiGLU bf16 44 tiles 13.9 / 9.1, 130 14.4 / 11.2, 304 15.5 / 17.5; SiLU 44 8.9 / 7.4, 165 9.3 / 9.5; GELU fp32 110 11.6 / 10.1, 165 11.8 / 13.6.
+    // One border for all, where SiLU and GELU have theirs; SwiGLU's lies between 130 and 304 tiles, so that from 129 tiles up to there it takes some 3 us longer
+    // than split.
     if constexpr (SOURCE != FROM_PACKED) {
         const bool both = (p.row_q || p.part || p.sums[0]) && p.column_q;
         if (2ll * tiles <= cu_count() && (ACT == ETR_ACT_SWIGLU || both)) {

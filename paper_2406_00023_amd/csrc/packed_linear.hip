@@ -5,8 +5,12 @@
 // Every operand is rows of whole 128-byte blocks, padded with zeros, so that every product is C[m][n] = sum_k A(m, k) B(n, k) with both
 // contractions contiguous, and a k-tile is one block: 128 bytes and one scale for each row of a tile.
 // Results in bf16: the scaled MFMA, 32 x 32 x 64 8-bit values, takes the bytes and the scales as they are.  It cuts products off 2^-13 below the
-// largest of some 16 neighbours (measured: 1.5e-5 of a result's size on normal data).  Results in fp32 go without it: the values are
-// converted to bf16, which holds them and their scale exactly, and multiplied there, with sums in fp32 (6e-8).
+// largest of some 16 neighbours, which is less than sums in fp32 keep (measured: 1.5e-5 of a result's size on normal data; 1.6e-4, all to one side, where one
+// value of every block is 100 times the others).  A rounding to bf16 (2^-8) covers it.  Packed results are not rounded to bf16: of theirs 1 in 600 to 1200
+// lies so near a tie that it goes to the other side, 1e-3 off in norm from what is nearest (sums in fp32: 1e-4), and as far from the unrounded
+// results as those (2.65e-2).  Chosen for the rate: 32768 x 4096 x 1408 SwiGLU with everything kept packed 455 us, with sums in fp32 691.
+// Results in fp32 go without it: the values are converted to bf16, which holds them and their scale exactly, and multiplied there, with
+// sums in fp32 (6e-8); so do packed results by themselves where the type says fp32.
 //
 // Bound by the matrix pipe where an expert has a few hundred rows (there: by the power that it draws), by the weights' bytes where it has a
 // few, by latency in between.  Measured, bf16: 8192 cubed 440 us (2.5 PFLOP/s; a library product 2.6); 16 experts, SwiGLU of 2048 x 5632, 16 384 uneven rows 395 us
@@ -658,8 +662,11 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void packed_tiles_kernel(PackedPara
 // ---- few rows ----------------------------------------------------------------------------------------------------------
 //
 // 16 rows x 16 NW output columns to a workgroup: waves with 16 columns each (SwiGLU: 16 gate and 16 up), KS of them to share a
-// contraction, stream their weight rows straight into registers, a 16 x 16 x 128 MFMA to a k-tile.  Bound by the weights' bytes.  A lane has row
+// contraction, stream their weight rows straight into registers, a 16 x 16 x 128 MFMA to a k-tile.  A lane has row
 // lane % 16 of a block and 16 bytes out of each half of the k-tile, so that a load takes 64 bytes of a row.
+// Bound by the weights' bytes where a CU has waves enough (64 rows in 16 groups, 2048 x 5632 SwiGLU 65 us, 5.7 TB/s).  Else by latency: the branch at the
+// contraction's end lets the compiler move each k-tile's loads down to their MFMA, so that a wave has one k-tile on its way, not the four that are
+// written beside each other (32 rows in 8 groups, 4096 x 1408 SwiGLU, packed results: 39 us).
 // PACK: results are packed too, which takes a workgroup with all 128 columns of a block.
 template <bool WIDE, int NW, int KS, bool GLU, bool PACK>
 __global__ __launch_bounds__(64 * NW * KS, NW * KS > 8 ? 4 : 2) void packed_rows_kernel(PackedParams p) {
@@ -690,7 +697,7 @@ __global__ __launch_bounds__(64 * NW * KS, NW * KS > 8 ? 4 : 2) void packed_rows
         f32x4 acc[NG];
 #pragma unroll
         for (int h = 0; h < NG; ++h) acc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
-        // four k-tiles, whose scales are a dword, at a time; a group of waves takes every KS-th four
+        // four k-tiles, whose scales are a dword, in turn; a group of waves takes every KS-th four
         for (int g = group; g < G; g += KS) {
             const uint32_t sa = as[static_cast<size_t>(g) * p.rows];
             uint32_t sb[NG];
@@ -710,7 +717,7 @@ __global__ __launch_bounds__(64 * NW * KS, NW * KS > 8 ? 4 : 2) void packed_rows
             }
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                if (4 * g + u >= p.blocks) break;        // (uniform)
+                if (4 * g + u >= p.blocks) break;        // (uniform; this k-tile's loads end up behind it)
                 const uint32_t xa = (sa >> (8 * u)) & 255u;
                 if constexpr (!WIDE) {
                     const v8i x{fa[u][0][0], fa[u][0][1], fa[u][0][2], fa[u][0][3], fa[u][1][0], fa[u][1][1], fa[u][1][2], fa[u][1][3]};
@@ -834,7 +841,10 @@ hipError_t launch_rows(PackedParams p, hipStream_t st) {
 enum class Form { ROWS16, ROWS32, ROWS128, T32, T64, T128, T256 };
 struct Choice { Form form; double us; };
 // Microseconds: rounds of tiles over the places that they have on the chip, each a time per k-tile (alone ... chip full) and a time besides; and the
-// weights' bytes at 5 TB/s at least.  ROWS: the weights' bytes for every 16 rows, at 5.5 TB/s.  (bf16; fp32 takes longer with all of them.)  Measured, us, in this order:
+// weights' bytes at 5 TB/s at least.  ROWS: the weights' bytes for every 16 rows, at 5.5 TB/s.  (bf16; fp32 takes longer with all of them.)
+// What it leaves out: the rows' bytes and a workgroup's own time in ROWS, so that many rows of few columns go there (2^20 rows, K = 128: N = 32
+// 181 us, N = 64, in tiles, 77); how uneven the groups are, since it goes by the average; and a contraction is never shared between
+// workgroups, so that the weights' gradient of few tiles takes as long as its rows (32768 rows, 128 x 128 131 us, 1024 x 1024 136).  Measured, us, in this order:
 // ROWS16 / 32, T32, T64, T128, T256 (SwiGLU without T128):
 //   18 rows dense, 3840 x 1472          6.3  9.5                       2048 in 16 groups, 5632 x 2048         59   57   42   48
 //   96 in 4, 2816 x 1024               10.3 12.6  12.0 14.6 18.2 24.8  4096 in 16, 2048 x 2048                44   37   34   30
@@ -881,7 +891,7 @@ Choice choose_form(const PackedParams& p, bool packs) {
     offer_tiles(Form::T32, 32, 128);
     if (MODE != WEIGHT) {
         const double bytes = weights * row_tiles(16), us = 3.5 + bytes / 5.5e6;
-        // (a CU alone takes in 27 KB a microsecond)
+        // (a CU takes in 27 KB a microsecond in that loop, one k-tile of each wave on its way)
         if (packs) offer(Form::ROWS128, std::max(us, 3.5 + std::ceil(groups * row_tiles(16) * blocks_of(p.N) / cu_count()) * kBlock * p.blocks * kBlock * (GLU ? 2 : 1) / 27e3));
         else offer(groups * row_tiles(16) * p.N / 16 < 2048 ? Form::ROWS16 : Form::ROWS32, us);
     }
