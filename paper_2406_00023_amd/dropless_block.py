@@ -15,10 +15,10 @@ what a step keeps for its backward (the sorted tokens, the pre-activations, the 
 """
 from __future__ import annotations
 
+import weakref
 from dataclasses import dataclass
 
 import torch
-from torch.multiprocessing.reductions import StorageWeakRef
 
 from . import binding as B
 from . import inputs as I
@@ -120,10 +120,19 @@ class DroplessBlock:
 EXPERT_WEIGHTS = ("w_gate", "w_up", "w_down")
 
 
-def _identity(t: torch.Tensor):
-    """Whose memory a tensor looks at, which part of it, and how often torch has changed that in place.  (The weak reference keeps the memory's
-    number from being given to another one.)"""
-    return StorageWeakRef(t.untyped_storage()), t.storage_offset(), t.shape, t.dtype, None if t.is_inference() else t._version
+class _Source:
+    """Which tensor was packed: the memory that it looks at (not kept alive), which part of it, and how often torch has changed that in place."""
+
+    def __init__(self, t: torch.Tensor):
+        self.memory, self.rest = weakref.ref(t.untyped_storage()), self._rest(t)
+
+    @staticmethod
+    def _rest(t):
+        return t.storage_offset(), t.shape, t.dtype, None if t.is_inference() else t._version
+
+    def __call__(self, t: torch.Tensor) -> bool:
+        """Whether t is that tensor, unchanged."""
+        return self.memory() is t.untyped_storage() and self.rest == self._rest(t)
 
 
 class PackedBlock(DroplessBlock):
@@ -170,13 +179,17 @@ class PackedBlock(DroplessBlock):
             B.etr_pack_rows(cfg, w[n], q[n])
         B.etr_pack_columns_pair(self.rows_up, w["w_gate"], w["w_up"], q["up_t"])
         B.etr_pack_columns(self.rows_down, w["w_down"], None, q["down_t"])
-        self.packed = {n: _identity(w[n]) for n in EXPERT_WEIGHTS}
+        self.packed = {n: _Source(w[n]) for n in EXPERT_WEIGHTS}
+
+    def __getstate__(self):
+        """A copy holds the packed weights, and does not know whose they are."""
+        return {**self.__dict__, "packed": self.packed and dict.fromkeys(self.packed)}
 
     def forward(self, x, w_emb, w):
         if self.packed is None:
             raise RuntimeError("PackedBlock.forward before pack_weights: the experts' weights are not packed yet")
         for n in EXPERT_WEIGHTS:
-            if n in w and _identity(w[n]) != self.packed[n]:
+            if n in w and not (self.packed[n] and self.packed[n](w[n])):
                 raise RuntimeError(f"PackedBlock.forward: {n} is not what pack_weights has packed, or has changed since; pack it again")
         return super().forward(x, w_emb, w)
 

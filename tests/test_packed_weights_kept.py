@@ -1,4 +1,8 @@
 """Which weights a packed block computes with: those that were packed last, or none.  On the CPU, with the library's calls left out."""
+import copy
+import gc
+import pickle
+
 import pytest
 import torch
 
@@ -93,3 +97,29 @@ def test_packing_that_failed_leaves_nothing_to_compute_with(block, weights, monk
         block.pack_weights(w)
     with pytest.raises(RuntimeError, match="pack_weights"):
         forward(block, weights)
+
+
+def test_the_weights_are_not_kept_alive(block, weights):
+    w = weights[1]
+    block.pack_weights({n: v.clone() for n, v in w.items()})
+    gc.collect()
+    assert all(block.packed[n].memory() is None for n in EXPERTS)
+    norms = {n: v for n, v in w.items() if n not in EXPERTS}
+    forward(block, (weights[0], norms))
+
+
+@pytest.mark.parametrize("copied", [copy.copy, copy.deepcopy, lambda b: pickle.loads(pickle.dumps(b))], ids=["copy", "deepcopy", "pickle"])
+def test_copies_have_the_packed_weights(block, weights, copied):
+    w = weights[1]
+    with pytest.raises(RuntimeError, match="pack_weights"):
+        forward(copied(block), weights)
+    block.pack_weights(w)
+    block.w8["w_gate"][0].fill_(7)
+    other = copied(block)
+    assert torch.equal(other.w8["w_gate"][0], block.w8["w_gate"][0])
+    forward(other, (weights[0], {n: v for n, v in w.items() if n not in EXPERTS}))
+    with pytest.raises(RuntimeError, match="w_gate"):          # whose they are it cannot say
+        forward(other, weights)
+    other.pack_weights(w)
+    forward(other, weights)
+    forward(block, weights)
