@@ -439,8 +439,7 @@ hipError_t launch_tiles(const TileParams& p, int chunks, hipStream_t st) {
     const unsigned tiles = static_cast<unsigned>(blocks_of(p.K)) * chunks;
     // A tile for each direction and half once a tile of all leaves half of the CUs idle; chip filled, what they compute twice costs more.  us, of all / split:
     // SwiGLU bf16 44 tiles 13.9 / 9.1, 130 14.4 / 11.2, 304 15.5 / 17.5; SiLU 44 8.9 / 7.4, 165 9.3 / 9.5; GELU fp32 110 11.6 / 10.1, 165 11.8 / 13.6.
-    // One border for all, where SiLU and GELU have theirs; SwiGLU's lies between 130 and 304 tiles, so that from 129 tiles up to there it takes some 3 us longer
-    // than split.
+    // One border for all, where SiLU and GELU have theirs; SwiGLU's lies between 130 and 304 tiles, and from 129 up to there it takes longer than split.
     if constexpr (SOURCE != FROM_PACKED) {
         const bool both = (p.row_q || p.part || p.sums[0]) && p.column_q;
         if (2ll * tiles <= cu_count() && (ACT == ETR_ACT_SWIGLU || both)) {

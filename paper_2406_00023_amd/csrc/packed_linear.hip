@@ -666,7 +666,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void packed_tiles_kernel(PackedPara
 // lane % 16 of a block and 16 bytes out of each half of the k-tile, so that a load takes 64 bytes of a row.
 // Bound by the weights' bytes where a CU has waves enough (64 rows in 16 groups, 2048 x 5632 SwiGLU 65 us, 5.7 TB/s).  Else by latency: the branch at the
 // contraction's end lets the compiler move each k-tile's loads down to their MFMA, so that a wave has one k-tile on its way, not the four that are
-// written beside each other (32 rows in 8 groups, 4096 x 1408 SwiGLU, packed results: 39 us).
+// written beside each other (32 rows in 8 groups, 4096 x 1408 SwiGLU, packed results: 39 us; tiles of 32 rows, which take it, 30).
 // PACK: results are packed too, which takes a workgroup with all 128 columns of a block.
 template <bool WIDE, int NW, int KS, bool GLU, bool PACK>
 __global__ __launch_bounds__(64 * NW * KS, NW * KS > 8 ? 4 : 2) void packed_rows_kernel(PackedParams p) {
